@@ -27,31 +27,31 @@ GRAD_SCALE = 0.5                # what gradients are multiplied by before use (l
 def listed():
     return [
         # one token through the first product of a 4,096-channel layer's MLP: serving, bound by the weights
-        linear("linear, one token", "forward", 1, 4096, 16384, "bf16", act="gelu_tanh", bias=True),
+        linear("linear one token", "forward", 1, 4096, 16384, "bf16", act="gelu_tanh", bias=True),
         # a few tokens, ragged sizes: the smallest call, its latency is what counts
-        linear("linear, seven tokens, odd", "forward", 7, 1000, 1037, "f16", act="silu", bias=True, residual=True),
+        linear("linear seven tokens odd", "forward", 7, 1000, 1037, "f16", act="silu", bias=True, residual=True),
         # a micro-batch of 4,096 tokens through the same product, with what its backward pass needs kept
-        linear("linear, 4096 tokens", "forward", 4096, 4096, 16384, "bf16", act="gelu_tanh", bias=True, save=True),
+        linear("linear 4096 tokens", "forward", 4096, 4096, 16384, "bf16", act="gelu_tanh", bias=True, save=True),
         # the second product's gradients: back through the activation, the weights' gradient summed over micro-batches
-        linear("linear gradients, 4096 tokens", "backward", 4096, 16384, 4096, "bf16", act="gelu_tanh", bias=True,
+        linear("linear gradients 4096 tokens", "backward", 4096, 16384, 4096, "bf16", act="gelu_tanh", bias=True,
                accumulate=True),
         # a packed batch of no round length through a narrower layer
-        linear("linear gradients, 1537 tokens", "backward", 1537, 1224, 4904, "f16", act="relu", bias=True, residual=True),
+        linear("linear gradients 1537 tokens", "backward", 1537, 1224, 4904, "f16", act="relu", bias=True, residual=True),
         # one token between two blocks of an 8,192-channel layer: latency
-        norm("norm, one token", "forward", 1, 8192, "bf16", "rms", "rms", scale=True),
+        norm("norm one token", "forward", 1, 8192, "bf16", "rms", "rms", scale=True),
         # a cut's 4,096 tokens of 8,192 channels, norms on both sides of the block
-        norm("norm, 4096 tokens", "forward", 4096, 8192, "bf16", "rms", "rms", rows_per_gate=4096, scale=True),
+        norm("norm 4096 tokens", "forward", 4096, 8192, "bf16", "rms", "rms", rows_per_gate=4096, scale=True),
         # its gradients
-        norm("norm gradients, 4096 tokens", "backward", 4096, 8192, "bf16", "rms", "rms", rows_per_gate=4096, scale=True),
+        norm("norm gradients 4096 tokens", "backward", 4096, 8192, "bf16", "rms", "rms", rows_per_gate=4096, scale=True),
         # a gate for every sample of 257 tokens, layer norms, an odd number of channels in 32 bits
-        norm("norm gradients, gate a sample", "backward", 2313, 1155, "f32", "layer", "layer", rows_per_gate=257,
+        norm("norm gradients gate a sample", "backward", 2313, 1155, "f32", "layer", "layer", rows_per_gate=257,
              gate_act="sigmoid"),
         # one 4,096-channel layer, 201 million parameters: 16 bytes of weight, gradient, master and moments each
-        adamw("adamw, a layer", 32, 1, 4096, "bf16"),
+        adamw("adamw a layer", 32, 1, 4096, "bf16"),
         # a 2,048-channel layer, 50 million parameters, moments in 8 bits
-        adamw("adamw, a layer, 8 bits", 8, 1, 2048, "bf16"),
+        adamw("adamw a layer 8 bits", 8, 1, 2048, "bf16"),
         # the 400 tensors of a small model, most of them a few dozen values long
-        adamw("adamw, 400 small tensors", 32, 40, 37, "f16"),
+        adamw("adamw 400 small tensors", 32, 40, 37, "f16"),
     ]
 
 
