@@ -401,6 +401,82 @@ int harp_argmin_batch(harp_ctx *ctx, int32_t C, const int64_t *iter_time, const 
 int harp_measure_valu_int32(harp_ctx *ctx, int32_t blocks, int32_t iters, uint32_t *sink,
                             void *hip_stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators of a stage's training step.
+ *
+ * What a plan assigns to a stage is a run of operators, each described by the time and the memory it
+ * takes on one device.  The calls below are the operators of a transformer's MLP block as they run on
+ * an MI355X, forward, backward and optimizer step, so that the rows of a problem (fwd_us, bwd_us,
+ * param_bytes, stash_bytes) can be taken on the card instead of being assumed:
+ *   harp_linear_*   a matrix product with bias, activation and residual in its epilogue, its gradients
+ *   harp_norm_*     the norm after a block, its gate and residual scale, the residual sum, the norm
+ *                   before the next block, and their gradients
+ *   harp_adamw_*    one AdamW step over many tensors, with moments in 32 bits or in 8
+ *
+ * Matrices are row-major; a leading dimension (ld) is the distance between rows in elements, at least
+ * the number of columns.  Pointers inside the structs are DEVICE; a NULL pointer to something optional
+ * leaves it out.  All sums, statistics and moments are held in 32 bits; a result of 16 bits is rounded
+ * once, to the nearest, when it is stored.  Infinities and NaN go where the formulas take them.
+ * Calls are asynchronous on `hip_stream`, allocate nothing, give the same bits for the same inputs on
+ * every call, and can be captured in a graph.  Outputs must not overlap inputs unless stated.
+ * ------------------------------------------------------------------------------------------------ */
+enum { HARP_F32 = 0, HARP_BF16 = 1, HARP_F16 = 2 };
+enum {
+    HARP_ACT_NONE = 0,
+    HARP_ACT_RELU = 1,      /* max(z, 0); its derivative at 0 is 0 */
+    HARP_ACT_GELU = 2,      /* z (1 + erf(z / sqrt 2)) / 2 */
+    HARP_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+    HARP_ACT_SILU = 4       /* z / (1 + exp(-z)) */
+};
+enum { HARP_NORM_NONE = 0, HARP_NORM_RMS = 1, HARP_NORM_LAYER = 2 };
+enum { HARP_GATE_LINEAR = 0, HARP_GATE_SIGMOID = 1 };
+enum { HARP_STATE_F32 = 32, HARP_STATE_8BIT = 8 };
+
+/* One tensor of an AdamW step.  m and v: float [n], or uint8_t [n] with one exponent byte per block of
+ * 256 elements, [ceil(n / 256)].  8 bits stand for
+ *   m: sign, 4 bits e, 3 bits f    v: 5 bits e, 3 bits f,   value = (e ? (8 + f) 2^(e-1) : f) 2^(E-129-R),
+ * R = 15 for m, 31 for v, E the block's exponent byte: that of the block's largest value as a float,
+ * after rounding up to 3 bits of fraction, kept in 64..254 (a byte below 64 counts as 64); 255 marks a block that holds an infinity or
+ * NaN and stands for NaN throughout.  A value between two codes goes up with the probability of the part
+ * cut off, by a hash of hyper.seed and the element's place: moving averages whose increments are under
+ * half a step would stand still otherwise.  A state of zeros is zero bytes throughout. */
+typedef struct {
+    int64_t n;
+    int32_t state;        /* HARP_STATE_F32 or HARP_STATE_8BIT */
+    int32_t grad_type;    /* HARP_F32, HARP_BF16 or HARP_F16 */
+    int32_t copy_type;    /* HARP_BF16 or HARP_F16, of copy */
+    int32_t flags;        /* must be 0 */
+    float *p;             /* [n] master weights, updated */
+    const void *grad;     /* [n] */
+    void *copy;           /* [n] or NULL: receives the new weights rounded to copy_type */
+    void *m, *v;          /* [n] moments, updated */
+    uint8_t *m_exp, *v_exp;
+    void *m_seen, *v_seen;/* [n] bfloat16 or NULL: where harp_adamw_read_state puts the values */
+    double weight_decay;
+} harp_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps;
+    int64_t step;             /* 1 for the first */
+    uint64_t seed;            /* of the rounding to 8 bits; another one every step */
+    const float *grad_scale;  /* DEVICE scalar that gradients are multiplied by, or NULL */
+    const int32_t *skip;      /* DEVICE scalar, or NULL: not 0 leaves everything as it is */
+} harp_adamw_hyper;
+typedef struct harp_adamw harp_adamw;   /* opaque host-side view of a caller-lent plan buffer */
+
+/* Bytes of DEVICE memory for the plan of these tensors (0 on malformed arguments). */
+size_t harp_adamw_plan_bytes(const harp_adamw_tensor *tensors /* HOST */, int32_t n_tensors);
+/* Writes the plan (the tensors' places and how the work is split) into plan_buf, DEVICE, 256-byte aligned,
+ * and waits for `hip_stream`; the tensors and the buffer must stay where they are until
+ * harp_adamw_release. */
+int harp_adamw_plan(harp_ctx *ctx, const harp_adamw_tensor *tensors, int32_t n_tensors, void *plan_buf,
+                    size_t plan_bytes, harp_adamw **out, void *hip_stream);
+/* For every tensor:  g = grad_scale * grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps). */
+int harp_adamw_step(harp_ctx *ctx, const harp_adamw *plan, const harp_adamw_hyper *hyper, void *hip_stream);
+/* The values that the 8-bit states stand for (exact in bfloat16), into m_seen and v_seen. */
+int harp_adamw_read_state(harp_ctx *ctx, const harp_adamw *plan, void *hip_stream);
+void harp_adamw_release(harp_adamw *plan);
+
 #ifdef __cplusplus
 }
 #endif

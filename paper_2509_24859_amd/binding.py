@@ -32,6 +32,7 @@ EXPORTS = (
     "harp_plan_mesh_h1f1b_sweep_batch", "harp_plan_mesh_sweep_workspace_bytes",
     "harp_plan_h1f1b_sweep_batch", "harp_plan_h1f1b_sweep_workspace_bytes",
     "harp_score_1f1b", "harp_argmin_batch", "harp_measure_valu_int32",
+    "harp_adamw_plan_bytes", "harp_adamw_plan", "harp_adamw_step", "harp_adamw_read_state", "harp_adamw_release",
 )
 
 
@@ -126,6 +127,13 @@ def load_library() -> C.CDLL:
     lib.harp_score_1f1b.argtypes = [vp, vp, C.POINTER(harp_candidates), vp, vp, vp, vp, vp]
     lib.harp_argmin_batch.argtypes = [vp, i32, vp, vp, vp, vp, vp]
     lib.harp_measure_valu_int32.argtypes = [vp, i32, i32, vp, vp]
+    lib.harp_adamw_plan_bytes.argtypes = [vp, i32]
+    lib.harp_adamw_plan_bytes.restype = sz
+    lib.harp_adamw_plan.argtypes = [vp, vp, i32, vp, sz, C.POINTER(vp), vp]
+    lib.harp_adamw_step.argtypes = [vp, vp, vp, vp]
+    lib.harp_adamw_read_state.argtypes = [vp, vp, vp]
+    lib.harp_adamw_release.argtypes = [vp]
+    lib.harp_adamw_release.restype = None
     _lib = lib
     return lib
 

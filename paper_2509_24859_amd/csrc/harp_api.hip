@@ -1,24 +1,14 @@
 // Host layer of the C ABI declared in include/harp.h: argument checks, layout of the caller-lent
 // buffers, kernel selection and launches.  Allocates no device memory (one small pinned host
 // buffer per context receives the build verdict).
-#include <stdarg.h>
-#include <stdio.h>
 #include <string.h>
 
 #include <new>
 
+#include "harp_ctx.h"
 #include "harp_internal.h"
 
 using namespace harp;
-
-struct harp_ctx {
-    int device;
-    int n_cu;
-    int plan_path;
-    BuildHeader *pinned;   // host, pinned
-    unsigned char *scratch;   // this device's copy of the library's static scratch array
-    char err[512];
-};
 
 // Planner workspace of harp_plan_batch_static.  In host code this name is only a handle for
 // hipGetSymbolAddress: harp_create asks for the device address once per context, with the
@@ -40,20 +30,6 @@ struct harp_tables {
 };
 
 namespace {
-
-int fail(harp_ctx *ctx, int code, const char *fmt, ...) {
-    if (ctx) {
-        va_list ap;
-        va_start(ap, fmt);
-        vsnprintf(ctx->err, sizeof(ctx->err), fmt, ap);
-        va_end(ap);
-    }
-    return code;
-}
-
-int hip_fail(harp_ctx *ctx, hipError_t e, const char *what) {
-    return fail(ctx, HARP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

@@ -1,0 +1,42 @@
+// What the kernels of a stage's operators share: element types, rounding, sums over a wavefront.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "harp.h"
+
+namespace harp {
+namespace ops {
+
+constexpr int kWave = 64;
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Elements as they are stored and as they are computed with.  Conversions round to nearest, ties to even.
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__bf16 x) { return float(x); }
+__device__ __forceinline__ float to_f32(_Float16 x) { return float(x); }
+
+template <typename T> struct Vec4 {                   // 4 elements of 2 bytes as one load
+    typedef T type __attribute__((ext_vector_type(4)));
+};
+
+template <typename T> __device__ __forceinline__ f32x4 load4(const T *p) {
+    const typename Vec4<T>::type v = *reinterpret_cast<const typename Vec4<T>::type *>(p);
+    return f32x4{to_f32(v.x), to_f32(v.y), to_f32(v.z), to_f32(v.w)};
+}
+template <typename T> __device__ __forceinline__ void store4(T *p, f32x4 v) {
+    typename Vec4<T>::type o = {T(v.x), T(v.y), T(v.z), T(v.w)};
+    *reinterpret_cast<typename Vec4<T>::type *>(p) = o;
+}
+
+// Bytes of an element, 0 for a type that there is none of.
+inline int type_bytes(int type) { return type == HARP_F32 ? 4 : type == HARP_BF16 || type == HARP_F16 ? 2 : 0; }
+inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+}  // namespace ops
+}  // namespace harp
