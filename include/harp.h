@@ -432,6 +432,51 @@ enum { HARP_NORM_NONE = 0, HARP_NORM_RMS = 1, HARP_NORM_LAYER = 2 };
 enum { HARP_GATE_LINEAR = 0, HARP_GATE_SIGMOID = 1 };
 enum { HARP_STATE_F32 = 32, HARP_STATE_8BIT = 8 };
 
+/* Between two blocks, per row r of `cols` channels:
+ *   t = after(y)                               the norm after the block, HARP_NORM_NONE: t = y
+ *   h = x + scale * gate(r / rows_per_gate) * t
+ *   z = before(h)                              the norm before the next block
+ *   RMS:   a / sqrt(mean(a^2) + eps) * w + b       LAYER: the same of a - mean(a)
+ * y NULL: h = x, only the norm before (h is not written); x NULL: h = scale * gate * t (at least one of
+ * the two is there); before HARP_NORM_NONE: no z.  z is taken of h before it is rounded.  gate_act says
+ * whether gate holds the factor itself or what a sigmoid makes it from; gate row r / rows_per_gate, so
+ * rows_per_gate = 1 is a gate of its own for every row, `rows` one for all; scale is one vector.
+ * x, y, h, z, gate, and the gradients of x, y and gate are of `type` (any); w, b, scale and their
+ * gradients [cols] are in 32 bits.  w and b may be NULL (1 and 0).  1 <= cols <= HARP_NORM_MAX_COLS. */
+#define HARP_NORM_MAX_COLS 8192
+typedef struct {
+    int64_t rows;
+    int32_t cols, type;
+    int32_t after, before;
+    float eps_after, eps_before;
+    const float *w_after, *b_after, *w_before, *b_before;
+    const float *scale;
+    const void *gate;
+    int64_t ldgate, rows_per_gate;
+    int32_t gate_act;
+} harp_norm;
+
+/* h may be x or y, z may be y; h NULL: not stored. */
+int harp_norm_forward(harp_ctx *ctx, const harp_norm *norm, const void *x, int64_t ldx, const void *y,
+                      int64_t ldy, void *h, int64_t ldh, void *z, int64_t ldz, void *hip_stream);
+
+/* The gradients of that, given dh and dz (one may be NULL: zero), h as the forward pass stored it (x where
+ * y was NULL) and y:  with D = dh + the gradient of `before` at h,  dx = D,  dy = the gradient of `after`
+ * at y of scale * gate * D, and the sums over rows.  dx, dy, and every sum may be NULL: not wanted.
+ * dgate [ceil(rows / rows_per_gate)][cols], ld lddgate.  accumulate not 0: the sums in 32 bits (not
+ * dgate) are added to what they hold.  dx may be dh or dz, dy may be y. */
+typedef struct {
+    const void *dh, *dz, *h, *y;
+    int64_t lddh, lddz, ldh, ldy;
+    void *dx, *dy, *dgate;
+    int64_t lddx, lddy, lddgate;
+    float *dw_after, *db_after, *dw_before, *db_before, *dscale;
+    int32_t accumulate;
+} harp_norm_grads;
+size_t harp_norm_workspace_bytes(harp_ctx *ctx, const harp_norm *norm);
+int harp_norm_backward(harp_ctx *ctx, const harp_norm *norm, const harp_norm_grads *grads,
+                       void *workspace, size_t workspace_bytes, void *hip_stream);
+
 /* One tensor of an AdamW step.  m and v: float [n], or uint8_t [n] with one exponent byte per block of
  * 256 elements, [ceil(n / 256)].  8 bits stand for
  *   m: sign, 4 bits e, 3 bits f    v: 5 bits e, 3 bits f,   value = (e ? (8 + f) 2^(e-1) : f) 2^(E-129-R),

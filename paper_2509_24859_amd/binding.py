@@ -33,6 +33,7 @@ EXPORTS = (
     "harp_plan_h1f1b_sweep_batch", "harp_plan_h1f1b_sweep_workspace_bytes",
     "harp_score_1f1b", "harp_argmin_batch", "harp_measure_valu_int32",
     "harp_adamw_plan_bytes", "harp_adamw_plan", "harp_adamw_step", "harp_adamw_read_state", "harp_adamw_release",
+    "harp_norm_forward", "harp_norm_workspace_bytes", "harp_norm_backward",
 )
 
 
@@ -134,6 +135,11 @@ def load_library() -> C.CDLL:
     lib.harp_adamw_read_state.argtypes = [vp, vp, vp]
     lib.harp_adamw_release.argtypes = [vp]
     lib.harp_adamw_release.restype = None
+    i64 = C.c_int64
+    lib.harp_norm_forward.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    lib.harp_norm_workspace_bytes.argtypes = [vp, vp]
+    lib.harp_norm_workspace_bytes.restype = sz
+    lib.harp_norm_backward.argtypes = [vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 

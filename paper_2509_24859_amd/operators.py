@@ -12,12 +12,18 @@ from .binding import ERR_INVALID_ARG, ERR_SHAPE, Context, HarpError, _torch
 
 F32, BF16, F16 = 0, 1, 2
 STATE_F32, STATE_8BIT = 32, 8
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+GATE_LINEAR, GATE_SIGMOID = 0, 1
+NORM_MAX_COLS = 8192
+_NORMS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
+_GATES = {"none": GATE_LINEAR, "linear": GATE_LINEAR, "sigmoid": GATE_SIGMOID}
 ADAMW_BLOCK = 256           # elements that share an exponent in an 8-bit state
 
 _types = {}
 
 
 def _type(t, allowed=(F32, BF16, F16)) -> int:
+    """The ABI's number of a tensor's type."""
     if not _types:
         torch = _torch()
         _types.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
@@ -41,6 +47,27 @@ def _vector(t, n, dtype, name):
         raise HarpError(ERR_SHAPE, "%s: %d contiguous elements of %s are wanted, got %s of %s"
                         % (name, n, dtype, tuple(t.shape), t.dtype))
     return t.data_ptr()
+
+
+def _named(value, names):
+    """A constant of the ABI, by its number or by its name."""
+    if isinstance(value, str):
+        if value not in names:
+            raise HarpError(ERR_INVALID_ARG, "%r is none of %s" % (value, ", ".join(names)))
+        return names[value]
+    return int(value)
+
+
+def _matrix(t, rows, cols, dtype, name):
+    """(pointer, leading dimension) of a matrix whose rows are contiguous; (None, cols) for None."""
+    if t is None:
+        return None, cols
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise HarpError(ERR_SHAPE, "%s: %s of %s is wanted, got %s of %s" % (name, (rows, cols), dtype, tuple(t.shape), t.dtype))
+    row, col = t.stride()
+    if (col != 1 and cols > 1) or (row < cols and rows > 1):
+        raise HarpError(ERR_SHAPE, "%s: rows must be contiguous and apart, its strides are %s" % (name, (row, col)))
+    return t.data_ptr(), row if rows > 1 else max(row, cols)
 
 
 def _stream(ctx: Context, stream, tensors):
@@ -151,3 +178,89 @@ class AdamW:
             self.release()
         except Exception:
             pass
+
+
+class harp_norm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int32), ("type", C.c_int32), ("after", C.c_int32), ("before", C.c_int32),
+                ("eps_after", C.c_float), ("eps_before", C.c_float), ("w_after", C.c_void_p), ("b_after", C.c_void_p),
+                ("w_before", C.c_void_p), ("b_before", C.c_void_p), ("scale", C.c_void_p), ("gate", C.c_void_p),
+                ("ldgate", C.c_int64), ("rows_per_gate", C.c_int64), ("gate_act", C.c_int32)]
+
+
+class harp_norm_grads(C.Structure):
+    _fields_ = [("dh", C.c_void_p), ("dz", C.c_void_p), ("h", C.c_void_p), ("y", C.c_void_p), ("lddh", C.c_int64),
+                ("lddz", C.c_int64), ("ldh", C.c_int64), ("ldy", C.c_int64), ("dx", C.c_void_p), ("dy", C.c_void_p),
+                ("dgate", C.c_void_p), ("lddx", C.c_int64), ("lddy", C.c_int64), ("lddgate", C.c_int64),
+                ("dw_after", C.c_void_p), ("db_after", C.c_void_p), ("dw_before", C.c_void_p), ("db_before", C.c_void_p),
+                ("dscale", C.c_void_p), ("accumulate", C.c_int32)]
+
+
+def _norm(ctx, rows, cols, dtype, after, before, eps, gate, rows_per_gate, gate_act, scale, w_after, b_after, w_before, b_before):
+    f32 = _torch().float32
+    n = harp_norm(rows, cols, _types[dtype], _named(after, _NORMS), _named(before, _NORMS), eps, eps,
+                  _vector(w_after, cols, f32, "w_after"), _vector(b_after, cols, f32, "b_after"),
+                  _vector(w_before, cols, f32, "w_before"), _vector(b_before, cols, f32, "b_before"),
+                  _vector(scale, cols, f32, "scale"))
+    n.gate_act = _named(gate_act, _GATES)
+    if gate is not None:
+        if rows_per_gate < 1:
+            raise HarpError(ERR_SHAPE, "rows_per_gate must be at least 1")
+        n.gate, n.ldgate = _matrix(gate, -(-rows // rows_per_gate), cols, dtype, "gate")
+        n.rows_per_gate = rows_per_gate
+    return n
+
+
+def harp_norm_forward(ctx: Context, x, y, h, z, after="rms", before="rms", gate=None, rows_per_gate=1, gate_act="linear",
+                      scale=None, w_after=None, b_after=None, w_before=None, b_before=None, eps=1e-5, stream=None):
+    """h = x + scale * gate * after(y),  z = before(h); see include/harp.h.  x, y, h, z: [rows][cols] or None."""
+    first = x if x is not None else y
+    if first is None or first.dim() != 2:
+        raise HarpError(ERR_INVALID_ARG, "x or y is wanted, as a matrix")
+    _type(first)
+    (rows, cols), dtype = first.shape, first.dtype
+    tensors = (x, y, h, z, gate, scale, w_after, b_after, w_before, b_before)
+    _on(ctx, *tensors)
+    n = _norm(ctx, rows, cols, dtype, after, before, eps, gate, rows_per_gate, gate_act, scale, w_after, b_after, w_before, b_before)
+    ctx.check(ctx.lib.harp_norm_forward(ctx.handle, C.byref(n), *_matrix(x, rows, cols, dtype, "x"), *_matrix(y, rows, cols, dtype, "y"),
+                                        *_matrix(h, rows, cols, dtype, "h"), *_matrix(z, rows, cols, dtype, "z"),
+                                        _stream(ctx, stream, tensors)))
+
+
+def norm_workspace(ctx: Context, rows: int, cols: int, rows_per_gate: int = 0):
+    """What harp_norm_backward needs for these sizes; rows_per_gate 0: no gate."""
+    n = harp_norm(rows, cols, F32)
+    if rows_per_gate:
+        n.gate, n.ldgate, n.rows_per_gate = 256, cols, rows_per_gate     # only whether there is a gate counts
+    size = ctx.lib.harp_norm_workspace_bytes(ctx.handle, C.byref(n))
+    if size == 0:
+        raise HarpError(ERR_SHAPE, ctx.lib.harp_last_error(ctx.handle).decode())
+    return _torch().empty(size, dtype=_torch().uint8, device=ctx.device)
+
+
+def harp_norm_backward(ctx: Context, dh, dz, h, y, dx, dy, after="rms", before="rms", gate=None, rows_per_gate=1, gate_act="linear",
+                       scale=None, w_after=None, b_after=None, w_before=None, b_before=None, eps=1e-5, dgate=None, dscale=None,
+                       dw_after=None, db_after=None, dw_before=None, db_before=None, accumulate=False, workspace=None, stream=None):
+    """The gradients of harp_norm_forward; see include/harp.h.  Whatever is None is not there or not wanted."""
+    first = dh if dh is not None else dz
+    if first is None or first.dim() != 2:
+        raise HarpError(ERR_INVALID_ARG, "dh or dz is wanted, as a matrix")
+    _type(first)
+    (rows, cols), dtype, f32 = first.shape, first.dtype, _torch().float32
+    sums = dict(dw_after=dw_after, db_after=db_after, dw_before=dw_before, db_before=db_before, dscale=dscale)
+    tensors = (dh, dz, h, y, dx, dy, gate, scale, w_after, b_after, w_before, b_before, dgate, workspace, *sums.values())
+    _on(ctx, *tensors)
+    n = _norm(ctx, rows, cols, dtype, after, before, eps, gate, rows_per_gate, gate_act, scale, w_after, b_after, w_before, b_before)
+    g = harp_norm_grads()
+    for name, t in (("dh", dh), ("dz", dz), ("h", h), ("y", y), ("dx", dx), ("dy", dy)):
+        p, ld = _matrix(t, rows, cols, dtype, name)
+        setattr(g, name, p)
+        setattr(g, "ld" + name, ld)
+    g.dgate, g.lddgate = _matrix(dgate, -(-rows // rows_per_gate) if dgate is not None else 0, cols, dtype, "dgate")
+    for name, t in sums.items():
+        setattr(g, name, _vector(t, cols, f32, name))
+    g.accumulate = int(bool(accumulate))
+    ctx.check(ctx.lib.harp_norm_backward(ctx.handle, C.byref(n), C.byref(g), *_workspace(workspace), _stream(ctx, stream, tensors)))
+
+
+def _workspace(w):
+    return (None, 0) if w is None else (w.data_ptr(), w.numel() * w.element_size())
