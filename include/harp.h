@@ -432,6 +432,74 @@ enum { HARP_NORM_NONE = 0, HARP_NORM_RMS = 1, HARP_NORM_LAYER = 2 };
 enum { HARP_GATE_LINEAR = 0, HARP_GATE_SIGMOID = 1 };
 enum { HARP_STATE_F32 = 32, HARP_STATE_8BIT = 8 };
 
+/* Z = X W^T + bias,  Y = act(Z) + residual.  X [M][K], W [N][K], Y, Z and residual [M][N], bias [N], all
+ * of `type`, HARP_BF16 or HARP_F16 (what the matrix instructions multiply at full rate).  Z NULL: not
+ * stored.  residual may be Y itself.  M >= 0, N, K >= 1, each below 2^31. */
+typedef struct {
+    int64_t M, N, K;
+    int32_t type, act;
+    const void *X;
+    int64_t ldx;
+    const void *W;
+    int64_t ldw;
+    const void *bias;
+    const void *residual;
+    int64_t ldr;
+    void *Y;
+    int64_t ldy;
+    void *Z;
+    int64_t ldz;
+} harp_linear;
+
+/* dX = (dY W) * act'(Z) + residual: the gradient of the product's input, taken back through the
+ * activation that made this input of Z [M][K] (act HARP_ACT_NONE: Z unused), plus the gradient that
+ * reaches the same tensor another way.  dY [M][N], W [N][K], dX, Z and residual [M][K], all of `type`.
+ * residual may be dX itself. */
+typedef struct {
+    int64_t M, N, K;
+    int32_t type, act;
+    const void *dY;
+    int64_t lddy;
+    const void *W;
+    int64_t ldw;
+    const void *Z;
+    int64_t ldz;
+    const void *residual;
+    int64_t ldr;
+    void *dX;
+    int64_t lddx;
+} harp_linear_input;
+
+/* dW = dY^T X, dbias = column sums of dY; accumulate not 0: added to what dW and dbias hold (the sum
+ * over a pipeline's micro-batches).  dY [M][N] and X [M][K] of `type`, dW [N][K] of `type` or HARP_F32
+ * (dw_type), dbias [N] in 32 bits or NULL.  M == 0 gives zeros, or leaves the sums as they are. */
+typedef struct {
+    int64_t M, N, K;
+    int32_t type, dw_type, accumulate;
+    const void *dY;
+    int64_t lddy;
+    const void *X;
+    int64_t ldx;
+    void *dW;
+    int64_t lddw;
+    float *dbias;
+} harp_linear_weight;
+
+/* Bytes of DEVICE workspace, 256-byte aligned, that any of the three calls needs for these sizes,
+ * whatever its strides and alignment (0 on sizes out of range). */
+size_t harp_linear_workspace_bytes(harp_ctx *ctx, int64_t M, int64_t N, int64_t K);
+int harp_linear_forward(harp_ctx *ctx, const harp_linear *args, void *workspace, size_t workspace_bytes,
+                        void *hip_stream);
+int harp_linear_grad_input(harp_ctx *ctx, const harp_linear_input *args, void *workspace,
+                           size_t workspace_bytes, void *hip_stream);
+int harp_linear_grad_weight(harp_ctx *ctx, const harp_linear_weight *args, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+/* dZ = dY * act'(Z) over [M][N]: for an activation whose output goes elsewhere than into a product
+ * (there harp_linear_grad_input's epilogue does it).  type HARP_F32, HARP_BF16 or HARP_F16; dZ may be
+ * dY or Z. */
+int harp_act_grad(harp_ctx *ctx, int64_t M, int64_t N, int32_t type, int32_t act, const void *dY,
+                  int64_t lddy, const void *Z, int64_t ldz, void *dZ, int64_t lddz, void *hip_stream);
+
 /* Between two blocks, per row r of `cols` channels:
  *   t = after(y)                               the norm after the block, HARP_NORM_NONE: t = y
  *   h = x + scale * gate(r / rows_per_gate) * t

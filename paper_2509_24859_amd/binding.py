@@ -32,6 +32,7 @@ EXPORTS = (
     "harp_plan_mesh_h1f1b_sweep_batch", "harp_plan_mesh_sweep_workspace_bytes",
     "harp_plan_h1f1b_sweep_batch", "harp_plan_h1f1b_sweep_workspace_bytes",
     "harp_score_1f1b", "harp_argmin_batch", "harp_measure_valu_int32",
+    "harp_linear_workspace_bytes", "harp_linear_forward", "harp_linear_grad_input", "harp_linear_grad_weight", "harp_act_grad",
     "harp_adamw_plan_bytes", "harp_adamw_plan", "harp_adamw_step", "harp_adamw_read_state", "harp_adamw_release",
     "harp_norm_forward", "harp_norm_workspace_bytes", "harp_norm_backward",
 )
@@ -136,6 +137,11 @@ def load_library() -> C.CDLL:
     lib.harp_adamw_release.argtypes = [vp]
     lib.harp_adamw_release.restype = None
     i64 = C.c_int64
+    lib.harp_linear_workspace_bytes.argtypes = [vp, i64, i64, i64]
+    lib.harp_linear_workspace_bytes.restype = sz
+    for name in ("harp_linear_forward", "harp_linear_grad_input", "harp_linear_grad_weight"):
+        getattr(lib, name).argtypes = [vp, vp, vp, sz, vp]
+    lib.harp_act_grad.argtypes = [vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp]
     lib.harp_norm_forward.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp]
     lib.harp_norm_workspace_bytes.argtypes = [vp, vp]
     lib.harp_norm_workspace_bytes.restype = sz

@@ -12,9 +12,11 @@ from .binding import ERR_INVALID_ARG, ERR_SHAPE, Context, HarpError, _torch
 
 F32, BF16, F16 = 0, 1, 2
 STATE_F32, STATE_8BIT = 32, 8
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 GATE_LINEAR, GATE_SIGMOID = 0, 1
 NORM_MAX_COLS = 8192
+_ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 _NORMS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
 _GATES = {"none": GATE_LINEAR, "linear": GATE_LINEAR, "sigmoid": GATE_SIGMOID}
 ADAMW_BLOCK = 256           # elements that share an exponent in an 8-bit state
@@ -81,6 +83,89 @@ def _stream(ctx: Context, stream, tensors):
         if t is not None:
             t.record_stream(stream)
     return int(stream.cuda_stream)
+
+
+def _workspace(w):
+    return (None, 0) if w is None else (w.data_ptr(), w.numel() * w.element_size())
+
+
+class harp_linear(C.Structure):
+    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("type", C.c_int32), ("act", C.c_int32),
+                ("X", C.c_void_p), ("ldx", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("ldr", C.c_int64), ("Y", C.c_void_p), ("ldy", C.c_int64),
+                ("Z", C.c_void_p), ("ldz", C.c_int64)]
+
+
+class harp_linear_input(C.Structure):
+    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("type", C.c_int32), ("act", C.c_int32),
+                ("dY", C.c_void_p), ("lddy", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64), ("Z", C.c_void_p),
+                ("ldz", C.c_int64), ("residual", C.c_void_p), ("ldr", C.c_int64), ("dX", C.c_void_p), ("lddx", C.c_int64)]
+
+
+class harp_linear_weight(C.Structure):
+    _fields_ = [("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64), ("type", C.c_int32), ("dw_type", C.c_int32),
+                ("accumulate", C.c_int32), ("dY", C.c_void_p), ("lddy", C.c_int64), ("X", C.c_void_p), ("ldx", C.c_int64),
+                ("dW", C.c_void_p), ("lddw", C.c_int64), ("dbias", C.c_void_p)]
+
+
+def linear_workspace(ctx: Context, tokens: int, outputs: int, inputs: int):
+    """What harp_linear_forward, harp_linear_grad_input and harp_linear_grad_weight need for X [tokens][inputs] and
+    W [outputs][inputs]."""
+    size = ctx.lib.harp_linear_workspace_bytes(ctx.handle, tokens, outputs, inputs)
+    if size == 0:
+        raise HarpError(ERR_SHAPE, "sizes out of range: %s tokens, %s outputs, %s inputs" % (tokens, outputs, inputs))
+    return _torch().empty(size, dtype=_torch().uint8, device=ctx.device)
+
+
+def _two(a, b, name_a, name_b):
+    if a.dim() != 2 or b.dim() != 2:
+        raise HarpError(ERR_SHAPE, "%s and %s must be matrices" % (name_a, name_b))
+
+
+def harp_linear_forward(ctx: Context, x, w, y, bias=None, act="none", residual=None, z=None, workspace=None, stream=None):
+    """Z = x w^T + bias,  y = act(Z) + residual; see include/harp.h.  z: receives Z, or None."""
+    _two(x, w, "x", "w")
+    (m, k), n, t = x.shape, w.shape[0], x.dtype
+    tensors = (x, w, y, bias, residual, z, workspace)
+    _on(ctx, *tensors)
+    a = harp_linear(m, n, k, _type(x, (BF16, F16)), _named(act, _ACTS), *_matrix(x, m, k, t, "x"), *_matrix(w, n, k, t, "w"),
+                    _vector(bias, n, t, "bias"), *_matrix(residual, m, n, t, "residual"), *_matrix(y, m, n, t, "y"),
+                    *_matrix(z, m, n, t, "z"))
+    ctx.check(ctx.lib.harp_linear_forward(ctx.handle, C.byref(a), *_workspace(workspace), _stream(ctx, stream, tensors)))
+
+
+def harp_linear_grad_input(ctx: Context, dy, w, dx, act="none", z=None, residual=None, workspace=None, stream=None):
+    """dx = (dy w) * act'(z) + residual; see include/harp.h."""
+    _two(dy, w, "dy", "w")
+    (m, n), k, t = dy.shape, w.shape[1], dy.dtype
+    tensors = (dy, w, dx, z, residual, workspace)
+    _on(ctx, *tensors)
+    a = harp_linear_input(m, n, k, _type(dy, (BF16, F16)), _named(act, _ACTS), *_matrix(dy, m, n, t, "dy"),
+                          *_matrix(w, n, k, t, "w"), *_matrix(z, m, k, t, "z"), *_matrix(residual, m, k, t, "residual"),
+                          *_matrix(dx, m, k, t, "dx"))
+    ctx.check(ctx.lib.harp_linear_grad_input(ctx.handle, C.byref(a), *_workspace(workspace), _stream(ctx, stream, tensors)))
+
+
+def harp_linear_grad_weight(ctx: Context, dy, x, dw, dbias=None, accumulate=False, workspace=None, stream=None):
+    """dw = dy^T x,  dbias = column sums of dy, added to what they hold with `accumulate`; see include/harp.h."""
+    _two(dy, x, "dy", "x")
+    (m, n), k, t = dy.shape, x.shape[1], dy.dtype
+    tensors = (dy, x, dw, dbias, workspace)
+    _on(ctx, *tensors)
+    a = harp_linear_weight(m, n, k, _type(dy, (BF16, F16)), _type(dw), int(bool(accumulate)), *_matrix(dy, m, n, t, "dy"),
+                           *_matrix(x, m, k, t, "x"), *_matrix(dw, n, k, dw.dtype, "dw"),
+                           _vector(dbias, n, _torch().float32, "dbias"))
+    ctx.check(ctx.lib.harp_linear_grad_weight(ctx.handle, C.byref(a), *_workspace(workspace), _stream(ctx, stream, tensors)))
+
+
+def harp_act_grad(ctx: Context, dy, z, dz, act, stream=None):
+    """dz = dy * act'(z); see include/harp.h."""
+    _two(dy, z, "dy", "z")
+    (m, n), t = dy.shape, dy.dtype
+    tensors = (dy, z, dz)
+    _on(ctx, *tensors)
+    ctx.check(ctx.lib.harp_act_grad(ctx.handle, m, n, _type(dy), _named(act, _ACTS), *_matrix(dy, m, n, t, "dy"),
+                                    *_matrix(z, m, n, t, "z"), *_matrix(dz, m, n, t, "dz"), _stream(ctx, stream, tensors)))
 
 
 class harp_adamw_tensor(C.Structure):
@@ -260,7 +345,3 @@ def harp_norm_backward(ctx: Context, dh, dz, h, y, dx, dy, after="rms", before="
         setattr(g, name, _vector(t, cols, f32, name))
     g.accumulate = int(bool(accumulate))
     ctx.check(ctx.lib.harp_norm_backward(ctx.handle, C.byref(n), C.byref(g), *_workspace(workspace), _stream(ctx, stream, tensors)))
-
-
-def _workspace(w):
-    return (None, 0) if w is None else (w.data_ptr(), w.numel() * w.element_size())
