@@ -61,7 +61,7 @@ __device__ __forceinline__ float slope(float z, int act) {
 // What becomes of D[p][q].
 enum { kForward, kInput, kWeight };
 struct Epilogue {
-    int kind, act, accumulate, out_f32;
+    int kind, act, accumulate, out_f32, wide;
     void *out;
     const void *bias, *residual;     // residual: [p][q]
     const void *slope_at;            // kInput: Z
@@ -86,43 +86,292 @@ template <typename T> __device__ __forceinline__ void finish(const Epilogue &e, 
     }
 }
 
-// A(p, r) = a[p * row + r * col].
-template <typename T> struct Operand { const T *a; int64_t row, col; };
-
-constexpr int kTile = 64, kDeep = 32, kPitch = kDeep + 8;
-
-// Four wavefronts on a tile of 64 x 64, each 32 x 32; elements are staged one by one, so any stride and size will do.
-template <typename T>
-__global__ __launch_bounds__(256) void product(Operand<T> a, Operand<T> b, int64_t P, int64_t Q, int64_t R, Epilogue e) {
-    __shared__ __align__(16) T la[kTile * kPitch], lb[kTile * kPitch];
-    const int64_t p0 = int64_t(blockIdx.y) * kTile, q0 = int64_t(blockIdx.x) * kTile;
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int wp = wave / 2 * 32, wq = wave % 2 * 32;
-    f32x4 acc[2][2] = {};
-    for (int64_t r0 = 0; r0 < R; r0 += kDeep) {
-        for (int i = threadIdx.x; i < kTile * kDeep; i += 256) {
-            const int pa = a.col == 1 ? i / kDeep : i % kTile, ra = a.col == 1 ? i % kDeep : i / kTile;
-            la[pa * kPitch + ra] = p0 + pa < P && r0 + ra < R ? a.a[(p0 + pa) * a.row + (r0 + ra) * a.col] : T(0.0f);
-            const int qb = b.col == 1 ? i / kDeep : i % kTile, rb = b.col == 1 ? i % kDeep : i / kTile;
-            lb[qb * kPitch + rb] = q0 + qb < Q && r0 + rb < R ? b.a[(q0 + qb) * b.row + (r0 + rb) * b.col] : T(0.0f);
+// The same for q .. q + 3.  `wide`: all of it is there and aligned.
+template <typename T> __device__ __forceinline__ void finish4(const Epilogue &e, int64_t p, int64_t q, int64_t Q, f32x4 d) {
+    if (!e.wide) {
+#pragma unroll 1
+        for (int k = 0; k < 4 && q < Q; ++k, ++q) {
+            finish<T>(e, p, q, d.x);
+            d = f32x4{d.y, d.z, d.w, 0};
         }
-        __syncthreads();
-        typename Mfma<T>::Frag fa[2], fb[2];
-        for (int i = 0; i < 2; ++i) {
-            fa[i] = *reinterpret_cast<const typename Mfma<T>::Frag *>(la + (wp + 16 * i + lane % 16) * kPitch + 8 * (lane / 16));
-            fb[i] = *reinterpret_cast<const typename Mfma<T>::Frag *>(lb + (wq + 16 * i + lane % 16) * kPitch + 8 * (lane / 16));
-        }
-        // the q operand first: a lane then holds four neighbouring q of one p
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2; ++j) acc[i][j] = Mfma<T>::run(fb[j], fa[i], acc[i][j]);
-        __syncthreads();
+        return;
     }
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j)
-            for (int k = 0; k < 4; ++k) {
-                const int64_t p = p0 + wp + 16 * i + lane % 16, q = q0 + wq + 16 * j + 4 * (lane / 16) + k;
-                if (p < P && q < Q) finish<T>(e, p, q, acc[i][j][k]);
+    if (e.kind == kForward) {
+        if (e.bias) d += load4(static_cast<const T *>(e.bias) + q);
+        if (e.keep) store4(static_cast<T *>(e.keep) + p * e.ldz + q, d);
+        for (int k = 0; k < 4; ++k) d[k] = activate(d[k], e.act);
+    } else if (e.kind == kInput && e.act != HARP_ACT_NONE) {
+        const f32x4 z = load4(static_cast<const T *>(e.slope_at) + p * e.ldz + q);
+        for (int k = 0; k < 4; ++k) d[k] *= slope(z[k], e.act);
+    }
+    if (e.residual) d += load4(static_cast<const T *>(e.residual) + p * e.ldr + q);
+    if (e.out_f32) {
+        float *o = static_cast<float *>(e.out) + p * e.ldo + q;
+        store4(o, e.accumulate ? d + load4(o) : d);
+    } else {
+        T *o = static_cast<T *>(e.out) + p * e.ldo + q;
+        store4(o, e.accumulate ? d + load4(o) : d);
+    }
+}
+
+// Shares of r that several workgroups summed up apart, in their order, and the epilogue.
+template <typename T>
+__global__ __launch_bounds__(256) void join(const float *partial, int shares, int64_t P, int64_t Q, Epilogue e) {
+    const int64_t across = (Q + 3) / 4;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < P * across; i += int64_t(gridDim.x) * 256) {
+        const int64_t p = i / across, q = i % across * 4;
+        f32x4 d = {0, 0, 0, 0};
+        for (int s = 0; s < shares; ++s) {
+            const float *o = partial + (s * P + p) * Q + q;
+            for (int k = 0; k < 4; ++k)
+                if (q + k < Q) d[k] += o[k];
+        }
+        finish4<T>(e, p, q, Q, d);
+    }
+}
+
+// Rows of `cols` elements anywhere, to rows of a multiple of 8 that begin at multiples of 16 bytes and end with zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void pack(const T *from, int64_t ld, int64_t rows, int64_t cols, T *to, int64_t ldto) {
+    const int64_t across = ldto / 8;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < rows * across; i += int64_t(gridDim.x) * 256) {
+        const int64_t row = i / across, c = i % across * 8;
+        typename Mfma<T>::Frag v;
+        for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? from[row * ld + c + k] : T(0.0f);
+        *reinterpret_cast<typename Mfma<T>::Frag *>(to + row * ldto + c) = v;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- tiles
+// A workgroup makes a tile of BP x BQ of D, 64 of r at a time.  Both operands go from memory straight into LDS, the next
+// 64 of r while the current ones are multiplied (two buffers).
+//
+// LDS holds pieces of 16 bytes.  Where r is contiguous in memory a row of the tile is 8 pieces of 8 r, piece c of row
+// `row` at place c ^ (row & 7): the 8 rows that a wavefront reads at once then lie in 8 different places.  Where p or q is
+// contiguous a row is one r with B / 8 pieces of 8 p, moved by swap(r); four rows of 16 p are transposed by the read.
+constexpr int kDeep = 64;
+
+__device__ __forceinline__ int swap_of(int r) { return (r & 3) << 1 | (r >> 3 & 1) << 3; }
+
+template <typename T> __device__ __forceinline__ void load_to_lds(const T *from, T *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+// One operand of a workgroup of THREADS threads: ACROSS: p is contiguous, else r.
+template <typename T, bool ACROSS, int B, int THREADS> struct Side {
+    static constexpr int kLoads = B * kDeep * 2 / 16 / THREADS;      // pieces a thread brings
+    static constexpr int kRow = ACROSS ? B / 8 : kDeep / 8;          // pieces in a row of LDS
+    const T *from[kLoads];
+    int64_t step;
+
+    __device__ __forceinline__ static int place(int i) { return i * THREADS + int(threadIdx.x); }
+    // r (relative to the tile) of piece i of this thread
+    __device__ __forceinline__ static int depth(int i) {
+        const int id = place(i);
+        return ACROSS ? id / kRow : ((id % kRow) ^ (id / kRow & 7)) * 8;
+    }
+    __device__ __forceinline__ void begin(const T *a, int64_t ld, int64_t p0, int64_t P, int64_t r0) {
+        step = ACROSS ? kDeep * ld : kDeep;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int id = place(i);
+            if (ACROSS) {
+                const int64_t p = p0 + ((id % kRow) ^ swap_of(id / kRow)) * 8, last = (P + 7) / 8 * 8 - 8;
+                const int64_t at = p < last ? p : last;              // beyond the edge: anything that is there
+                from[i] = a + (r0 + depth(i)) * ld + at;
+            } else {
+                int64_t p = p0 + id / kRow;
+                p = p < P ? p : P - 1;
+                from[i] = a + p * ld + r0 + depth(i);
             }
+        }
+    }
+    __device__ __forceinline__ void load(T *lds) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            load_to_lds(from[i], lds + (i * THREADS + int(threadIdx.x) / kWave * kWave) * 8);
+            from[i] += step;
+        }
+    }
+    // the last, partial 64 of r: zeros from `left` on (rows of r end with zeros up to a multiple of 8)
+    __device__ __forceinline__ void load_partial(T *lds, int left) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            u32x4 v = {0, 0, 0, 0};
+            if (depth(i) < (ACROSS ? left : (left + 7) / 8 * 8)) v = *reinterpret_cast<const u32x4 *>(from[i]);
+            *reinterpret_cast<u32x4 *>(lds + place(i) * 8) = v;
+        }
+    }
+};
+
+// Fragments of 16 p by 32 r of a tile in LDS: lane l has p = l % 16 and r = 8 (l / 16) .. + 7 of the 32.
+template <typename T, bool ACROSS, int B, int COUNT> struct Fragments {
+    typedef typename Mfma<T>::Frag Frag;
+    int at[ACROSS ? COUNT : 2];
+    __device__ __forceinline__ void begin(int p0) {
+        const int lane = threadIdx.x % kWave, i = lane % 16, g = lane / 16;
+        if constexpr (ACROSS) {
+            const int r = 8 * g + i / 4;
+            for (int j = 0; j < COUNT; ++j) at[j] = r * B + (((p0 / 8 + 2 * j) ^ swap_of(r)) | (i % 4 / 2)) * 8 + i % 2 * 4;
+        } else {
+            for (int k = 0; k < 2; ++k) at[k] = (p0 + i) * kDeep + ((4 * k + g) ^ (i & 7)) * 8;
+        }
+    }
+    __device__ __forceinline__ Frag read(const T *lds, int j, int k) const {
+        if constexpr (ACROSS) {
+            typedef short s16x4 __attribute__((ext_vector_type(4)));
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            typedef __attribute__((address_space(3))) s16x4 *Lds;
+            const T *a = lds + at[j] + 32 * k * B;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)a);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(a + 4 * B));
+            const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            return __builtin_bit_cast(Frag, v);
+        } else {
+            return *reinterpret_cast<const Frag *>(lds + at[k] + 16 * j * kDeep);
+        }
+    }
+};
+
+// Which tile a workgroup takes.  Workgroups go to the 8 dies in turn, each with an L2 of its own: a die takes tiles that
+// are neighbours, in columns of kGroup tiles, so that what they share is read into one L2.
+constexpr int kDies = 8, kGroup = 8;
+__device__ __forceinline__ void tile_of(int id, int tiles_p, int tiles_q, int &tp, int &tq) {
+    const int n = tiles_p * tiles_q, die = id % kDies, each = n / kDies, more = n % kDies;
+    id = id / kDies + die * each + (die < more ? die : more);
+    const int wide = kGroup * tiles_q, first = id / wide * kGroup;
+    const int high = tiles_p - first < kGroup ? tiles_p - first : kGroup;
+    tp = first + id % wide % high;
+    tq = id % wide / high;
+}
+
+// WP x WQ wavefronts, each a part of BP / WP x BQ / WQ of the tile.  With `partial` the sums of blockIdx.y's share of r go
+// there, [share][P][Q], instead of through the epilogue.
+template <typename T, bool A_ACROSS, bool B_ACROSS, int BP, int BQ, int WP, int WQ>
+__global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t lda, const T *b, int64_t ldb, int64_t P, int64_t Q, int64_t R,
+                                                           int tiles_p, int tiles_q, int64_t share, float *partial, Epilogue e) {
+    constexpr int kThreads = WP * WQ * kWave, kP = BP / WP / 16, kQ = BQ / WQ / 16;
+    __shared__ __align__(16) T la[2][BP * kDeep];
+    __shared__ __align__(16) T lb[2][BQ * kDeep];
+    int tp, tq;
+    tile_of(blockIdx.x, tiles_p, tiles_q, tp, tq);
+    const int64_t p0 = int64_t(tp) * BP, q0 = int64_t(tq) * BQ;
+    const int64_t r0 = int64_t(blockIdx.y) * share, r1 = r0 + share < R ? r0 + share : R;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int wp = wave / WQ * (BP / WP), wq = wave % WQ * (BQ / WQ);
+    Side<T, A_ACROSS, BP, kThreads> sa;
+    Side<T, B_ACROSS, BQ, kThreads> sb;
+    sa.begin(a, lda, p0, P, r0);
+    sb.begin(b, ldb, q0, Q, r0);
+    Fragments<T, A_ACROSS, BP, kP> fa;
+    Fragments<T, B_ACROSS, BQ, kQ> fb;
+    fa.begin(wp);
+    fb.begin(wq);
+    f32x4 acc[kP][kQ] = {};
+    auto bring = [&](int buffer, int64_t left) {
+        if (left >= kDeep) {
+            sa.load(la[buffer]);
+            sb.load(lb[buffer]);
+        } else {
+            sa.load_partial(la[buffer], int(left));
+            sb.load_partial(lb[buffer], int(left));
+        }
+    };
+    auto multiply = [&](int buffer) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            typename Mfma<T>::Frag x[kP], y[kQ];
+#pragma unroll
+            for (int i = 0; i < kP; ++i) x[i] = fa.read(la[buffer], i, k);
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) y[j] = fb.read(lb[buffer], j, k);
+            // the q operand first: a lane then holds four neighbouring q of one p
+#pragma unroll
+            for (int i = 0; i < kP; ++i)
+#pragma unroll
+                for (int j = 0; j < kQ; ++j) acc[i][j] = Mfma<T>::run(y[j], x[i], acc[i][j]);
+        }
+    };
+    // what was brought is in LDS for everybody: loads into LDS are counted by vmcnt, which a barrier does not wait for
+    auto arrived = [] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+    };
+    if (r0 < r1) bring(0, r1 - r0);
+    arrived();
+    int buffer = 0;
+    for (int64_t r = r0; r < r1; r += kDeep) {
+        if (r + kDeep < r1) bring(buffer ^ 1, r1 - r - kDeep);
+        multiply(buffer);
+        arrived();
+        buffer ^= 1;
+    }
+    // 16 p at a time through LDS (the tiles are done with): a lane then holds four q of a row whose other q its neighbours
+    // hold, and rows are stored in whole lines.
+    if (partial) e = Epilogue{kWeight, HARP_ACT_NONE, 0, 1, Q % 4 == 0, partial + int64_t(blockIdx.y) * P * Q, nullptr, nullptr, nullptr, nullptr, Q, 0, 0};
+    constexpr int kCols = BQ / WQ, kPitch = kCols + 4, kAtOnce = kWave / (kCols / 4);
+    static_assert(WP * WQ * 16 * kPitch * 4 <= 2 * BP * kDeep * 2, "the wavefronts' rows have to fit into the first operand's LDS");
+    float *rows = reinterpret_cast<float *>(&la[0][0]) + wave * 16 * kPitch;
+    const int64_t q = q0 + wq + lane % (kCols / 4) * 4;
+#pragma unroll
+    for (int i = 0; i < kP; ++i) {
+#pragma unroll
+        for (int j = 0; j < kQ; ++j) *reinterpret_cast<f32x4 *>(rows + lane % 16 * kPitch + 16 * j + lane / 16 * 4) = acc[i][j];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int k = lane / (kCols / 4); k < 16; k += kAtOnce) {
+            const int64_t p = p0 + wp + 16 * i + k;
+            if (p < P && q < Q) finish4<T>(e, p, q, Q, *reinterpret_cast<const f32x4 *>(rows + k * kPitch + lane % (kCols / 4) * 4));
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- few tokens
+// Y of at most 16 TILES tokens: the weights are read once, straight into registers, and bound it.  A workgroup makes 16
+// outputs of all tokens; its four wavefronts take 64 of r in turn and are joined at the end.  In a piece of 64 r lane l
+// has row l % 16 and the 16 r from 16 (l / 16) on, 32 bytes of a row, so that four lanes read whole lines; the same r of
+// the tokens meet them, whatever their order.
+constexpr int kFewWaves = 4;
+template <typename T, bool WIDE> __device__ __forceinline__ typename Mfma<T>::Frag eight(const T *row, int64_t r, int64_t R) {
+    typename Mfma<T>::Frag v = {};
+    if (WIDE) {
+        if (r < R) v = *reinterpret_cast<const typename Mfma<T>::Frag *>(row + r);
+    } else {
+        for (int k = 0; k < 8; ++k)
+            if (r + k < R) v[k] = row[r + k];
+    }
+    return v;
+}
+template <typename T, bool WIDE, int TILES>
+__global__ __launch_bounds__(kFewWaves * kWave) void few_tokens(const T *x, int64_t ldx, const T *w, int64_t ldw, int64_t M, int64_t N, int64_t R,
+                                                                int64_t share, float *partial, Epilogue e) {
+    __shared__ float sums[kFewWaves][TILES * 16][17];
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, i = lane % 16, g = lane / 16;
+    const int64_t n0 = int64_t(blockIdx.x) * 16;
+    const int64_t r0 = int64_t(blockIdx.y) * share, r1 = r0 + share < R ? r0 + share : R;
+    const T *wr = w + (n0 + i < N ? n0 + i : N - 1) * ldw;
+    const T *xr[TILES];
+    for (int t = 0; t < TILES; ++t) xr[t] = x + (16 * t + i < M ? 16 * t + i : M - 1) * ldx;
+    f32x4 acc[TILES] = {};
+    for (int64_t r = r0 + wave * 64 + 16 * g; r - 16 * g < r1; r += kFewWaves * 64) {
+        const typename Mfma<T>::Frag a = eight<T, WIDE>(wr, r, r1), b = eight<T, WIDE>(wr, r + 8, r1);
+        for (int t = 0; t < TILES; ++t) {
+            acc[t] = Mfma<T>::run(a, eight<T, WIDE>(xr[t], r, r1), acc[t]);
+            acc[t] = Mfma<T>::run(b, eight<T, WIDE>(xr[t], r + 8, r1), acc[t]);
+        }
+    }
+    for (int t = 0; t < TILES; ++t)
+        for (int k = 0; k < 4; ++k) sums[wave][16 * t + i][4 * g + k] = acc[t][k];
+    __syncthreads();
+    for (int at = threadIdx.x; at < TILES * 256; at += kFewWaves * kWave) {
+        const int m = at / 16, n = at % 16;
+        float d = 0;
+        for (int v = 0; v < kFewWaves; ++v) d += sums[v][m][n];
+        if (m >= M || n0 + n >= N) continue;
+        if (partial) partial[(int64_t(blockIdx.y) * M + m) * N + n0 + n] = d;
+        else finish<T>(e, m, n0 + n, d);
+    }
 }
 
 // Column sums of dY: partial sums of slabs of rows, then the slabs in order.
@@ -160,7 +409,58 @@ bool sizes_fit(int64_t M, int64_t N, int64_t K) {
     return M >= 0 && N >= 1 && K >= 1 && M < most && N < most && K < most;
 }
 
-size_t workspace_for(int64_t M, int64_t N, int64_t) { return round_up(size_t(slabs_of(M)) * size_t(N) * 4, 256) + 256; }
+// How a product is launched.
+struct Plan {
+    bool few, big;               // few tokens; tiles of 256 x 256, else of 128 x 128
+    int shares;                  // of r, joined by a second launch
+    int64_t share;               // r of one, a multiple of kDeep
+};
+constexpr int kFewTokens = 64;
+
+int64_t tiles(int64_t P, int64_t Q, int side) { return (P + side - 1) / side * ((Q + side - 1) / side); }
+
+Plan split(Plan p, int64_t R, int64_t shares) {
+    const int64_t steps = (R + kDeep - 1) / kDeep;
+    shares = shares < steps ? shares : steps;
+    shares = shares < 1 ? 1 : shares;
+    const int64_t each = (steps + shares - 1) / shares;
+    p.share = (each < 1 ? 1 : each) * kDeep;
+    p.shares = int(steps ? (steps + each - 1) / each : 1);
+    return p;
+}
+
+Plan plan_for(const harp_ctx *ctx, int kind, int64_t P, int64_t Q, int64_t R) {
+    Plan p = {};
+    const int64_t cu = ctx->n_cu;
+    if (kind == kForward && P <= kFewTokens) {
+        p.few = true;
+        const int64_t groups = (Q + 15) / 16;
+        // 8 workgroups a compute unit, of at least four pieces a wavefront
+        int64_t shares = 8 * cu / (groups > 0 ? groups : 1);
+        const int64_t most = R / (16 * kDeep);
+        shares = shares < most ? shares : most;
+        return split(p, R, shares < 16 ? shares : 16);
+    }
+    p.big = tiles(P, Q, 256) >= cu;
+    const int64_t n = tiles(P, Q, p.big ? 256 : 128), slots = p.big ? cu : 2 * cu;
+    return split(p, R, n > 0 && n < slots ? slots / n : 1);
+}
+
+size_t packed_bytes(int64_t rows, int64_t cols) { return round_up(size_t(rows) * round_up(size_t(cols), 8) * 2, 256); }
+size_t partial_bytes(const harp_ctx *ctx, int kind, int64_t P, int64_t Q, int64_t R) {
+    const Plan p = plan_for(ctx, kind, P, Q, R);
+    return p.shares > 1 ? round_up(size_t(p.shares) * size_t(P) * size_t(Q) * 4, 256) : 0;
+}
+size_t most(size_t a, size_t b) { return a > b ? a : b; }
+
+// Both operands packed, and shares of r or column sums.
+size_t workspace_for(const harp_ctx *ctx, int64_t M, int64_t N, int64_t K) {
+    const size_t x = packed_bytes(M, K), w = packed_bytes(N, K), dy = packed_bytes(M, N);
+    const size_t forward = x + w + partial_bytes(ctx, kForward, M, N, K);
+    const size_t input = dy + w + partial_bytes(ctx, kInput, M, K, N);
+    const size_t weight = dy + x + most(partial_bytes(ctx, kWeight, N, K, M), round_up(size_t(slabs_of(M)) * size_t(N) * 4, 256));
+    return most(most(forward, input), weight) + 256;
+}
 
 struct Matrix { const char *name; const void *p; int64_t ld, cols; size_t element; bool needed; };
 
@@ -175,7 +475,7 @@ int check(harp_ctx *ctx, int64_t M, int64_t N, int64_t K, int type, int act, con
         if (m[i].ld < m[i].cols) return fail(ctx, HARP_ERR_SHAPE, "%s: leading dimension below its columns", m[i].name);
         if (!aligned(m[i].p, m[i].element)) return fail(ctx, HARP_ERR_INVALID_ARG, "%s is not aligned to its elements", m[i].name);
     }
-    const size_t need = workspace_for(M, N, K);
+    const size_t need = workspace_for(ctx, M, N, K);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < need)
         return fail(ctx, HARP_ERR_WORKSPACE, "the workspace needs %zu bytes, aligned to 256", need);
     const hipError_t e = hipSetDevice(ctx->device);
@@ -183,11 +483,69 @@ int check(harp_ctx *ctx, int64_t M, int64_t N, int64_t K, int type, int act, con
     return HARP_OK;
 }
 
+// One operand as it is called with: A(p, r), rows of `cols` elements ld apart.
+struct Given { const void *a; int64_t ld, rows, cols; };
+
+bool wide_rows(const Given &g) { return g.cols % 8 == 0 && g.ld % 8 == 0 && aligned(g.a, 16); }
+
+uint32_t blocks_for(int64_t threads) {
+    const int64_t n = (threads + 255) / 256;
+    return uint32_t(n < 16384 ? n : 16384);
+}
+
+template <typename T> Given packed(Given g, unsigned char *&ws, hipStream_t st) {
+    if (wide_rows(g) || g.rows == 0) return g;
+    const int64_t ld = int64_t(round_up(size_t(g.cols), 8));
+    T *to = reinterpret_cast<T *>(ws);
+    ws += packed_bytes(g.rows, g.cols);
+    pack<T><<<dim3(blocks_for(g.rows * (ld / 8))), dim3(256), 0, st>>>(static_cast<const T *>(g.a), g.ld, g.rows, g.cols, to, ld);
+    return Given{to, ld, g.rows, g.cols};
+}
+
+template <typename T, bool A_ACROSS, bool B_ACROSS>
+void launch_tiles(const Plan &plan, const Given &a, const Given &b, int64_t P, int64_t Q, int64_t R, float *partial, const Epilogue &e,
+                  hipStream_t st) {
+    const int side = plan.big ? 256 : 128;
+    const int tp = int((P + side - 1) / side), tq = int((Q + side - 1) / side);
+    const dim3 grid(uint32_t(tp) * uint32_t(tq), uint32_t(plan.shares));
+    const T *pa = static_cast<const T *>(a.a), *pb = static_cast<const T *>(b.a);
+    if (plan.big) product<T, A_ACROSS, B_ACROSS, 256, 256, 2, 4><<<grid, dim3(512), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
+    else product<T, A_ACROSS, B_ACROSS, 128, 128, 2, 2><<<grid, dim3(256), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
+}
+
+template <typename T, bool WIDE>
+void launch_few(const Plan &plan, const Given &x, const Given &w, int64_t M, int64_t N, int64_t R, float *partial, const Epilogue &e,
+                hipStream_t st) {
+    const dim3 grid(uint32_t((N + 15) / 16), uint32_t(plan.shares)), block(kFewWaves * kWave);
+    const T *px = static_cast<const T *>(x.a), *pw = static_cast<const T *>(w.a);
+    if (M <= 16) few_tokens<T, WIDE, 1><<<grid, block, 0, st>>>(px, x.ld, pw, w.ld, M, N, R, plan.share, partial, e);
+    else if (M <= 32) few_tokens<T, WIDE, 2><<<grid, block, 0, st>>>(px, x.ld, pw, w.ld, M, N, R, plan.share, partial, e);
+    else few_tokens<T, WIDE, 4><<<grid, block, 0, st>>>(px, x.ld, pw, w.ld, M, N, R, plan.share, partial, e);
+}
+
 template <typename T>
-void launch_product(const void *a, int64_t a_row, int64_t a_col, const void *b, int64_t b_row, int64_t b_col, int64_t P, int64_t Q,
-                    int64_t R, const Epilogue &e, hipStream_t st) {
-    const Operand<T> oa = {static_cast<const T *>(a), a_row, a_col}, ob = {static_cast<const T *>(b), b_row, b_col};
-    product<T><<<dim3(uint32_t((Q + kTile - 1) / kTile), uint32_t((P + kTile - 1) / kTile)), dim3(256), 0, st>>>(oa, ob, P, Q, R, e);
+void launch_product(const harp_ctx *ctx, Given a, Given b, int64_t P, int64_t Q, int64_t R, Epilogue e, void *workspace, hipStream_t st) {
+    const Plan plan = plan_for(ctx, e.kind, P, Q, R);
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    const size_t out = e.out_f32 ? 16 : 8;
+    e.wide = Q % 4 == 0 && e.ldo % 4 == 0 && aligned(e.out, out) && aligned(e.bias, 8) && aligned(e.residual, 8) && aligned(e.slope_at, 8) &&
+             aligned(e.keep, 8) && (!e.residual || e.ldr % 4 == 0) && ((!e.slope_at && !e.keep) || e.ldz % 4 == 0);
+    if (!plan.few) {
+        a = packed<T>(a, ws, st);
+        b = packed<T>(b, ws, st);
+    }
+    float *partial = plan.shares > 1 ? reinterpret_cast<float *>(ws) : nullptr;
+    if (plan.few) {
+        if (wide_rows(a) && wide_rows(b)) launch_few<T, true>(plan, a, b, P, Q, R, partial, e, st);
+        else launch_few<T, false>(plan, a, b, P, Q, R, partial, e, st);
+    } else if (e.kind == kForward) {
+        launch_tiles<T, false, false>(plan, a, b, P, Q, R, partial, e, st);
+    } else if (e.kind == kInput) {
+        launch_tiles<T, false, true>(plan, a, b, P, Q, R, partial, e, st);
+    } else {
+        launch_tiles<T, true, true>(plan, a, b, P, Q, R, partial, e, st);
+    }
+    if (partial) join<T><<<dim3(blocks_for(P * ((Q + 3) / 4))), dim3(256), 0, st>>>(partial, plan.shares, P, Q, e);
 }
 
 int launched(harp_ctx *ctx) {
@@ -200,7 +558,7 @@ int launched(harp_ctx *ctx) {
 extern "C" {
 
 size_t harp_linear_workspace_bytes(harp_ctx *ctx, int64_t M, int64_t N, int64_t K) {
-    return ctx && sizes_fit(M, N, K) ? workspace_for(M, N, K) : 0;
+    return ctx && sizes_fit(M, N, K) ? workspace_for(ctx, M, N, K) : 0;
 }
 
 int harp_linear_forward(harp_ctx *ctx, const harp_linear *g, void *workspace, size_t workspace_bytes, void *hip_stream) {
@@ -211,10 +569,10 @@ int harp_linear_forward(harp_ctx *ctx, const harp_linear *g, void *workspace, si
                         {"residual", g->residual, g->ldr, g->N, 2, false}, {"Y", g->Y, g->ldy, g->N, 2, some}, {"Z", g->Z, g->ldz, g->N, 2, false}};
     const int rc = check(ctx, g->M, g->N, g->K, g->type, g->act, m, 6, workspace, workspace_bytes);
     if (rc != HARP_OK || !some) return rc;
-    const Epilogue e = {kForward, g->act, 0, 0, g->Y, g->bias, g->residual, nullptr, g->Z, g->ldy, g->ldr, g->ldz};
+    const Epilogue e = {kForward, g->act, 0, 0, 0, g->Y, g->bias, g->residual, nullptr, g->Z, g->ldy, g->ldr, g->ldz};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (g->type == HARP_BF16) launch_product<__bf16>(g->X, g->ldx, 1, g->W, g->ldw, 1, g->M, g->N, g->K, e, st);
-    else launch_product<_Float16>(g->X, g->ldx, 1, g->W, g->ldw, 1, g->M, g->N, g->K, e, st);
+    if (g->type == HARP_BF16) launch_product<__bf16>(ctx, {g->X, g->ldx, g->M, g->K}, {g->W, g->ldw, g->N, g->K}, g->M, g->N, g->K, e, workspace, st);
+    else launch_product<_Float16>(ctx, {g->X, g->ldx, g->M, g->K}, {g->W, g->ldw, g->N, g->K}, g->M, g->N, g->K, e, workspace, st);
     return launched(ctx);
 }
 
@@ -227,10 +585,10 @@ int harp_linear_grad_input(harp_ctx *ctx, const harp_linear_input *g, void *work
                         {"residual", g->residual, g->ldr, g->K, 2, false}, {"dX", g->dX, g->lddx, g->K, 2, some}};
     const int rc = check(ctx, g->M, g->N, g->K, g->type, g->act, m, 5, workspace, workspace_bytes);
     if (rc != HARP_OK || !some) return rc;
-    const Epilogue e = {kInput, g->act, 0, 0, g->dX, nullptr, g->residual, g->Z, nullptr, g->lddx, g->ldr, g->ldz};
+    const Epilogue e = {kInput, g->act, 0, 0, 0, g->dX, nullptr, g->residual, g->act != HARP_ACT_NONE ? g->Z : nullptr, nullptr, g->lddx, g->ldr, g->ldz};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (g->type == HARP_BF16) launch_product<__bf16>(g->dY, g->lddy, 1, g->W, 1, g->ldw, g->M, g->K, g->N, e, st);
-    else launch_product<_Float16>(g->dY, g->lddy, 1, g->W, 1, g->ldw, g->M, g->K, g->N, e, st);
+    if (g->type == HARP_BF16) launch_product<__bf16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->W, g->ldw, g->N, g->K}, g->M, g->K, g->N, e, workspace, st);
+    else launch_product<_Float16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->W, g->ldw, g->N, g->K}, g->M, g->K, g->N, e, workspace, st);
     return launched(ctx);
 }
 
@@ -244,10 +602,10 @@ int harp_linear_grad_weight(harp_ctx *ctx, const harp_linear_weight *g, void *wo
     const int rc = check(ctx, g->M, g->N, g->K, g->type, HARP_ACT_NONE, m, 4, workspace, workspace_bytes);
     if (rc != HARP_OK) return rc;
     if (!some && g->accumulate) return HARP_OK;
-    const Epilogue e = {kWeight, HARP_ACT_NONE, g->accumulate, g->dw_type == HARP_F32, g->dW, nullptr, nullptr, nullptr, nullptr, g->lddw, 0, 0};
+    const Epilogue e = {kWeight, HARP_ACT_NONE, g->accumulate, g->dw_type == HARP_F32, 0, g->dW, nullptr, nullptr, nullptr, nullptr, g->lddw, 0, 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (g->type == HARP_BF16) launch_product<__bf16>(g->dY, 1, g->lddy, g->X, 1, g->ldx, g->N, g->K, g->M, e, st);
-    else launch_product<_Float16>(g->dY, 1, g->lddy, g->X, 1, g->ldx, g->N, g->K, g->M, e, st);
+    if (g->type == HARP_BF16) launch_product<__bf16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->X, g->ldx, g->M, g->K}, g->N, g->K, g->M, e, workspace, st);
+    else launch_product<_Float16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->X, g->ldx, g->M, g->K}, g->N, g->K, g->M, e, workspace, st);
     if (g->dbias) {
         float *partial = static_cast<float *>(workspace);
         const uint32_t across = uint32_t((g->N + 255) / 256);
