@@ -17,7 +17,6 @@ namespace {
 constexpr int kPer = 8;                               // channels a thread holds
 constexpr int kMaxThreads = HARP_NORM_MAX_COLS / kPer;
 constexpr int kMaxWaves = kMaxThreads / kWave;
-constexpr int kSums = 5;                              // column sums in 32 bits: dw_after, db_after, dscale, dw_before, db_before
 
 // Everything but the data, as the kernels see it.
 struct Form {
@@ -33,104 +32,176 @@ template <bool WIDE> __device__ __forceinline__ int channel(int j) {
     return WIDE ? int(threadIdx.x) * kPer + j : int(threadIdx.x) + j * int(blockDim.x);
 }
 
-template <typename T, bool WIDE> __device__ __forceinline__ void load_row(const T *row, int cols, float (&v)[kPer]) {
-    if (WIDE) {
-        const bool in = int(threadIdx.x) * kPer < cols;
-        for (int k = 0; k < kPer; k += 4) {
-            const f32x4 q = in ? load4(row + channel<WIDE>(k)) : f32x4{0, 0, 0, 0};
-            for (int j = 0; j < 4; ++j) v[k + j] = q[j];
+// A thread's channels of a row as they are stored: what is asked for ahead of its use takes half the registers in 16 bits.
+template <typename T, bool WIDE> struct Raw {
+    typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T))));
+    static constexpr int kPieces = WIDE ? kPer * int(sizeof(T)) / 16 : 1;
+    Piece piece[kPieces];
+    T one[WIDE ? 1 : kPer];
+
+    __device__ __forceinline__ void load(const T *row, int cols) {
+        if constexpr (WIDE) {
+            if (int(threadIdx.x) * kPer < cols)
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) piece[k] = *reinterpret_cast<const Piece *>(row + channel<WIDE>(0) + k * (16 / int(sizeof(T))));
+            else
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) piece[k] = Piece(T(0.0f));
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) one[j] = channel<WIDE>(j) < cols ? row[channel<WIDE>(j)] : T(0.0f);
         }
-    } else {
-        for (int j = 0; j < kPer; ++j) v[j] = channel<WIDE>(j) < cols ? to_f32(row[channel<WIDE>(j)]) : 0.0f;
     }
-}
-template <typename T, bool WIDE> __device__ __forceinline__ void store_row(T *row, int cols, const float (&v)[kPer]) {
-    if (WIDE) {
-        if (int(threadIdx.x) * kPer < cols)
-            for (int k = 0; k < kPer; k += 4) store4(row + channel<WIDE>(k), f32x4{v[k], v[k + 1], v[k + 2], v[k + 3]});
-    } else {
-        for (int j = 0; j < kPer; ++j)
-            if (channel<WIDE>(j) < cols) row[channel<WIDE>(j)] = T(v[j]);
+    __device__ __forceinline__ void get(float (&v)[kPer]) const {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if constexpr (WIDE) v[j] = to_f32(piece[j / (16 / int(sizeof(T)))][j % (16 / int(sizeof(T)))]);
+            else v[j] = to_f32(one[j]);
+        }
     }
-}
+    __device__ __forceinline__ void store(T *row, int cols, const float (&v)[kPer]) {
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) piece[j / (16 / int(sizeof(T)))][j % (16 / int(sizeof(T)))] = T(v[j]);
+            if (int(threadIdx.x) * kPer < cols)
+#pragma unroll
+                for (int k = 0; k < kPieces; ++k) *reinterpret_cast<Piece *>(row + channel<WIDE>(0) + k * (16 / int(sizeof(T)))) = piece[k];
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (channel<WIDE>(j) < cols) row[channel<WIDE>(j)] = T(v[j]);
+        }
+    }
+};
+
 // A vector over the channels, `other` where there is none.
 template <bool WIDE> __device__ __forceinline__ void load_vector(const float *p, int cols, float other, float (&v)[kPer]) {
+#pragma unroll
     for (int j = 0; j < kPer; ++j) v[j] = p && channel<WIDE>(j) < cols ? p[channel<WIDE>(j)] : other;
 }
 
+// Sum over 16 lanes, the same bits in each: a tree of rotations.
+template <int CTRL> __device__ __forceinline__ float rotated(float x) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float sum16(float x) {
+    x += rotated<0x128>(x);      // row_ror:8, 4, 2, 1
+    x += rotated<0x124>(x);
+    x += rotated<0x122>(x);
+    return x + rotated<0x121>(x);
+}
+__device__ __forceinline__ float lane_of(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
+
 // N sums over the workgroup, the same in every thread.  `turn` alternates between two buffers, so that one barrier a
 // round is enough: a buffer is written again only after everybody has passed the next round's barrier.
-template <int N> __device__ __forceinline__ void block_sum(float (&v)[N], float (*buf)[kMaxWaves][4], int &turn) {
-    for (int k = 0; k < N; ++k)
-        for (int d = 32; d; d >>= 1) v[k] += __shfl_xor(v[k], d);
+struct Exchange {
+    f32x4 (*buf)[kMaxWaves];
+    int turn;
+};
+template <int N> __device__ __forceinline__ void block_sum(float (&v)[N], Exchange &x) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const float s = sum16(v[k]);
+        v[k] = (lane_of(s, 0) + lane_of(s, 16)) + (lane_of(s, 32) + lane_of(s, 48));
+    }
     const int waves = blockDim.x / kWave;
     if (waves == 1) return;
-    float(*b)[4] = buf[turn];
-    turn ^= 1;
-    if (threadIdx.x % kWave == 0)
-        for (int k = 0; k < N; ++k) b[threadIdx.x / kWave][k] = v[k];
+    f32x4 *b = x.buf[x.turn];
+    x.turn ^= 1;
+    if (threadIdx.x % kWave == 0) {
+        f32x4 q = {0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < N; ++k) q[k] = v[k];
+        b[threadIdx.x / kWave] = q;
+    }
     __syncthreads();
-    for (int k = 0; k < N; ++k) v[k] = 0;
-    for (int w = 0; w < waves; ++w)
-        for (int k = 0; k < N; ++k) v[k] += b[w][k];
+    const int w = threadIdx.x % 16;
+    const f32x4 q = w < waves ? b[w] : f32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = sum16(q[k]);
 }
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
+__device__ __forceinline__ float rstd_of(float squares, float inv_cols, float eps) { return 1.0f / sqrtf(squares * inv_cols + eps); }
 
-// v - mean (LAYER), and 1 / sqrt(mean of squares + eps) of what is left.  Channels beyond cols stay 0.
-template <bool WIDE>
-__device__ __forceinline__ float center(float (&v)[kPer], int kind, int cols, float eps, float (*buf)[kMaxWaves][4], int &turn) {
-    if (kind == HARP_NORM_LAYER) {
-        float s[1] = {0};
-        for (int j = 0; j < kPer; ++j) s[0] += v[j];
-        block_sum(s, buf, turn);
-        const float mean = s[0] / float(cols);
-        for (int j = 0; j < kPer; ++j)
-            if (channel<WIDE>(j) < cols) v[j] -= mean;
-    }
-    float s[1] = {0};
-    for (int j = 0; j < kPer; ++j) s[0] += v[j] * v[j];
-    block_sum(s, buf, turn);
-    return 1.0f / sqrtf(s[0] / float(cols) + eps);
+template <bool WIDE> __device__ __forceinline__ void subtract(float (&v)[kPer], float mean, int cols) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+        if (channel<WIDE>(j) < cols) v[j] -= mean;           // channels beyond cols stay 0
 }
 
-template <typename T, bool WIDE>
+// v - mean (LAYER), and 1 / sqrt(mean of squares + eps) of what is left.
+template <bool WIDE> __device__ __forceinline__ float center(float (&v)[kPer], int kind, int cols, float eps, Exchange &x) {
+    const float inv_cols = 1.0f / float(cols);
+    if (kind == HARP_NORM_LAYER) {
+        float s[1] = {0};
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) s[0] += v[j];
+        block_sum(s, x);
+        subtract<WIDE>(v, s[0] * inv_cols, cols);
+    }
+    float s[1] = {0};
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) s[0] += v[j] * v[j];
+    block_sum(s, x);
+    return rstd_of(s[0], inv_cols, eps);
+}
+
+// BIAS: there is a b_after or b_before.
+template <typename T, bool WIDE, bool BIAS>
 __global__ __launch_bounds__(kMaxThreads) void norm_forward(Form f, const T *x, int64_t ldx, const T *y, int64_t ldy, T *h,
                                                             int64_t ldh, T *z, int64_t ldz) {
-    __shared__ float buf[2][kMaxWaves][4];
-    int turn = 0;
+    __shared__ f32x4 buf[2][kMaxWaves];
+    Exchange ex = {buf, 0};
     const int cols = f.cols;
     float wa[kPer], ba[kPer], wb[kPer], bb[kPer], sc[kPer];
-    load_vector<WIDE>(f.w_after, cols, 1.0f, wa);
-    load_vector<WIDE>(f.b_after, cols, 0.0f, ba);
-    load_vector<WIDE>(f.w_before, cols, 1.0f, wb);
-    load_vector<WIDE>(f.b_before, cols, 0.0f, bb);
     load_vector<WIDE>(f.scale, cols, 1.0f, sc);
+    load_vector<WIDE>(f.w_after, cols, 1.0f, wa);
+    load_vector<WIDE>(f.w_before, cols, 1.0f, wb);
+    load_vector<WIDE>(BIAS ? f.b_after : nullptr, cols, 0.0f, ba);
+    load_vector<WIDE>(BIAS ? f.b_before : nullptr, cols, 0.0f, bb);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        wa[j] *= sc[j];
+        ba[j] *= sc[j];
+    }
+    Raw<T, WIDE> next_x, next_y;
+    auto ask = [&](int64_t r) {
+        if (y) next_y.load(y + r * ldy, cols);
+        if (x) next_x.load(x + r * ldx, cols);
+    };
+    ask(blockIdx.x);                                     // there are no more workgroups than rows
     for (int64_t r = blockIdx.x; r < f.rows; r += gridDim.x) {
-        float a[kPer], v[kPer];
+        float v[kPer];
+        Raw<T, WIDE> here_x = next_x, gate;
+        if (f.gate && y) gate.load(static_cast<const T *>(f.gate) + r / f.rows_per_gate * f.ldgate, cols);
+        if (y) next_y.get(v);
+        else next_x.get(v);
+        if (r + gridDim.x < f.rows) ask(r + gridDim.x);
         if (y) {
-            load_row<T, WIDE>(y + r * ldy, cols, v);
-            if (x) load_row<T, WIDE>(x + r * ldx, cols, a);
-            if (f.after != HARP_NORM_NONE) {
-                const float rstd = center<WIDE>(v, f.after, cols, f.eps_after, buf, turn);
-                for (int j = 0; j < kPer; ++j) v[j] = v[j] * rstd * wa[j] + ba[j];
-            }
+            float rstd = 1.0f;
+            if (f.after != HARP_NORM_NONE) rstd = center<WIDE>(v, f.after, cols, f.eps_after, ex);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[j] = BIAS ? v[j] * rstd * wa[j] + ba[j] : v[j] * rstd * wa[j];
             if (f.gate) {
                 float g[kPer];
-                load_row<T, WIDE>(static_cast<const T *>(f.gate) + r / f.rows_per_gate * f.ldgate, cols, g);
+                gate.get(g);
+#pragma unroll
                 for (int j = 0; j < kPer; ++j) v[j] *= f.gate_act == HARP_GATE_SIGMOID ? sigmoid(g[j]) : g[j];
             }
-            for (int j = 0; j < kPer; ++j) v[j] = channel<WIDE>(j) < cols ? v[j] * sc[j] : 0.0f;
-            if (x)
+            if (x) {
+                float a[kPer];
+                here_x.get(a);
+#pragma unroll
                 for (int j = 0; j < kPer; ++j) v[j] += a[j];
-            if (h) store_row<T, WIDE>(h + r * ldh, cols, v);
-        } else {
-            load_row<T, WIDE>(x + r * ldx, cols, v);
+            }
+            if (h) here_x.store(h + r * ldh, cols, v);
         }
         if (f.before != HARP_NORM_NONE) {
-            const float rstd = center<WIDE>(v, f.before, cols, f.eps_before, buf, turn);
-            for (int j = 0; j < kPer; ++j) v[j] = v[j] * rstd * wb[j] + bb[j];
-            store_row<T, WIDE>(z + r * ldz, cols, v);
+            const float rstd = center<WIDE>(v, f.before, cols, f.eps_before, ex);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[j] = BIAS ? v[j] * rstd * wb[j] + bb[j] : v[j] * rstd * wb[j];
+            here_x.store(z + r * ldz, cols, v);
         }
     }
 }
@@ -163,107 +234,233 @@ __device__ __forceinline__ float through(float d, float a, float rstd, float c0,
     return (d - m - a * (rstd * rstd) * (c1 * inv_cols)) * rstd;
 }
 
-template <typename T, bool WIDE>
+// With D the gradient of h, n = the normalised y, f the gate's factor, the sums over rows are all made of four:
+//   A1 = sum D f n, A0 = sum D f:   dw_after = scale A1, db_after = scale A0, dscale = w_after A1 + b_after A0
+//   B1 = sum dz n(h), B0 = sum dz:  dw_before, db_before
+// and a gate's f is the same for all rows of its group: with G1 = sum D n, G0 = sum D over them A1 = f G1, A0 = f G0 and
+// dgate = f' scale (w_after G1 + b_after G0).  A slab inside one group (GROUPS false) adds up G alone.
+// BIAS: there is a b_after, or db_after or db_before is wanted; without, A0, B0 and G0 are not needed.
+// The statistics of both norms are summed in one round, what the second gradient needs in another; the next row is
+// asked for before the current one is worked on.
+enum { kA1, kB1, kA0, kB0 };
+template <typename T, bool WIDE, bool BIAS, bool GROUPS>
 __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs, const T *dh, int64_t lddh, const T *dz, int64_t lddz,
                                                              const T *h, int64_t ldh, const T *y, int64_t ldy, T *dx, int64_t lddx,
                                                              T *dy, int64_t lddy, T *dgate, int64_t lddgate, float *partial,
                                                              float *gate_partial) {
-    __shared__ float buf[2][kMaxWaves][4];
-    int turn = 0;
+    __shared__ f32x4 buf[2][kMaxWaves];
+    Exchange ex = {buf, 0};
     const int cols = f.cols;
     const float inv_cols = 1.0f / float(cols);
-    float wa[kPer], ba[kPer], wb[kPer], sc[kPer];
-    load_vector<WIDE>(f.w_after, cols, 1.0f, wa);
-    load_vector<WIDE>(f.b_after, cols, 0.0f, ba);
-    load_vector<WIDE>(f.w_before, cols, 1.0f, wb);
-    load_vector<WIDE>(f.scale, cols, 1.0f, sc);
-    float sum[kSums][kPer] = {}, dg[kPer] = {};
     int64_t begin, end;
     slab_rows(slabs, f.rows, blockIdx.x, begin, end);
-    for (int64_t r = begin; r < end; ++r) {
-        float d[kPer];                                   // D, the gradient of h
-        if (dh) load_row<T, WIDE>(dh + r * lddh, cols, d);
-        else for (int j = 0; j < kPer; ++j) d[j] = 0;
-        if (dz) {
-            float a[kPer], e[kPer];
-            load_row<T, WIDE>(h + r * ldh, cols, a);
-            load_row<T, WIDE>(dz + r * lddz, cols, e);
-            const float rstd = center<WIDE>(a, f.before, cols, f.eps_before, buf, turn);
-            float c[2] = {0, 0};
-            for (int j = 0; j < kPer; ++j) {
-                sum[3][j] += e[j] * (a[j] * rstd);
-                sum[4][j] += e[j];
-                e[j] *= wb[j];
-                c[0] += e[j];
-                c[1] += e[j] * a[j];
-            }
-            block_sum(c, buf, turn);
-            for (int j = 0; j < kPer; ++j) d[j] += through(e[j], a[j], rstd, c[0], c[1], f.before, inv_cols);
-        }
-        if (dx) store_row<T, WIDE>(dx + r * lddx, cols, d);
-        if (!y) continue;
-        float a[kPer], g[kPer];
-        load_row<T, WIDE>(y + r * ldy, cols, a);
-        float rstd = 1.0f;
-        if (f.after != HARP_NORM_NONE) rstd = center<WIDE>(a, f.after, cols, f.eps_after, buf, turn);
-        if (f.gate) load_row<T, WIDE>(static_cast<const T *>(f.gate) + r / f.rows_per_gate * f.ldgate, cols, g);
-        float c[2] = {0, 0};
+
+    float wb[kPer], c[kPer];                             // c: scale w_after, times the gate's factor where that is one vector
+    float B1[kPer] = {}, B0[kPer] = {}, A1[kPer] = {}, A0[kPer] = {}, G1[kPer] = {}, G0[kPer] = {};
+    auto gate_of = [&](int64_t r, float (&factor)[kPer], float (&slope)[kPer]) {
+        Raw<T, WIDE> raw;
+        raw.load(static_cast<const T *>(f.gate) + r / f.rows_per_gate * f.ldgate, cols);
+        raw.get(factor);
+#pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            if (channel<WIDE>(j) >= cols) d[j] = 0;
-            const float hat = a[j] * rstd, t = hat * wa[j] + ba[j];
-            float factor = 1.0f, slope = 1.0f;
-            if (f.gate) {
-                factor = g[j];
-                if (f.gate_act == HARP_GATE_SIGMOID) {
-                    factor = sigmoid(g[j]);
-                    slope = factor * (1.0f - factor);
-                }
-                dg[j] += d[j] * t * sc[j] * slope;
+            slope[j] = 1.0f;
+            if (f.gate_act == HARP_GATE_SIGMOID) {
+                factor[j] = sigmoid(factor[j]);
+                slope[j] = factor[j] * (1.0f - factor[j]);
             }
-            sum[2][j] += d[j] * t * factor;
-            d[j] *= factor * sc[j];
-            sum[0][j] += d[j] * hat;
-            sum[1][j] += d[j];
-            d[j] *= wa[j];
-            c[0] += d[j];
-            c[1] += d[j] * a[j];
         }
-        if (f.after != HARP_NORM_NONE) {
-            block_sum(c, buf, turn);
-            for (int j = 0; j < kPer; ++j) d[j] = through(d[j], a[j], rstd, c[0], c[1], f.after, inv_cols);
-        }
-        if (dy) store_row<T, WIDE>(dy + r * lddy, cols, d);
-        if (dgate && slabs.per_group == 0 && (r + 1 == f.rows || (r + 1) % f.rows_per_gate == 0)) {
-            store_row<T, WIDE>(dgate + r / f.rows_per_gate * lddgate, cols, dg);
-            for (int j = 0; j < kPer; ++j) dg[j] = 0;
+    };
+    load_vector<WIDE>(f.w_before, cols, 1.0f, wb);
+    load_vector<WIDE>(f.scale, cols, 1.0f, c);
+    {
+        float wa[kPer];
+        load_vector<WIDE>(f.w_after, cols, 1.0f, wa);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) c[j] *= wa[j];
+        if (!GROUPS && f.gate && begin < end) {
+            float factor[kPer], slope[kPer];
+            gate_of(begin, factor, slope);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) c[j] *= factor[j];
         }
     }
+    // A group is done: its gate's gradient, and its share of the sums.
+    auto close = [&](int64_t r, float *to_partial) {
+        float factor[kPer], slope[kPer], wa[kPer], ba[kPer], sc[kPer];
+        gate_of(r, factor, slope);
+        load_vector<WIDE>(f.w_after, cols, 1.0f, wa);
+        load_vector<WIDE>(BIAS ? f.b_after : nullptr, cols, 0.0f, ba);
+        load_vector<WIDE>(f.scale, cols, 1.0f, sc);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            A1[j] += factor[j] * G1[j];
+            const float s = BIAS ? wa[j] * G1[j] + ba[j] * G0[j] : wa[j] * G1[j];
+            slope[j] *= sc[j] * s;
+            if (BIAS) A0[j] += factor[j] * G0[j];
+            G1[j] = G0[j] = 0;
+        }
+        if (to_partial) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j)
+                if (channel<WIDE>(j) < cols) to_partial[channel<WIDE>(j)] = slope[j];
+        } else if (dgate) {
+            Raw<T, WIDE> raw;
+            raw.store(dgate + r / f.rows_per_gate * lddgate, cols, slope);
+        }
+    };
+
+    Raw<T, WIDE> next_h, next_dz, next_y, next_dh;
+    auto ask = [&](int64_t r) {
+        if (dz) {
+            next_h.load(h + r * ldh, cols);
+            next_dz.load(dz + r * lddz, cols);
+        }
+        if (y) next_y.load(y + r * ldy, cols);
+        if (dh) next_dh.load(dh + r * lddh, cols);
+    };
+    if (begin < end) ask(begin);
+    for (int64_t r = begin; r < end; ++r) {
+        float a[kPer] = {}, e[kPer] = {}, b[kPer] = {}, d[kPer] = {};
+        if (dz) {
+            next_h.get(a);
+            next_dz.get(e);
+        }
+        if (y) next_y.get(b);
+        if (dh) next_dh.get(d);
+        if (r + 1 < end) ask(r + 1);
+        if (f.before == HARP_NORM_LAYER || f.after == HARP_NORM_LAYER) {
+            float m[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                m[0] += a[j];
+                m[1] += b[j];
+            }
+            block_sum(m, ex);
+            if (f.before == HARP_NORM_LAYER) subtract<WIDE>(a, m[0] * inv_cols, cols);
+            if (f.after == HARP_NORM_LAYER) subtract<WIDE>(b, m[1] * inv_cols, cols);
+        }
+        float s[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            const float g = e[j] * wb[j];
+            s[0] += a[j] * a[j];
+            s[1] += g * a[j];
+            s[2] += g;
+            s[3] += b[j] * b[j];
+        }
+        block_sum(s, ex);
+        const float rstd_h = rstd_of(s[0], inv_cols, f.eps_before);
+        const float rstd_y = f.after != HARP_NORM_NONE ? rstd_of(s[3], inv_cols, f.eps_after) : 1.0f;
+        if (dz) {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                B1[j] += e[j] * (a[j] * rstd_h);
+                if (BIAS) B0[j] += e[j];
+                d[j] += through(e[j] * wb[j], a[j], rstd_h, s[2], s[1], f.before, inv_cols);
+            }
+        }
+        Raw<T, WIDE> out;
+        if (dx) out.store(dx + r * lddx, cols, d);
+        if (!y) continue;
+        float k[2] = {0, 0}, factor[kPer], slope[kPer];
+        if (GROUPS) gate_of(r, factor, slope);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if (!WIDE && channel<WIDE>(j) >= cols) d[j] = 0;
+            G1[j] += d[j] * (b[j] * rstd_y);
+            if (BIAS) G0[j] += d[j];
+            d[j] *= GROUPS ? c[j] * factor[j] : c[j];
+            if (WIDE && int(threadIdx.x) * kPer >= cols) d[j] = 0;
+            k[0] += d[j];
+            k[1] += d[j] * b[j];
+        }
+        if (f.after != HARP_NORM_NONE) {
+            block_sum(k, ex);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) d[j] = through(d[j], b[j], rstd_y, k[0], k[1], f.after, inv_cols);
+        }
+        if (dy) out.store(dy + r * lddy, cols, d);
+        if (GROUPS && (r + 1 == f.rows || (r + 1) % f.rows_per_gate == 0)) close(r, nullptr);
+    }
+    if (!GROUPS) {
+        if (f.gate && y && begin < end) {
+            close(begin, gate_partial ? gate_partial + int64_t(blockIdx.x) * cols : nullptr);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                A1[j] = G1[j];
+                A0[j] = G0[j];
+                if (gate_partial && channel<WIDE>(j) < cols) gate_partial[int64_t(blockIdx.x) * cols + channel<WIDE>(j)] = 0;
+            }
+        }
+    }
+    if (!partial) return;
+    constexpr int kSums = BIAS ? 4 : 2;
+    float *p = partial + int64_t(blockIdx.x) * kSums * cols;
+#pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int c = channel<WIDE>(j);
-        if (c >= cols) continue;
-        for (int k = 0; k < kSums; ++k) partial[(int64_t(blockIdx.x) * kSums + k) * cols + c] = sum[k][j];
-        if (gate_partial) gate_partial[int64_t(blockIdx.x) * cols + c] = dg[j];
+        const int at = channel<WIDE>(j);
+        if (at >= cols) continue;
+        p[kA1 * int64_t(cols) + at] = A1[j];
+        p[kB1 * int64_t(cols) + at] = B1[j];
+        if (BIAS) {
+            p[kA0 * int64_t(cols) + at] = A0[j];
+            p[kB0 * int64_t(cols) + at] = B0[j];
+        }
     }
 }
 
-// The slabs' partial sums to one vector each, in the slabs' order; one thread a channel.
-struct Sums { float *out[kSums]; };
-__global__ __launch_bounds__(256) void norm_sums(const float *partial, int64_t count, int cols, Sums sums, int accumulate) {
-    const int c = blockIdx.x * 256 + threadIdx.x, k = blockIdx.y;
-    if (c >= cols || !sums.out[k]) return;
-    float s = 0;
-    for (int64_t i = 0; i < count; ++i) s += partial[(i * kSums + k) * cols + c];
-    sums.out[k][c] = accumulate ? sums.out[k][c] + s : s;
+// Sums of the slabs' partial sums: 32 channels a workgroup, 32 threads to a channel, each a run of slabs in order, then
+// the runs in order.
+constexpr int kJoinCols = 32, kJoinRuns = 32;
+template <int N> __device__ __forceinline__ void join_runs(const float *partial, int64_t count, int64_t stride, int64_t pitch, int cols, float (&v)[N]) {
+    __shared__ float runs[N][kJoinRuns][kJoinCols + 1];
+    const int c = blockIdx.x * kJoinCols + threadIdx.x % kJoinCols, run = threadIdx.x / kJoinCols;
+    const int64_t each = (count + kJoinRuns - 1) / kJoinRuns, first = run * each, last = first + each < count ? first + each : count;
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = 0;
+    if (c < cols)
+#pragma unroll 4
+        for (int64_t i = first; i < last; ++i)
+#pragma unroll
+            for (int k = 0; k < N; ++k) v[k] += partial[i * stride + k * pitch + c];
+#pragma unroll
+    for (int k = 0; k < N; ++k) runs[k][run][threadIdx.x % kJoinCols] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        v[k] = 0;
+        if (run == 0)
+            for (int i = 0; i < kJoinRuns; ++i) v[k] += runs[k][i][threadIdx.x % kJoinCols];
+    }
+}
+struct Sums { float *dw_after, *db_after, *dscale, *dw_before, *db_before; };
+template <bool BIAS>
+__global__ __launch_bounds__(kJoinCols *kJoinRuns) void norm_sums(Form f, const float *partial, int64_t count, Sums out, int accumulate) {
+    constexpr int N = BIAS ? 4 : 2;
+    float v[N];
+    join_runs<N>(partial, count, int64_t(N) * f.cols, f.cols, f.cols, v);
+    const int c = blockIdx.x * kJoinCols + threadIdx.x;
+    if (threadIdx.x >= kJoinCols || c >= f.cols) return;
+    const float w = f.w_after ? f.w_after[c] : 1.0f, s = f.scale ? f.scale[c] : 1.0f;
+    auto put = [&](float *p, float x) {
+        if (p) p[c] = accumulate ? p[c] + x : x;
+    };
+    const float a0 = BIAS ? v[N > 2 ? kA0 : 0] : 0.0f, b0 = BIAS ? v[N > 2 ? kB0 : 0] : 0.0f;
+    put(out.dw_after, s * v[kA1]);
+    put(out.db_after, s * a0);
+    put(out.dscale, BIAS && f.b_after ? w * v[kA1] + f.b_after[c] * a0 : w * v[kA1]);
+    put(out.dw_before, v[kB1]);
+    put(out.db_before, b0);
 }
 template <typename T>
-__global__ __launch_bounds__(256) void gate_sums(const float *partial, int64_t per_group, int cols, T *dgate, int64_t lddgate,
-                                                 int64_t first_group) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(kJoinCols *kJoinRuns) void gate_sums(const float *partial, int64_t per_group, int cols, T *dgate, int64_t lddgate,
+                                                                  int64_t first_group) {
     const int64_t group = first_group + blockIdx.y;
-    if (c >= cols) return;
-    float s = 0;
-    for (int64_t i = 0; i < per_group; ++i) s += partial[(group * per_group + i) * cols + c];
-    dgate[group * lddgate + c] = T(s);
+    float v[1];
+    join_runs<1>(partial + group * per_group * cols, per_group, cols, 0, cols, v);
+    const int c = blockIdx.x * kJoinCols + threadIdx.x;
+    if (threadIdx.x < kJoinCols && c < cols) dgate[group * lddgate + c] = T(v[0]);
 }
 
 int threads_for(int cols) { return int(round_up(size_t((cols + kPer - 1) / kPer), kWave)); }
@@ -335,35 +532,50 @@ void run_forward(const harp_ctx *ctx, const harp_norm *n, const void *x, int64_t
                  void *z, int64_t ldz, hipStream_t st) {
     const int threads = threads_for(n->cols);
     const int64_t most = int64_t(ctx->n_cu) * (2048 / threads < 16 ? 2048 / threads : 16);
-    norm_forward<T, WIDE><<<dim3(uint32_t(n->rows < most ? n->rows : most)), dim3(threads), 0, st>>>(
-        form_of(n), static_cast<const T *>(x), ldx, static_cast<const T *>(y), ldy, static_cast<T *>(h), ldh, static_cast<T *>(z), ldz);
+    const dim3 grid(uint32_t(n->rows < most ? n->rows : most)), block(threads);
+#define RUN(BIAS) norm_forward<T, WIDE, BIAS><<<grid, block, 0, st>>>(form_of(n), static_cast<const T *>(x), ldx, static_cast<const T *>(y), ldy, static_cast<T *>(h), ldh, static_cast<T *>(z), ldz)
+    if (n->b_after || n->b_before) RUN(true);
+    else RUN(false);
+#undef RUN
 }
 
+constexpr int kMostSums = 4;
+
 template <typename T, bool WIDE>
-void run_backward(const harp_norm *n, const harp_norm_grads *g, const Slabs &s, float *partial, hipStream_t st) {
+void run_backward(const harp_norm *n, const harp_norm_grads *g, const Slabs &s, float *workspace, hipStream_t st) {
     const int threads = threads_for(n->cols);
-    float *gate_partial = s.per_group && g->dgate ? partial + s.count * kSums * n->cols : nullptr;
-    if (s.count > 0)
-        norm_backward<T, WIDE><<<dim3(uint32_t(s.count)), dim3(threads), 0, st>>>(
-            form_of(n), s, static_cast<const T *>(g->dh), g->lddh, static_cast<const T *>(g->dz), g->lddz,
-            static_cast<const T *>(g->h), g->ldh, static_cast<const T *>(g->y), g->ldy, static_cast<T *>(g->dx), g->lddx,
-            static_cast<T *>(g->dy), g->lddy, static_cast<T *>(g->dgate), g->lddgate, partial, gate_partial);
-    const uint32_t across = uint32_t((n->cols + 255) / 256);
-    const Sums sums = {{g->dw_after, g->db_after, g->dscale, g->dw_before, g->db_before}};
-    bool any = false;
-    for (int k = 0; k < kSums; ++k) any = any || sums.out[k];
-    if (any) norm_sums<<<dim3(across, kSums), dim3(256), 0, st>>>(partial, s.count, n->cols, sums, g->accumulate);
+    const bool bias = n->b_after || g->db_after || g->db_before;
+    const bool sums = g->dw_after || g->db_after || g->dscale || g->dw_before || g->db_before;
+    float *partial = sums ? workspace : nullptr;
+    float *gate_partial = s.per_group && g->dgate ? workspace + s.count * kMostSums * n->cols : nullptr;
+#define RUN(BIAS, GROUPS)                                                                                                          \
+    norm_backward<T, WIDE, BIAS, GROUPS><<<dim3(uint32_t(s.count)), dim3(threads), 0, st>>>(                                        \
+        form_of(n), s, static_cast<const T *>(g->dh), g->lddh, static_cast<const T *>(g->dz), g->lddz, static_cast<const T *>(g->h), \
+        g->ldh, static_cast<const T *>(g->y), g->ldy, static_cast<T *>(g->dx), g->lddx, static_cast<T *>(g->dy), g->lddy,            \
+        static_cast<T *>(g->dgate), g->lddgate, partial, gate_partial)
+    if (s.count > 0) {
+        const bool groups = n->gate && s.per_group == 0;
+        if (bias && groups) RUN(true, true);
+        else if (bias) RUN(true, false);
+        else if (groups) RUN(false, true);
+        else RUN(false, false);
+    }
+#undef RUN
+    const uint32_t across = uint32_t((n->cols + kJoinCols - 1) / kJoinCols);
+    const Sums out = {g->dw_after, g->db_after, g->dscale, g->dw_before, g->db_before};
+    if (sums && bias) norm_sums<true><<<dim3(across), dim3(kJoinCols * kJoinRuns), 0, st>>>(form_of(n), partial, s.count, out, g->accumulate);
+    else if (sums) norm_sums<false><<<dim3(across), dim3(kJoinCols * kJoinRuns), 0, st>>>(form_of(n), partial, s.count, out, g->accumulate);
     if (gate_partial) {
         const int64_t groups = s.count / s.per_group;
         for (int64_t first = 0; first < groups; first += 65535)
-            gate_sums<T><<<dim3(across, uint32_t(groups - first < 65535 ? groups - first : 65535)), dim3(256), 0, st>>>(
+            gate_sums<T><<<dim3(across, uint32_t(groups - first < 65535 ? groups - first : 65535)), dim3(kJoinCols * kJoinRuns), 0, st>>>(
                 gate_partial, s.per_group, n->cols, static_cast<T *>(g->dgate), g->lddgate, first);
     }
 }
 
 size_t workspace_for(const harp_ctx *ctx, const harp_norm *n) {
     const Slabs s = slabs_for(ctx, n);
-    return round_up(size_t(s.count) * (kSums + (s.per_group ? 1 : 0)) * size_t(n->cols) * 4, 256) + 256;
+    return round_up(size_t(s.count) * (kMostSums + (s.per_group ? 1 : 0)) * size_t(n->cols) * 4, 256) + 256;
 }
 
 }  // namespace
