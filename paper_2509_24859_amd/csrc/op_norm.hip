@@ -6,6 +6,8 @@
 // (weights, biases, scale, and in the backward pass the sums over rows) in registers throughout.
 #include <math.h>
 
+#include <type_traits>
+
 #include "harp_ctx.h"
 #include "ops_common.h"
 
@@ -17,6 +19,7 @@ namespace {
 constexpr int kPer = 8;                               // channels a thread holds
 constexpr int kMaxThreads = HARP_NORM_MAX_COLS / kPer;
 constexpr int kMaxWaves = kMaxThreads / kWave;
+constexpr int kFewThreads = 512;
 
 // Everything but the data, as the kernels see it.
 struct Form {
@@ -27,57 +30,66 @@ struct Form {
     const void *gate;
 };
 
-// The channels of thread t: 8 t .. 8 t + 7 where rows can be read in wide pieces, else t, t + blockDim, ...
-template <bool WIDE> __device__ __forceinline__ int channel(int j) {
-    return WIDE ? int(threadIdx.x) * kPer + j : int(threadIdx.x) + j * int(blockDim.x);
-}
+// The channels of a thread: 8 t .. 8 t + 7.
+__device__ __forceinline__ int channel(int j) { return int(threadIdx.x) * kPer + j; }
 
 // A thread's channels of a row as they are stored: what is asked for ahead of its use takes half the registers in 16 bits.
+// Pieces of 16 bytes; WIDE: every row begins at a multiple of 16 bytes and holds whole pieces.  Without, the pieces are read
+// where they lie (memory takes any alignment of elements: the backward pass of 2,313 rows of 1,155 floats 38 us element by
+// element, 33 so), and the last one of a row element by element.
 template <typename T, bool WIDE> struct Raw {
-    typedef T Piece __attribute__((ext_vector_type(16 / sizeof(T))));
-    static constexpr int kPieces = WIDE ? kPer * int(sizeof(T)) / 16 : 1;
+    static constexpr int kHold = 16 / int(sizeof(T)), kPieces = kPer / kHold;
+    typedef T Piece __attribute__((ext_vector_type(kHold)));
+    typedef Piece Loose __attribute__((aligned(sizeof(T))));
+    typedef typename std::conditional<WIDE, Piece, Loose>::type Stored;
     Piece piece[kPieces];
-    T one[WIDE ? 1 : kPer];
 
+    // In the row's last piece the elements that are there, the last one in the place of those that are not (no load waits
+    // for another to be chosen from); get() puts zeros there.
     __device__ __forceinline__ void load(const T *row, int cols) {
-        if constexpr (WIDE) {
-            if (int(threadIdx.x) * kPer < cols)
+        if (WIDE || channel(kPer) <= cols) {
 #pragma unroll
-                for (int k = 0; k < kPieces; ++k) piece[k] = *reinterpret_cast<const Piece *>(row + channel<WIDE>(0) + k * (16 / int(sizeof(T))));
-            else
+            for (int k = 0; k < kPieces; ++k) piece[k] = Piece(T(0.0f));
+            if (channel(kPer) <= cols)
 #pragma unroll
-                for (int k = 0; k < kPieces; ++k) piece[k] = Piece(T(0.0f));
+                for (int k = 0; k < kPieces; ++k) piece[k] = *reinterpret_cast<const Stored *>(row + channel(k * kHold));
         } else {
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) one[j] = channel<WIDE>(j) < cols ? row[channel<WIDE>(j)] : T(0.0f);
+            for (int j = 0; j < kPer; ++j) piece[j / kHold][j % kHold] = row[channel(j) < cols ? channel(j) : cols - 1];
         }
     }
-    __device__ __forceinline__ void get(float (&v)[kPer]) const {
+    __device__ __forceinline__ void get(float (&v)[kPer], int cols) const {
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            if constexpr (WIDE) v[j] = to_f32(piece[j / (16 / int(sizeof(T)))][j % (16 / int(sizeof(T)))]);
-            else v[j] = to_f32(one[j]);
+            v[j] = to_f32(T(piece[j / kHold][j % kHold]));
+            if (!WIDE && channel(j) >= cols) v[j] = 0;
         }
     }
     __device__ __forceinline__ void store(T *row, int cols, const float (&v)[kPer]) {
-        if constexpr (WIDE) {
+        row += channel(0);
 #pragma unroll
-            for (int j = 0; j < kPer; ++j) piece[j / (16 / int(sizeof(T)))][j % (16 / int(sizeof(T)))] = T(v[j]);
-            if (int(threadIdx.x) * kPer < cols)
+        for (int j = 0; j < kPer; ++j) piece[j / kHold][j % kHold] = T(v[j]);
+        if (channel(kPer) <= cols) {
 #pragma unroll
-                for (int k = 0; k < kPieces; ++k) *reinterpret_cast<Piece *>(row + channel<WIDE>(0) + k * (16 / int(sizeof(T)))) = piece[k];
-        } else {
+            for (int k = 0; k < kPieces; ++k) *reinterpret_cast<Stored *>(row + k * kHold) = piece[k];
+        } else if (!WIDE) {
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
-                if (channel<WIDE>(j) < cols) row[channel<WIDE>(j)] = T(v[j]);
+                if (channel(j) < cols) row[j] = T(v[j]);
         }
     }
 };
 
 // A vector over the channels, `other` where there is none.
-template <bool WIDE> __device__ __forceinline__ void load_vector(const float *p, int cols, float other, float (&v)[kPer]) {
+__device__ __forceinline__ void load_vector(const float *p, int cols, float other, float (&v)[kPer]) {
+    if (p) {
+        Raw<float, false> raw;
+        raw.load(p, cols);
+        raw.get(v, cols);
+    } else {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) v[j] = p && channel<WIDE>(j) < cols ? p[channel<WIDE>(j)] : other;
+        for (int j = 0; j < kPer; ++j) v[j] = other;
+    }
 }
 
 // Sum over 16 lanes, the same bits in each: a tree of rotations.
@@ -124,21 +136,21 @@ template <int N> __device__ __forceinline__ void block_sum(float (&v)[N], Exchan
 __device__ __forceinline__ float sigmoid(float x) { return 1.0f / (1.0f + __expf(-x)); }
 __device__ __forceinline__ float rstd_of(float squares, float inv_cols, float eps) { return 1.0f / sqrtf(squares * inv_cols + eps); }
 
-template <bool WIDE> __device__ __forceinline__ void subtract(float (&v)[kPer], float mean, int cols) {
+__device__ __forceinline__ void subtract(float (&v)[kPer], float mean, int cols) {
 #pragma unroll
     for (int j = 0; j < kPer; ++j)
-        if (channel<WIDE>(j) < cols) v[j] -= mean;           // channels beyond cols stay 0
+        if (channel(j) < cols) v[j] -= mean;           // channels beyond cols stay 0
 }
 
 // v - mean (LAYER), and 1 / sqrt(mean of squares + eps) of what is left.
-template <bool WIDE> __device__ __forceinline__ float center(float (&v)[kPer], int kind, int cols, float eps, Exchange &x) {
+__device__ __forceinline__ float center(float (&v)[kPer], int kind, int cols, float eps, Exchange &x) {
     const float inv_cols = 1.0f / float(cols);
     if (kind == HARP_NORM_LAYER) {
         float s[1] = {0};
 #pragma unroll
         for (int j = 0; j < kPer; ++j) s[0] += v[j];
         block_sum(s, x);
-        subtract<WIDE>(v, s[0] * inv_cols, cols);
+        subtract(v, s[0] * inv_cols, cols);
     }
     float s[1] = {0};
 #pragma unroll
@@ -147,58 +159,59 @@ template <bool WIDE> __device__ __forceinline__ float center(float (&v)[kPer], i
     return rstd_of(s[0], inv_cols, eps);
 }
 
-// BIAS: there is a b_after or b_before.
-template <typename T, bool WIDE, bool BIAS>
-__global__ __launch_bounds__(kMaxThreads) void norm_forward(Form f, const T *x, int64_t ldx, const T *y, int64_t ldy, T *h,
+// BIAS: there is a b_after or b_before.  MOST: threads of a workgroup at most; up to 512 of them a thread has 256 registers,
+// with 1,024 it has 128, and what does not fit goes through memory, row by row.
+template <typename T, bool WIDE, bool BIAS, int MOST>
+__global__ __launch_bounds__(MOST) void norm_forward(Form f, const T *x, int64_t ldx, const T *y, int64_t ldy, T *h,
                                                             int64_t ldh, T *z, int64_t ldz) {
     __shared__ f32x4 buf[2][kMaxWaves];
     Exchange ex = {buf, 0};
     const int cols = f.cols;
-    float wa[kPer], ba[kPer], wb[kPer], bb[kPer], sc[kPer];
-    load_vector<WIDE>(f.scale, cols, 1.0f, sc);
-    load_vector<WIDE>(f.w_after, cols, 1.0f, wa);
-    load_vector<WIDE>(f.w_before, cols, 1.0f, wb);
-    load_vector<WIDE>(BIAS ? f.b_after : nullptr, cols, 0.0f, ba);
-    load_vector<WIDE>(BIAS ? f.b_before : nullptr, cols, 0.0f, bb);
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        wa[j] *= sc[j];
-        ba[j] *= sc[j];
-    }
     Raw<T, WIDE> next_x, next_y;
     auto ask = [&](int64_t r) {
         if (y) next_y.load(y + r * ldy, cols);
         if (x) next_x.load(x + r * ldx, cols);
     };
     ask(blockIdx.x);                                     // there are no more workgroups than rows
+    float wa[kPer], ba[kPer], wb[kPer], bb[kPer], sc[kPer];
+    load_vector(f.scale, cols, 1.0f, sc);
+    load_vector(f.w_after, cols, 1.0f, wa);
+    load_vector(f.w_before, cols, 1.0f, wb);
+    load_vector(BIAS ? f.b_after : nullptr, cols, 0.0f, ba);
+    load_vector(BIAS ? f.b_before : nullptr, cols, 0.0f, bb);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        wa[j] *= sc[j];
+        ba[j] *= sc[j];
+    }
     for (int64_t r = blockIdx.x; r < f.rows; r += gridDim.x) {
         float v[kPer];
         Raw<T, WIDE> here_x = next_x, gate;
         if (f.gate && y) gate.load(static_cast<const T *>(f.gate) + r / f.rows_per_gate * f.ldgate, cols);
-        if (y) next_y.get(v);
-        else next_x.get(v);
+        if (y) next_y.get(v, cols);
+        else next_x.get(v, cols);
         if (r + gridDim.x < f.rows) ask(r + gridDim.x);
         if (y) {
             float rstd = 1.0f;
-            if (f.after != HARP_NORM_NONE) rstd = center<WIDE>(v, f.after, cols, f.eps_after, ex);
+            if (f.after != HARP_NORM_NONE) rstd = center(v, f.after, cols, f.eps_after, ex);
 #pragma unroll
             for (int j = 0; j < kPer; ++j) v[j] = BIAS ? v[j] * rstd * wa[j] + ba[j] : v[j] * rstd * wa[j];
             if (f.gate) {
                 float g[kPer];
-                gate.get(g);
+                gate.get(g, cols);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) v[j] *= f.gate_act == HARP_GATE_SIGMOID ? sigmoid(g[j]) : g[j];
             }
             if (x) {
                 float a[kPer];
-                here_x.get(a);
+                here_x.get(a, cols);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) v[j] += a[j];
             }
             if (h) here_x.store(h + r * ldh, cols, v);
         }
         if (f.before != HARP_NORM_NONE) {
-            const float rstd = center<WIDE>(v, f.before, cols, f.eps_before, ex);
+            const float rstd = center(v, f.before, cols, f.eps_before, ex);
 #pragma unroll
             for (int j = 0; j < kPer; ++j) v[j] = BIAS ? v[j] * rstd * wb[j] + bb[j] : v[j] * rstd * wb[j];
             here_x.store(z + r * ldz, cols, v);
@@ -243,8 +256,8 @@ __device__ __forceinline__ float through(float d, float a, float rstd, float c0,
 // The statistics of both norms are summed in one round, what the second gradient needs in another; the next row is
 // asked for before the current one is worked on.
 enum { kA1, kB1, kA0, kB0 };
-template <typename T, bool WIDE, bool BIAS, bool GROUPS>
-__global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs, const T *dh, int64_t lddh, const T *dz, int64_t lddz,
+template <typename T, bool WIDE, bool BIAS, bool GROUPS, int MOST>
+__global__ __launch_bounds__(MOST) void norm_backward(Form f, Slabs slabs, const T *dh, int64_t lddh, const T *dz, int64_t lddz,
                                                              const T *h, int64_t ldh, const T *y, int64_t ldy, T *dx, int64_t lddx,
                                                              T *dy, int64_t lddy, T *dgate, int64_t lddgate, float *partial,
                                                              float *gate_partial) {
@@ -260,7 +273,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
     auto gate_of = [&](int64_t r, float (&factor)[kPer], float (&slope)[kPer]) {
         Raw<T, WIDE> raw;
         raw.load(static_cast<const T *>(f.gate) + r / f.rows_per_gate * f.ldgate, cols);
-        raw.get(factor);
+        raw.get(factor, cols);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             slope[j] = 1.0f;
@@ -270,11 +283,11 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
             }
         }
     };
-    load_vector<WIDE>(f.w_before, cols, 1.0f, wb);
-    load_vector<WIDE>(f.scale, cols, 1.0f, c);
+    load_vector(f.w_before, cols, 1.0f, wb);
+    load_vector(f.scale, cols, 1.0f, c);
     {
         float wa[kPer];
-        load_vector<WIDE>(f.w_after, cols, 1.0f, wa);
+        load_vector(f.w_after, cols, 1.0f, wa);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) c[j] *= wa[j];
         if (!GROUPS && f.gate && begin < end) {
@@ -288,9 +301,9 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
     auto close = [&](int64_t r, float *to_partial) {
         float factor[kPer], slope[kPer], wa[kPer], ba[kPer], sc[kPer];
         gate_of(r, factor, slope);
-        load_vector<WIDE>(f.w_after, cols, 1.0f, wa);
-        load_vector<WIDE>(BIAS ? f.b_after : nullptr, cols, 0.0f, ba);
-        load_vector<WIDE>(f.scale, cols, 1.0f, sc);
+        load_vector(f.w_after, cols, 1.0f, wa);
+        load_vector(BIAS ? f.b_after : nullptr, cols, 0.0f, ba);
+        load_vector(f.scale, cols, 1.0f, sc);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             A1[j] += factor[j] * G1[j];
@@ -302,7 +315,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
         if (to_partial) {
 #pragma unroll
             for (int j = 0; j < kPer; ++j)
-                if (channel<WIDE>(j) < cols) to_partial[channel<WIDE>(j)] = slope[j];
+                if (channel(j) < cols) to_partial[channel(j)] = slope[j];
         } else if (dgate) {
             Raw<T, WIDE> raw;
             raw.store(dgate + r / f.rows_per_gate * lddgate, cols, slope);
@@ -322,11 +335,11 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
     for (int64_t r = begin; r < end; ++r) {
         float a[kPer] = {}, e[kPer] = {}, b[kPer] = {}, d[kPer] = {};
         if (dz) {
-            next_h.get(a);
-            next_dz.get(e);
+            next_h.get(a, cols);
+            next_dz.get(e, cols);
         }
-        if (y) next_y.get(b);
-        if (dh) next_dh.get(d);
+        if (y) next_y.get(b, cols);
+        if (dh) next_dh.get(d, cols);
         if (r + 1 < end) ask(r + 1);
         if (f.before == HARP_NORM_LAYER || f.after == HARP_NORM_LAYER) {
             float m[2] = {0, 0};
@@ -336,8 +349,8 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
                 m[1] += b[j];
             }
             block_sum(m, ex);
-            if (f.before == HARP_NORM_LAYER) subtract<WIDE>(a, m[0] * inv_cols, cols);
-            if (f.after == HARP_NORM_LAYER) subtract<WIDE>(b, m[1] * inv_cols, cols);
+            if (f.before == HARP_NORM_LAYER) subtract(a, m[0] * inv_cols, cols);
+            if (f.after == HARP_NORM_LAYER) subtract(b, m[1] * inv_cols, cols);
         }
         float s[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -366,11 +379,10 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
         if (GROUPS) gate_of(r, factor, slope);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            if (!WIDE && channel<WIDE>(j) >= cols) d[j] = 0;
+            if (channel(j) >= cols) d[j] = 0;
             G1[j] += d[j] * (b[j] * rstd_y);
             if (BIAS) G0[j] += d[j];
             d[j] *= GROUPS ? c[j] * factor[j] : c[j];
-            if (WIDE && int(threadIdx.x) * kPer >= cols) d[j] = 0;
             k[0] += d[j];
             k[1] += d[j] * b[j];
         }
@@ -390,7 +402,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
             for (int j = 0; j < kPer; ++j) {
                 A1[j] = G1[j];
                 A0[j] = G0[j];
-                if (gate_partial && channel<WIDE>(j) < cols) gate_partial[int64_t(blockIdx.x) * cols + channel<WIDE>(j)] = 0;
+                if (gate_partial && channel(j) < cols) gate_partial[int64_t(blockIdx.x) * cols + channel(j)] = 0;
             }
         }
     }
@@ -399,7 +411,7 @@ __global__ __launch_bounds__(kMaxThreads) void norm_backward(Form f, Slabs slabs
     float *p = partial + int64_t(blockIdx.x) * kSums * cols;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
-        const int at = channel<WIDE>(j);
+        const int at = channel(j);
         if (at >= cols) continue;
         p[kA1 * int64_t(cols) + at] = A1[j];
         p[kB1 * int64_t(cols) + at] = B1[j];
@@ -468,7 +480,7 @@ int threads_for(int cols) { return int(round_up(size_t((cols + kPer - 1) / kPer)
 // As many workgroups as are resident: 1,024 threads a compute unit in the backward pass (it takes about 128 registers).
 Slabs slabs_for(const harp_ctx *ctx, const harp_norm *n) {
     Slabs s;
-    const int64_t want = int64_t(ctx->n_cu) * (kMaxThreads / threads_for(n->cols) < 16 ? kMaxThreads / threads_for(n->cols) : 16);
+    const int64_t want = int64_t(ctx->n_cu) * (kMaxThreads / threads_for(n->cols) < 3 ? kMaxThreads / threads_for(n->cols) : 3);
     s.rows = (n->rows + want - 1) / want;
     if (s.rows < 1) s.rows = 1;
     s.per_group = 0;
@@ -533,9 +545,12 @@ void run_forward(const harp_ctx *ctx, const harp_norm *n, const void *x, int64_t
     const int threads = threads_for(n->cols);
     const int64_t most = int64_t(ctx->n_cu) * (2048 / threads < 16 ? 2048 / threads : 16);
     const dim3 grid(uint32_t(n->rows < most ? n->rows : most)), block(threads);
-#define RUN(BIAS) norm_forward<T, WIDE, BIAS><<<grid, block, 0, st>>>(form_of(n), static_cast<const T *>(x), ldx, static_cast<const T *>(y), ldy, static_cast<T *>(h), ldh, static_cast<T *>(z), ldz)
-    if (n->b_after || n->b_before) RUN(true);
-    else RUN(false);
+#define RUN(BIAS, MOST) norm_forward<T, WIDE, BIAS, MOST><<<grid, block, 0, st>>>(form_of(n), static_cast<const T *>(x), ldx, static_cast<const T *>(y), ldy, static_cast<T *>(h), ldh, static_cast<T *>(z), ldz)
+    const bool bias = n->b_after || n->b_before;
+    if (bias && threads <= kFewThreads) RUN(true, kFewThreads);
+    else if (bias) RUN(true, kMaxThreads);
+    else if (threads <= kFewThreads) RUN(false, kFewThreads);
+    else RUN(false, kMaxThreads);
 #undef RUN
 }
 
@@ -548,17 +563,22 @@ void run_backward(const harp_norm *n, const harp_norm_grads *g, const Slabs &s, 
     const bool sums = g->dw_after || g->db_after || g->dscale || g->dw_before || g->db_before;
     float *partial = sums ? workspace : nullptr;
     float *gate_partial = s.per_group && g->dgate ? workspace + s.count * kMostSums * n->cols : nullptr;
-#define RUN(BIAS, GROUPS)                                                                                                          \
-    norm_backward<T, WIDE, BIAS, GROUPS><<<dim3(uint32_t(s.count)), dim3(threads), 0, st>>>(                                        \
+#define RUN(BIAS, GROUPS, MOST)                                                                                                     \
+    norm_backward<T, WIDE, BIAS, GROUPS, MOST><<<dim3(uint32_t(s.count)), dim3(threads), 0, st>>>(                                        \
         form_of(n), s, static_cast<const T *>(g->dh), g->lddh, static_cast<const T *>(g->dz), g->lddz, static_cast<const T *>(g->h), \
         g->ldh, static_cast<const T *>(g->y), g->ldy, static_cast<T *>(g->dx), g->lddx, static_cast<T *>(g->dy), g->lddy,            \
         static_cast<T *>(g->dgate), g->lddgate, partial, gate_partial)
     if (s.count > 0) {
         const bool groups = n->gate && s.per_group == 0;
-        if (bias && groups) RUN(true, true);
-        else if (bias) RUN(true, false);
-        else if (groups) RUN(false, true);
-        else RUN(false, false);
+        const bool few = threads <= kFewThreads;
+        if (bias && groups && few) RUN(true, true, kFewThreads);
+        else if (bias && groups) RUN(true, true, kMaxThreads);
+        else if (bias && few) RUN(true, false, kFewThreads);
+        else if (bias) RUN(true, false, kMaxThreads);
+        else if (groups && few) RUN(false, true, kFewThreads);
+        else if (groups) RUN(false, true, kMaxThreads);
+        else if (few) RUN(false, false, kFewThreads);
+        else RUN(false, false, kMaxThreads);
     }
 #undef RUN
     const uint32_t across = uint32_t((n->cols + kJoinCols - 1) / kJoinCols);
