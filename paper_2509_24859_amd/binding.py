@@ -150,9 +150,15 @@ def load_library() -> C.CDLL:
     return lib
 
 
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _stream_handle(stream=None) -> int:

@@ -35,17 +35,17 @@ def _type(t, allowed=(F32, BF16, F16)) -> int:
     return code
 
 
-def _on(ctx: Context, *tensors):
-    for t in tensors:
-        if t is not None and t.device != ctx.device:
-            raise HarpError(ERR_INVALID_ARG, "a tensor on %s, the context is on %s" % (t.device, ctx.device))
+def _elsewhere(ctx, t, name):
+    return HarpError(ERR_INVALID_ARG, "%s is on %s, the context is on %s" % (name, t.device, ctx.device))
 
 
-def _vector(t, n, dtype, name):
-    """A contiguous vector of n elements, or None."""
+def _vector(ctx, t, n, dtype, name):
+    """The address of a contiguous vector of n elements, or None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+    if t.get_device() != ctx.device.index:
+        raise _elsewhere(ctx, t, name)
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise HarpError(ERR_SHAPE, "%s: %d contiguous elements of %s are wanted, got %s of %s"
                         % (name, n, dtype, tuple(t.shape), t.dtype))
     return t.data_ptr()
@@ -60,33 +60,40 @@ def _named(value, names):
     return int(value)
 
 
-def _matrix(t, rows, cols, dtype, name):
-    """(pointer, leading dimension) of a matrix whose rows are contiguous; (None, cols) for None."""
+def _matrix(ctx, t, shape, dtype, name):
+    """(address, leading dimension) of a matrix whose rows are contiguous; (None, columns) for None."""
     if t is None:
-        return None, cols
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise HarpError(ERR_SHAPE, "%s: %s of %s is wanted, got %s of %s" % (name, (rows, cols), dtype, tuple(t.shape), t.dtype))
+        return None, shape[1]
+    if t.get_device() != ctx.device.index:
+        raise _elsewhere(ctx, t, name)
+    if t.dtype is not dtype or t.shape != shape:
+        raise HarpError(ERR_SHAPE, "%s: %s of %s is wanted, got %s of %s" % (name, tuple(shape), dtype, tuple(t.shape), t.dtype))
+    rows, cols = shape
     row, col = t.stride()
     if (col != 1 and cols > 1) or (row < cols and rows > 1):
         raise HarpError(ERR_SHAPE, "%s: rows must be contiguous and apart, its strides are %s" % (name, (row, col)))
-    return t.data_ptr(), row if rows > 1 else max(row, cols)
+    return t.data_ptr(), row if row > cols else cols
 
 
 def _stream(ctx: Context, stream, tensors):
     """The stream's handle.  Tensors used on another stream than torch's current one are recorded there, so that
     their memory is not handed out again before the call has run."""
-    torch = _torch()
-    current = torch.cuda.current_stream(ctx.device)
-    if stream is None or stream == current:
-        return int(current.cuda_stream)
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
+    if stream is None:
+        raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)      # the handle without an object around it
+        return raw(ctx.device.index) if raw else int(_torch().cuda.current_stream(ctx.device).cuda_stream)
+    if stream != _torch().cuda.current_stream(ctx.device):
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
     return int(stream.cuda_stream)
 
 
-def _workspace(w):
-    return (None, 0) if w is None else (w.data_ptr(), w.numel() * w.element_size())
+def _workspace(ctx, w):
+    if w is None:
+        return None, 0
+    if w.get_device() != ctx.device.index:
+        raise _elsewhere(ctx, w, "the workspace")
+    return w.data_ptr(), w.numel() * w.element_size()
 
 
 class harp_linear(C.Structure):
@@ -126,24 +133,22 @@ def harp_linear_forward(ctx: Context, x, w, y, bias=None, act="none", residual=N
     """Z = x w^T + bias,  y = act(Z) + residual; see include/harp.h.  z: receives Z, or None."""
     _two(x, w, "x", "w")
     (m, k), n, t = x.shape, w.shape[0], x.dtype
-    tensors = (x, w, y, bias, residual, z, workspace)
-    _on(ctx, *tensors)
-    a = harp_linear(m, n, k, _type(x, (BF16, F16)), _named(act, _ACTS), *_matrix(x, m, k, t, "x"), *_matrix(w, n, k, t, "w"),
-                    _vector(bias, n, t, "bias"), *_matrix(residual, m, n, t, "residual"), *_matrix(y, m, n, t, "y"),
-                    *_matrix(z, m, n, t, "z"))
-    ctx.check(ctx.lib.harp_linear_forward(ctx.handle, C.byref(a), *_workspace(workspace), _stream(ctx, stream, tensors)))
+    tensors, out = (x, w, y, bias, residual, z, workspace), (m, n)
+    a = harp_linear(m, n, k, _type(x, (BF16, F16)), _named(act, _ACTS), *_matrix(ctx, x, (m, k), t, "x"),
+                    *_matrix(ctx, w, (n, k), t, "w"), _vector(ctx, bias, n, t, "bias"),
+                    *_matrix(ctx, residual, out, t, "residual"), *_matrix(ctx, y, out, t, "y"), *_matrix(ctx, z, out, t, "z"))
+    ctx.check(ctx.lib.harp_linear_forward(ctx.handle, C.byref(a), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))
 
 
 def harp_linear_grad_input(ctx: Context, dy, w, dx, act="none", z=None, residual=None, workspace=None, stream=None):
     """dx = (dy w) * act'(z) + residual; see include/harp.h."""
     _two(dy, w, "dy", "w")
     (m, n), k, t = dy.shape, w.shape[1], dy.dtype
-    tensors = (dy, w, dx, z, residual, workspace)
-    _on(ctx, *tensors)
-    a = harp_linear_input(m, n, k, _type(dy, (BF16, F16)), _named(act, _ACTS), *_matrix(dy, m, n, t, "dy"),
-                          *_matrix(w, n, k, t, "w"), *_matrix(z, m, k, t, "z"), *_matrix(residual, m, k, t, "residual"),
-                          *_matrix(dx, m, k, t, "dx"))
-    ctx.check(ctx.lib.harp_linear_grad_input(ctx.handle, C.byref(a), *_workspace(workspace), _stream(ctx, stream, tensors)))
+    tensors, out = (dy, w, dx, z, residual, workspace), (m, k)
+    a = harp_linear_input(m, n, k, _type(dy, (BF16, F16)), _named(act, _ACTS), *_matrix(ctx, dy, (m, n), t, "dy"),
+                          *_matrix(ctx, w, (n, k), t, "w"), *_matrix(ctx, z, out, t, "z"),
+                          *_matrix(ctx, residual, out, t, "residual"), *_matrix(ctx, dx, out, t, "dx"))
+    ctx.check(ctx.lib.harp_linear_grad_input(ctx.handle, C.byref(a), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))
 
 
 def harp_linear_grad_weight(ctx: Context, dy, x, dw, dbias=None, accumulate=False, workspace=None, stream=None):
@@ -151,21 +156,20 @@ def harp_linear_grad_weight(ctx: Context, dy, x, dw, dbias=None, accumulate=Fals
     _two(dy, x, "dy", "x")
     (m, n), k, t = dy.shape, x.shape[1], dy.dtype
     tensors = (dy, x, dw, dbias, workspace)
-    _on(ctx, *tensors)
-    a = harp_linear_weight(m, n, k, _type(dy, (BF16, F16)), _type(dw), int(bool(accumulate)), *_matrix(dy, m, n, t, "dy"),
-                           *_matrix(x, m, k, t, "x"), *_matrix(dw, n, k, dw.dtype, "dw"),
-                           _vector(dbias, n, _torch().float32, "dbias"))
-    ctx.check(ctx.lib.harp_linear_grad_weight(ctx.handle, C.byref(a), *_workspace(workspace), _stream(ctx, stream, tensors)))
+    a = harp_linear_weight(m, n, k, _type(dy, (BF16, F16)), _type(dw), int(bool(accumulate)), *_matrix(ctx, dy, (m, n), t, "dy"),
+                           *_matrix(ctx, x, (m, k), t, "x"), *_matrix(ctx, dw, (n, k), dw.dtype, "dw"),
+                           _vector(ctx, dbias, n, _torch().float32, "dbias"))
+    ctx.check(ctx.lib.harp_linear_grad_weight(ctx.handle, C.byref(a), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))
 
 
 def harp_act_grad(ctx: Context, dy, z, dz, act, stream=None):
     """dz = dy * act'(z); see include/harp.h."""
     _two(dy, z, "dy", "z")
     (m, n), t = dy.shape, dy.dtype
-    tensors = (dy, z, dz)
-    _on(ctx, *tensors)
-    ctx.check(ctx.lib.harp_act_grad(ctx.handle, m, n, _type(dy), _named(act, _ACTS), *_matrix(dy, m, n, t, "dy"),
-                                    *_matrix(z, m, n, t, "z"), *_matrix(dz, m, n, t, "dz"), _stream(ctx, stream, tensors)))
+    tensors, all_of = (dy, z, dz), (m, n)
+    ctx.check(ctx.lib.harp_act_grad(ctx.handle, m, n, _type(dy), _named(act, _ACTS), *_matrix(ctx, dy, all_of, t, "dy"),
+                                    *_matrix(ctx, z, all_of, t, "z"), *_matrix(ctx, dz, all_of, t, "dz"),
+                                    _stream(ctx, stream, tensors)))
 
 
 class harp_adamw_tensor(C.Structure):
@@ -207,24 +211,23 @@ class AdamW:
             eight = t["m"].dtype == torch.uint8
             kind = torch.uint8 if eight else torch.float32
             a.n, a.state = n, STATE_8BIT if eight else STATE_F32
-            a.p = _vector(t["p"], n, torch.float32, "p")
+            a.p = _vector(ctx, t["p"], n, torch.float32, "p")
             a.grad_type = _type(t["grad"])
-            a.grad = _vector(t["grad"], n, t["grad"].dtype, "grad")
-            a.m, a.v = _vector(t["m"], n, kind, "m"), _vector(t["v"], n, kind, "v")
+            a.grad = _vector(ctx, t["grad"], n, t["grad"].dtype, "grad")
+            a.m, a.v = _vector(ctx, t["m"], n, kind, "m"), _vector(ctx, t["v"], n, kind, "v")
             if eight:
                 blocks = -(-n // ADAMW_BLOCK)
                 if t.get("m_exp") is None or t.get("v_exp") is None:
                     raise HarpError(ERR_INVALID_ARG, "8-bit moments need m_exp and v_exp")
-                a.m_exp = _vector(t["m_exp"], blocks, torch.uint8, "m_exp")
-                a.v_exp = _vector(t["v_exp"], blocks, torch.uint8, "v_exp")
+                a.m_exp = _vector(ctx, t["m_exp"], blocks, torch.uint8, "m_exp")
+                a.v_exp = _vector(ctx, t["v_exp"], blocks, torch.uint8, "v_exp")
             if t.get("copy") is not None:
                 a.copy_type = _type(t["copy"], (BF16, F16))
-                a.copy = _vector(t["copy"], n, t["copy"].dtype, "copy")
-            a.m_seen = _vector(t.get("m_seen"), n, torch.bfloat16, "m_seen")
-            a.v_seen = _vector(t.get("v_seen"), n, torch.bfloat16, "v_seen")
+                a.copy = _vector(ctx, t["copy"], n, t["copy"].dtype, "copy")
+            a.m_seen = _vector(ctx, t.get("m_seen"), n, torch.bfloat16, "m_seen")
+            a.v_seen = _vector(ctx, t.get("v_seen"), n, torch.bfloat16, "v_seen")
             a.weight_decay = float(t.get("weight_decay", 0.0))
             held += [x for x in t.values() if isinstance(x, torch.Tensor)]
-        _on(ctx, *held)
         self.held = held
         nbytes = ctx.lib.harp_adamw_plan_bytes(array, len(self.tensors))
         self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=ctx.device)
@@ -237,10 +240,9 @@ class AdamW:
         """One step.  grad_scale: a float32 scalar on the GPU that gradients are multiplied by; skip: an int32 one,
         not 0 leaves everything as it is; seed: of the rounding to 8 bits, another one every step."""
         torch = _torch()
-        _on(self.ctx, grad_scale, skip)
         hyper = harp_adamw_hyper(lr, beta1, beta2, eps, step, seed & ((1 << 64) - 1),
-                                 _vector(grad_scale, 1, torch.float32, "grad_scale"),
-                                 _vector(skip, 1, torch.int32, "skip"))
+                                 _vector(self.ctx, grad_scale, 1, torch.float32, "grad_scale"),
+                                 _vector(self.ctx, skip, 1, torch.int32, "skip"))
         self.ctx.check(self.ctx.lib.harp_adamw_step(self.ctx.handle, self.handle, C.byref(hyper),
                                                     self._on_stream(stream, grad_scale, skip)))
 
@@ -283,14 +285,14 @@ class harp_norm_grads(C.Structure):
 def _norm(ctx, rows, cols, dtype, after, before, eps, gate, rows_per_gate, gate_act, scale, w_after, b_after, w_before, b_before):
     f32 = _torch().float32
     n = harp_norm(rows, cols, _types[dtype], _named(after, _NORMS), _named(before, _NORMS), eps, eps,
-                  _vector(w_after, cols, f32, "w_after"), _vector(b_after, cols, f32, "b_after"),
-                  _vector(w_before, cols, f32, "w_before"), _vector(b_before, cols, f32, "b_before"),
-                  _vector(scale, cols, f32, "scale"))
+                  _vector(ctx, w_after, cols, f32, "w_after"), _vector(ctx, b_after, cols, f32, "b_after"),
+                  _vector(ctx, w_before, cols, f32, "w_before"), _vector(ctx, b_before, cols, f32, "b_before"),
+                  _vector(ctx, scale, cols, f32, "scale"))
     n.gate_act = _named(gate_act, _GATES)
     if gate is not None:
         if rows_per_gate < 1:
             raise HarpError(ERR_SHAPE, "rows_per_gate must be at least 1")
-        n.gate, n.ldgate = _matrix(gate, -(-rows // rows_per_gate), cols, dtype, "gate")
+        n.gate, n.ldgate = _matrix(ctx, gate, (-(-rows // rows_per_gate), cols), dtype, "gate")
         n.rows_per_gate = rows_per_gate
     return n
 
@@ -302,12 +304,12 @@ def harp_norm_forward(ctx: Context, x, y, h, z, after="rms", before="rms", gate=
     if first is None or first.dim() != 2:
         raise HarpError(ERR_INVALID_ARG, "x or y is wanted, as a matrix")
     _type(first)
-    (rows, cols), dtype = first.shape, first.dtype
+    all_of, dtype = first.shape, first.dtype
+    rows, cols = all_of
     tensors = (x, y, h, z, gate, scale, w_after, b_after, w_before, b_before)
-    _on(ctx, *tensors)
     n = _norm(ctx, rows, cols, dtype, after, before, eps, gate, rows_per_gate, gate_act, scale, w_after, b_after, w_before, b_before)
-    ctx.check(ctx.lib.harp_norm_forward(ctx.handle, C.byref(n), *_matrix(x, rows, cols, dtype, "x"), *_matrix(y, rows, cols, dtype, "y"),
-                                        *_matrix(h, rows, cols, dtype, "h"), *_matrix(z, rows, cols, dtype, "z"),
+    ctx.check(ctx.lib.harp_norm_forward(ctx.handle, C.byref(n), *_matrix(ctx, x, all_of, dtype, "x"), *_matrix(ctx, y, all_of, dtype, "y"),
+                                        *_matrix(ctx, h, all_of, dtype, "h"), *_matrix(ctx, z, all_of, dtype, "z"),
                                         _stream(ctx, stream, tensors)))
 
 
@@ -330,18 +332,18 @@ def harp_norm_backward(ctx: Context, dh, dz, h, y, dx, dy, after="rms", before="
     if first is None or first.dim() != 2:
         raise HarpError(ERR_INVALID_ARG, "dh or dz is wanted, as a matrix")
     _type(first)
-    (rows, cols), dtype, f32 = first.shape, first.dtype, _torch().float32
+    all_of, dtype, f32 = first.shape, first.dtype, _torch().float32
+    rows, cols = all_of
     sums = dict(dw_after=dw_after, db_after=db_after, dw_before=dw_before, db_before=db_before, dscale=dscale)
     tensors = (dh, dz, h, y, dx, dy, gate, scale, w_after, b_after, w_before, b_before, dgate, workspace, *sums.values())
-    _on(ctx, *tensors)
     n = _norm(ctx, rows, cols, dtype, after, before, eps, gate, rows_per_gate, gate_act, scale, w_after, b_after, w_before, b_before)
     g = harp_norm_grads()
     for name, t in (("dh", dh), ("dz", dz), ("h", h), ("y", y), ("dx", dx), ("dy", dy)):
-        p, ld = _matrix(t, rows, cols, dtype, name)
+        p, ld = _matrix(ctx, t, all_of, dtype, name)
         setattr(g, name, p)
         setattr(g, "ld" + name, ld)
-    g.dgate, g.lddgate = _matrix(dgate, -(-rows // rows_per_gate) if dgate is not None else 0, cols, dtype, "dgate")
+    g.dgate, g.lddgate = _matrix(ctx, dgate, (-(-rows // rows_per_gate) if dgate is not None else 0, cols), dtype, "dgate")
     for name, t in sums.items():
-        setattr(g, name, _vector(t, cols, f32, name))
+        setattr(g, name, _vector(ctx, t, cols, f32, name))
     g.accumulate = int(bool(accumulate))
-    ctx.check(ctx.lib.harp_norm_backward(ctx.handle, C.byref(n), C.byref(g), *_workspace(workspace), _stream(ctx, stream, tensors)))
+    ctx.check(ctx.lib.harp_norm_backward(ctx.handle, C.byref(n), C.byref(g), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))
