@@ -434,7 +434,7 @@ enum { HARP_STATE_F32 = 32, HARP_STATE_8BIT = 8 };
 
 /* Z = X W^T + bias,  Y = act(Z) + residual.  X [M][K], W [N][K], Y, Z and residual [M][N], bias [N], all
  * of `type`, HARP_BF16 or HARP_F16 (what the matrix instructions multiply at full rate).  Z NULL: not
- * stored.  residual may be Y itself.  M >= 0, N, K >= 1, each below 2^31. */
+ * stored.  residual may be Y itself.  0 <= M < 2^31, 1 <= N, K < 2^22. */
 typedef struct {
     int64_t M, N, K;
     int32_t type, act;

@@ -143,92 +143,105 @@ __global__ __launch_bounds__(256) void pack(const T *from, int64_t ld, int64_t r
 }
 
 // ---------------------------------------------------------------------------------------------- tiles
-// A workgroup makes a tile of BP x BQ of D, 64 of r at a time.  Both operands go from memory straight into LDS, the next
-// 64 of r while the current ones are multiplied (two buffers).
+// A workgroup makes a tile of BP x BQ of D, 32 of r at a time.  Both operands go from memory straight into LDS, three
+// steps before they are multiplied (four buffers).
 //
-// LDS holds pieces of 16 bytes.  Where r is contiguous in memory a row of the tile is 8 pieces of 8 r, piece c of row
-// `row` at place c ^ (row & 7): the 8 rows that a wavefront reads at once then lie in 8 different places.  Where p or q is
-// contiguous a row is one r with B / 8 pieces of 8 p, moved by swap(r); four rows of 16 p are transposed by the read.
-constexpr int kDeep = 64;
+// LDS holds pieces of 16 bytes.  Where r is contiguous in memory a row of the tile is 4 pieces of 8 r, piece c of row
+// `row` at place c ^ (row / 2 & 3): the 8 rows that a wavefront reads at once then lie in 8 different places of 128 bytes.
+// Where p or q is contiguous a row is one r with B / 8 pieces of 8 p, moved by swap(r); four rows of 16 p are transposed
+// by the read.
+constexpr int kDeep = 32;
 
 __device__ __forceinline__ int swap_of(int r) { return (r & 3) << 1 | (r >> 3 & 1) << 3; }
 
-template <typename T> __device__ __forceinline__ void load_to_lds(const T *from, T *to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+// 16 bytes a lane, from base + off to LDS, lane after lane from `to` on (the same for the wavefront).  Written out, because
+// the compiler waits for every such load before any read of LDS that it cannot tell from the load's target; here the waits
+// are the kernel's own (vmcnt counts these loads).  There is no result register, and addresses are taken at issue.
+__device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+}
+template <typename T> __device__ __forceinline__ uint32_t lds_address(const T *p) {
+    return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void *)p));
 }
 
 // One operand of a workgroup of THREADS threads: ACROSS: p is contiguous, else r.
 template <typename T, bool ACROSS, int B, int THREADS> struct Side {
     static constexpr int kLoads = B * kDeep * 2 / 16 / THREADS;      // pieces a thread brings
     static constexpr int kRow = ACROSS ? B / 8 : kDeep / 8;          // pieces in a row of LDS
-    const T *from[kLoads];
+    const char *base;                                                // the tile's r0, the same for all threads
     int64_t step;
+    uint32_t off[kLoads];                                            // bytes; a tile spans less than 2^31 (kMostCols)
 
+    // LDS address of the first of the pieces that this wavefront brings with its load i
+    __device__ __forceinline__ static uint32_t target(const T *lds, int i) {
+        return lds_address(lds) + uint32_t(i * THREADS + __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave) * kWave) * 16;
+    }
     __device__ __forceinline__ static int place(int i) { return i * THREADS + int(threadIdx.x); }
     // r (relative to the tile) of piece i of this thread
     __device__ __forceinline__ static int depth(int i) {
         const int id = place(i);
-        return ACROSS ? id / kRow : ((id % kRow) ^ (id / kRow & 7)) * 8;
+        return ACROSS ? id / kRow : ((id % kRow) ^ (id / kRow / 2 & 3)) * 8;
     }
     __device__ __forceinline__ void begin(const T *a, int64_t ld, int64_t p0, int64_t P, int64_t r0) {
-        step = ACROSS ? kDeep * ld : kDeep;
+        step = (ACROSS ? kDeep * ld : kDeep) * int64_t(sizeof(T));
+        base = reinterpret_cast<const char *>(ACROSS ? a + r0 * ld + p0 : a + p0 * ld + r0);
+        // beyond the edge: anything that is there
+        const int last = int(ACROSS ? (P + 7) / 8 * 8 - 8 - p0 : P - 1 - p0);
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            const int id = place(i);
-            if (ACROSS) {
-                const int64_t p = p0 + ((id % kRow) ^ swap_of(id / kRow)) * 8, last = (P + 7) / 8 * 8 - 8;
-                const int64_t at = p < last ? p : last;              // beyond the edge: anything that is there
-                from[i] = a + (r0 + depth(i)) * ld + at;
-            } else {
-                int64_t p = p0 + id / kRow;
-                p = p < P ? p : P - 1;
-                from[i] = a + p * ld + r0 + depth(i);
-            }
+            const int id = place(i), p = ACROSS ? ((id % kRow) ^ swap_of(id / kRow)) * 8 : id / kRow, at = p < last ? p : last;
+            off[i] = uint32_t(ACROSS ? depth(i) * ld + at : at * ld + depth(i)) * uint32_t(sizeof(T));
         }
     }
     __device__ __forceinline__ void load(T *lds) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-            load_to_lds(from[i], lds + (i * THREADS + int(threadIdx.x) / kWave * kWave) * 8);
-            from[i] += step;
-        }
+        for (int i = 0; i < kLoads; ++i) load_to_lds(base, off[i], target(lds, i));
+        base += step;
     }
-    // the last, partial 64 of r: zeros from `left` on (rows of r end with zeros up to a multiple of 8)
+    // The last, partial step of `left` r: what is beyond is read from the last r there are, and made zeros by clear() when
+    // it has arrived.  Rows of r that are not a multiple of 8 long have zeros up to there.
+    __device__ __forceinline__ int beyond(int i, int left) const { return depth(i) - (ACROSS ? left - 1 : (left + 7) / 8 * 8 - 8); }
     __device__ __forceinline__ void load_partial(T *lds, int left) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
-            u32x4 v = {0, 0, 0, 0};
-            if (depth(i) < (ACROSS ? left : (left + 7) / 8 * 8)) v = *reinterpret_cast<const u32x4 *>(from[i]);
-            *reinterpret_cast<u32x4 *>(lds + place(i) * 8) = v;
+            const int n = beyond(i, left);
+            const uint32_t back = n > 0 ? uint32_t(ACROSS ? n * (step / kDeep) : n * int64_t(sizeof(T))) : 0;
+            load_to_lds(base, off[i] - back, target(lds, i));
         }
+    }
+    __device__ __forceinline__ void clear(T *lds, int left) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+            if (beyond(i, left) > 0) *reinterpret_cast<u32x4 *>(lds + place(i) * 8) = u32x4{0, 0, 0, 0};
     }
 };
 
 // Fragments of 16 p by 32 r of a tile in LDS: lane l has p = l % 16 and r = 8 (l / 16) .. + 7 of the 32.
 template <typename T, bool ACROSS, int B, int COUNT> struct Fragments {
     typedef typename Mfma<T>::Frag Frag;
-    int at[ACROSS ? COUNT : 2];
+    int at[ACROSS ? COUNT : 1];
     __device__ __forceinline__ void begin(int p0) {
         const int lane = threadIdx.x % kWave, i = lane % 16, g = lane / 16;
         if constexpr (ACROSS) {
             const int r = 8 * g + i / 4;
+#pragma unroll
             for (int j = 0; j < COUNT; ++j) at[j] = r * B + (((p0 / 8 + 2 * j) ^ swap_of(r)) | (i % 4 / 2)) * 8 + i % 2 * 4;
         } else {
-            for (int k = 0; k < 2; ++k) at[k] = (p0 + i) * kDeep + ((4 * k + g) ^ (i & 7)) * 8;
+            at[0] = (p0 + i) * kDeep + (g ^ (i / 2 & 3)) * 8;
         }
     }
-    __device__ __forceinline__ Frag read(const T *lds, int j, int k) const {
+    __device__ __forceinline__ Frag read(const T *lds, int j) const {
         if constexpr (ACROSS) {
             typedef short s16x4 __attribute__((ext_vector_type(4)));
             typedef short s16x8 __attribute__((ext_vector_type(8)));
             typedef __attribute__((address_space(3))) s16x4 *Lds;
-            const T *a = lds + at[j] + 32 * k * B;
+            const T *a = lds + at[j];
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)a);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(a + 4 * B));
             const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             return __builtin_bit_cast(Frag, v);
         } else {
-            return *reinterpret_cast<const Frag *>(lds + at[k] + 16 * j * kDeep);
+            return *reinterpret_cast<const Frag *>(lds + at[0] + 16 * j * kDeep);
         }
     }
 };
@@ -247,12 +260,12 @@ __device__ __forceinline__ void tile_of(int id, int tiles_p, int tiles_q, int &t
 
 // WP x WQ wavefronts, each a part of BP / WP x BQ / WQ of the tile.  With `partial` the sums of blockIdx.y's share of r go
 // there, [share][P][Q], instead of through the epilogue.
-template <typename T, bool A_ACROSS, bool B_ACROSS, int BP, int BQ, int WP, int WQ>
+template <typename T, bool A_ACROSS, bool B_ACROSS, int BP, int BQ, int WP, int WQ, int kBuffers>
 __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t lda, const T *b, int64_t ldb, int64_t P, int64_t Q, int64_t R,
                                                            int tiles_p, int tiles_q, int64_t share, float *partial, Epilogue e) {
     constexpr int kThreads = WP * WQ * kWave, kP = BP / WP / 16, kQ = BQ / WQ / 16;
-    __shared__ __align__(16) T la[2][BP * kDeep];
-    __shared__ __align__(16) T lb[2][BQ * kDeep];
+    __shared__ __align__(16) T la[kBuffers][BP * kDeep];
+    __shared__ __align__(16) T lb[kBuffers][BQ * kDeep];
     int tp, tq;
     tile_of(blockIdx.x, tiles_p, tiles_q, tp, tq);
     const int64_t p0 = int64_t(tp) * BP, q0 = int64_t(tq) * BQ;
@@ -268,49 +281,108 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
     fa.begin(wp);
     fb.begin(wq);
     f32x4 acc[kP][kQ] = {};
-    auto bring = [&](int buffer, int64_t left) {
-        if (left >= kDeep) {
-            sa.load(la[buffer]);
-            sb.load(lb[buffer]);
+    typedef typename Mfma<T>::Frag Frag;
+    const int steps = int((r1 - r0 + kDeep - 1) / kDeep), odd = int((r1 - r0) % kDeep);     // odd: r of a partial last step
+    auto bring = [&](int i) {
+        if (i + 1 < steps || odd == 0) {
+            sa.load(la[i % kBuffers]);
+            sb.load(lb[i % kBuffers]);
         } else {
-            sa.load_partial(la[buffer], int(left));
-            sb.load_partial(lb[buffer], int(left));
+            sa.load_partial(la[i % kBuffers], odd);
+            sb.load_partial(lb[i % kBuffers], odd);
         }
     };
-    auto multiply = [&](int buffer) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            typename Mfma<T>::Frag x[kP], y[kQ];
-#pragma unroll
-            for (int i = 0; i < kP; ++i) x[i] = fa.read(la[buffer], i, k);
-#pragma unroll
-            for (int j = 0; j < kQ; ++j) y[j] = fb.read(lb[buffer], j, k);
-            // the q operand first: a lane then holds four neighbouring q of one p
-#pragma unroll
-            for (int i = 0; i < kP; ++i)
-#pragma unroll
-                for (int j = 0; j < kQ; ++j) acc[i][j] = Mfma<T>::run(y[j], x[i], acc[i][j]);
-        }
+    auto barrier = [] {
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
     };
-    // what was brought is in LDS for everybody: loads into LDS are counted by vmcnt, which a barrier does not wait for
-    auto arrived = [] {
+    // Step i is in LDS for everybody, and nobody reads the buffer of step i - 1 any more.  Loads into LDS are counted by
+    // vmcnt, which a barrier alone does not wait for; they arrive in order, so those of later steps may be out still.
+    constexpr int kLoads = decltype(sa)::kLoads + decltype(sb)::kLoads;
+    auto arrived = [&](int i) {
+        if (i + kBuffers - 2 < steps) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kBuffers - 2) * kLoads) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            if (i + 1 == steps && odd) {
+                sa.clear(la[i % kBuffers], odd);
+                sb.clear(lb[i % kBuffers], odd);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+        barrier();
+    };
+    auto read = [&](int buffer, Frag (&x)[kP], Frag (&y)[kQ]) {
+#pragma unroll
+        for (int j = 0; j < kQ; ++j) y[j] = fb.read(lb[buffer], j);
+#pragma unroll
+        for (int i = 0; i < kP; ++i) x[i] = fa.read(la[buffer], i);
+    };
+    // A step's products from registers.  The q operand first: a lane then holds four neighbouring q of one p.
+    auto multiply = [&](const Frag (&x)[kP], const Frag (&y)[kQ]) {
+#pragma unroll
+        for (int i = 0; i < kP; ++i)
+#pragma unroll
+            for (int j = 0; j < kQ; ++j) acc[i][j] = Mfma<T>::run(y[j], x[i], acc[i][j]);
+    };
+    // ... while the reads of the next step's operands go on among the instructions.
+    auto interleave = [] {
+        constexpr int kReads = kP * (A_ACROSS ? 2 : 1) + kQ * (B_ACROSS ? 2 : 1), kEach = kP * kQ / kReads;
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);       // matrix instructions
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);           // LDS read
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kP * kQ - kReads * kEach, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    Frag x[2][kP], y[2][kQ];
+    if (steps > 0) {
+        for (int i = 0; i < kBuffers && i < steps; ++i) bring(i);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-    if (r0 < r1) bring(0, r1 - r0);
-    arrived();
-    int buffer = 0;
-    for (int64_t r = r0; r < r1; r += kDeep) {
-        if (r + kDeep < r1) bring(buffer ^ 1, r1 - r - kDeep);
-        multiply(buffer);
-        arrived();
-        buffer ^= 1;
+        if (steps <= kBuffers && odd) {
+            sa.clear(la[steps - 1], odd);
+            sb.clear(lb[steps - 1], odd);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        barrier();
+        read(0, x[0], y[0]);
+        // Step i has its operands in registers.  Behind its barrier step i + 1 has arrived, and the buffer of step i is free
+        // for step i + kBuffers.  Several steps at a time while all that they bring is whole: buffers are known then.
+        int i = 0;
+        constexpr int kRound = kBuffers % 2 ? 2 * kBuffers : kBuffers;
+        for (; i + kRound + kBuffers < steps; i += kRound) {
+#pragma unroll
+            for (int k = 0; k < kRound; ++k) {
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kBuffers - 2) * kLoads) : "memory");
+                barrier();
+                sa.load(la[k % kBuffers]);
+                sb.load(lb[k % kBuffers]);
+                __builtin_amdgcn_sched_barrier(0);
+                read((k + 1) % kBuffers, x[(k + 1) % 2], y[(k + 1) % 2]);
+                multiply(x[k % 2], y[k % 2]);
+                interleave();
+            }
+        }
+        for (; i + 1 < steps; ++i) {
+            arrived(i + 1);
+            if (i + kBuffers < steps) bring(i + kBuffers);
+            read((i + 1) % kBuffers, x[1], y[1]);
+            multiply(x[0], y[0]);
+#pragma unroll
+            for (int k = 0; k < kP; ++k) x[0][k] = x[1][k];
+#pragma unroll
+            for (int k = 0; k < kQ; ++k) y[0][k] = y[1][k];
+        }
+        multiply(x[0], y[0]);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        barrier();                                       // all have read all: LDS is free
     }
     // 16 p at a time through LDS (the tiles are done with): a lane then holds four q of a row whose other q its neighbours
     // hold, and rows are stored in whole lines.
     if (partial) e = Epilogue{kWeight, HARP_ACT_NONE, 0, 1, Q % 4 == 0, partial + int64_t(blockIdx.y) * P * Q, nullptr, nullptr, nullptr, nullptr, Q, 0, 0};
     constexpr int kCols = BQ / WQ, kPitch = kCols + 4, kAtOnce = kWave / (kCols / 4);
-    static_assert(WP * WQ * 16 * kPitch * 4 <= 2 * BP * kDeep * 2, "the wavefronts' rows have to fit into the first operand's LDS");
+    static_assert(WP * WQ * 16 * kPitch * 4 <= kBuffers * BP * kDeep * 2, "the wavefronts' rows have to fit into the first operand's LDS");
     float *rows = reinterpret_cast<float *>(&la[0][0]) + wave * 16 * kPitch;
     const int64_t q = q0 + wq + lane % (kCols / 4) * 4;
 #pragma unroll
@@ -404,27 +476,28 @@ __global__ __launch_bounds__(256) void act_grad(int64_t M, int64_t N, int act, c
 
 int64_t slabs_of(int64_t M) { return (M + kSumRows - 1) / kSumRows; }
 
+// Columns at most (a tile of 256 rows then spans less than 2^31 bytes); rows further apart than that are packed.
+constexpr int64_t kMostCols = int64_t(1) << 22;
 bool sizes_fit(int64_t M, int64_t N, int64_t K) {
-    const int64_t most = int64_t(1) << 31;
-    return M >= 0 && N >= 1 && K >= 1 && M < most && N < most && K < most;
+    return M >= 0 && M < int64_t(1) << 31 && N >= 1 && K >= 1 && N < kMostCols && K < kMostCols;
 }
 
 // How a product is launched.
 struct Plan {
     bool few, big;               // few tokens; tiles of 256 x 256, else of 128 x 128
     int shares;                  // of r, joined by a second launch
-    int64_t share;               // r of one, a multiple of kDeep
+    int64_t share;               // r of one, a multiple of kPiece
 };
-constexpr int kFewTokens = 64;
+constexpr int kFewTokens = 64, kPiece = 64;
 
 int64_t tiles(int64_t P, int64_t Q, int side) { return (P + side - 1) / side * ((Q + side - 1) / side); }
 
 Plan split(Plan p, int64_t R, int64_t shares) {
-    const int64_t steps = (R + kDeep - 1) / kDeep;
+    const int64_t steps = (R + kPiece - 1) / kPiece;
     shares = shares < steps ? shares : steps;
     shares = shares < 1 ? 1 : shares;
     const int64_t each = (steps + shares - 1) / shares;
-    p.share = (each < 1 ? 1 : each) * kDeep;
+    p.share = (each < 1 ? 1 : each) * kPiece;
     p.shares = int(steps ? (steps + each - 1) / each : 1);
     return p;
 }
@@ -437,7 +510,7 @@ Plan plan_for(const harp_ctx *ctx, int kind, int64_t P, int64_t Q, int64_t R) {
         const int64_t groups = (Q + 15) / 16;
         // 8 workgroups a compute unit, of at least four pieces a wavefront
         int64_t shares = 8 * cu / (groups > 0 ? groups : 1);
-        const int64_t most = R / (16 * kDeep);
+        const int64_t most = R / (16 * kPiece);
         shares = shares < most ? shares : most;
         return split(p, R, shares < 16 ? shares : 16);
     }
@@ -466,7 +539,7 @@ struct Matrix { const char *name; const void *p; int64_t ld, cols; size_t elemen
 
 int check(harp_ctx *ctx, int64_t M, int64_t N, int64_t K, int type, int act, const Matrix *m, int count, const void *workspace,
           size_t workspace_bytes) {
-    if (!sizes_fit(M, N, K)) return fail(ctx, HARP_ERR_SHAPE, "M >= 0 and N, K >= 1 are wanted, each below 2^31");
+    if (!sizes_fit(M, N, K)) return fail(ctx, HARP_ERR_SHAPE, "0 <= M < 2^31 and 1 <= N, K < 2^22 are wanted");
     if (type != HARP_BF16 && type != HARP_F16) return fail(ctx, HARP_ERR_INVALID_ARG, "type must be HARP_BF16 or HARP_F16");
     if (act < HARP_ACT_NONE || act > HARP_ACT_SILU) return fail(ctx, HARP_ERR_INVALID_ARG, "unknown activation");
     for (int i = 0; i < count; ++i) {
@@ -486,7 +559,7 @@ int check(harp_ctx *ctx, int64_t M, int64_t N, int64_t K, int type, int act, con
 // One operand as it is called with: A(p, r), rows of `cols` elements ld apart.
 struct Given { const void *a; int64_t ld, rows, cols; };
 
-bool wide_rows(const Given &g) { return g.cols % 8 == 0 && g.ld % 8 == 0 && aligned(g.a, 16); }
+bool wide_rows(const Given &g) { return g.cols % 8 == 0 && g.ld % 8 == 0 && g.ld < kMostCols && aligned(g.a, 16); }
 
 uint32_t blocks_for(int64_t threads) {
     const int64_t n = (threads + 255) / 256;
@@ -509,8 +582,8 @@ void launch_tiles(const Plan &plan, const Given &a, const Given &b, int64_t P, i
     const int tp = int((P + side - 1) / side), tq = int((Q + side - 1) / side);
     const dim3 grid(uint32_t(tp) * uint32_t(tq), uint32_t(plan.shares));
     const T *pa = static_cast<const T *>(a.a), *pb = static_cast<const T *>(b.a);
-    if (plan.big) product<T, A_ACROSS, B_ACROSS, 256, 256, 2, 4><<<grid, dim3(512), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
-    else product<T, A_ACROSS, B_ACROSS, 128, 128, 2, 2><<<grid, dim3(256), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
+    if (plan.big) product<T, A_ACROSS, B_ACROSS, 256, 256, 2, 4, 4><<<grid, dim3(512), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
+    else product<T, A_ACROSS, B_ACROSS, 128, 128, 2, 2, 4><<<grid, dim3(256), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
 }
 
 template <typename T, bool WIDE>
