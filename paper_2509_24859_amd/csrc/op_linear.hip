@@ -446,22 +446,56 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_tokens(const T *x, int6
     }
 }
 
-// Column sums of dY: partial sums of slabs of rows, then the slabs in order.
-constexpr int kSumRows = 256;
+// Column sums of dY.  A workgroup takes 256 columns, 8 to a thread, and kSumRows rows, every eighth to a thread: pieces of 16
+// bytes wherever they lie, several rows asked for at a time; bound by reading dY.  The second launch adds the slabs up.
+// 4,096 x 4,096 in 61 us with a column and 256 rows to a thread.
+constexpr int kSumRows = 64, kSumCols = 256;
 template <typename T>
 __global__ __launch_bounds__(256) void column_sums(const T *dy, int64_t ld, int64_t M, int64_t N, float *partial) {
-    const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (n >= N) return;
-    const int64_t begin = int64_t(blockIdx.y) * kSumRows, end = begin + kSumRows < M ? begin + kSumRows : M;
-    float s = 0;
-    for (int64_t m = begin; m < end; ++m) s += to_f32(dy[m * ld + n]);
-    partial[int64_t(blockIdx.y) * N + n] = s;
+    typedef typename Mfma<T>::Frag Piece;
+    typedef Piece Loose __attribute__((aligned(sizeof(T))));
+    __shared__ float runs[8][kSumCols + 1];
+    const int part = threadIdx.x % 32, run = threadIdx.x / 32;
+    const int64_t n = int64_t(blockIdx.x) * kSumCols + part * 8, m0 = int64_t(blockIdx.y) * kSumRows;
+    float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (n + 8 <= N) {
+        Piece v[kSumRows / 8] = {};
+#pragma unroll
+        for (int i = 0; i < kSumRows / 8; ++i)
+            if (m0 + run + 8 * i < M) v[i] = *reinterpret_cast<const Loose *>(dy + (m0 + run + 8 * i) * ld + n);
+#pragma unroll
+        for (int i = 0; i < kSumRows / 8; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s[k] += to_f32(T(v[i][k]));
+    } else {
+        for (int64_t m = m0 + run; m < m0 + kSumRows && m < M; m += 8)
+            for (int k = 0; k < 8; ++k)
+                if (n + k < N) s[k] += to_f32(dy[m * ld + n + k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) runs[run][part * 8 + k] = s[k];
+    __syncthreads();
+    const int64_t at = int64_t(blockIdx.x) * kSumCols + threadIdx.x;
+    float d = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d += runs[i][threadIdx.x];
+    if (at < N) partial[int64_t(blockIdx.y) * N + at] = d;
 }
+// 16 columns a workgroup, 16 threads to a column, each a run of slabs in order, then the runs in order.
 __global__ __launch_bounds__(256) void column_join(const float *partial, int64_t count, int64_t N, float *out, int accumulate) {
-    const int64_t n = int64_t(blockIdx.x) * 256 + threadIdx.x;
-    if (n >= N) return;
+    __shared__ float runs[16][17];
+    const int c = threadIdx.x % 16, run = threadIdx.x / 16;
+    const int64_t n = int64_t(blockIdx.x) * 16 + c, each = (count + 15) / 16;
+    const int64_t last = (run + 1) * each < count ? (run + 1) * each : count;
     float s = 0;
-    for (int64_t i = 0; i < count; ++i) s += partial[i * N + n];
+    if (n < N)
+#pragma unroll 4
+        for (int64_t i = run * each; i < last; ++i) s += partial[i * N + n];
+    runs[run][c] = s;
+    __syncthreads();
+    if (run != 0 || n >= N) return;
+    s = 0;
+    for (int i = 0; i < 16; ++i) s += runs[i][c];
     out[n] = accumulate ? out[n] + s : s;
 }
 
@@ -621,6 +655,14 @@ void launch_product(const harp_ctx *ctx, Given a, Given b, int64_t P, int64_t Q,
     if (partial) join<T><<<dim3(blocks_for(P * ((Q + 3) / 4))), dim3(256), 0, st>>>(partial, plan.shares, P, Q, e);
 }
 
+template <typename T> void launch_sums(const harp_linear_weight *g, uint32_t across, int64_t slabs, float *partial, hipStream_t st) {
+    for (int64_t first = 0; first < slabs; first += 65535) {      // a launch has 65,535 rows of workgroups at most
+        const int64_t row = first * kSumRows;
+        column_sums<T><<<dim3(across, uint32_t(slabs - first < 65535 ? slabs - first : 65535)), dim3(256), 0, st>>>(
+            static_cast<const T *>(g->dY) + row * g->lddy, g->lddy, g->M - row, g->N, partial + first * g->N);
+    }
+}
+
 int launched(harp_ctx *ctx) {
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? HARP_OK : hip_fail(ctx, e, "launching the product's kernels");
@@ -681,13 +723,11 @@ int harp_linear_grad_weight(harp_ctx *ctx, const harp_linear_weight *g, void *wo
     else launch_product<_Float16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->X, g->ldx, g->M, g->K}, g->N, g->K, g->M, e, workspace, st);
     if (g->dbias) {
         float *partial = static_cast<float *>(workspace);
-        const uint32_t across = uint32_t((g->N + 255) / 256);
         const int64_t slabs = slabs_of(g->M);
-        if (some) {
-            if (g->type == HARP_BF16) column_sums<__bf16><<<dim3(across, uint32_t(slabs)), dim3(256), 0, st>>>(static_cast<const __bf16 *>(g->dY), g->lddy, g->M, g->N, partial);
-            else column_sums<_Float16><<<dim3(across, uint32_t(slabs)), dim3(256), 0, st>>>(static_cast<const _Float16 *>(g->dY), g->lddy, g->M, g->N, partial);
-        }
-        column_join<<<dim3(across), dim3(256), 0, st>>>(partial, slabs, g->N, g->dbias, g->accumulate);
+        const uint32_t across = uint32_t((g->N + kSumCols - 1) / kSumCols);
+        if (some && g->type == HARP_BF16) launch_sums<__bf16>(g, across, slabs, partial, st);
+        else if (some) launch_sums<_Float16>(g, across, slabs, partial, st);
+        column_join<<<dim3(uint32_t((g->N + 15) / 16)), dim3(256), 0, st>>>(partial, slabs, g->N, g->dbias, g->accumulate);
     }
     return launched(ctx);
 }
