@@ -424,16 +424,33 @@ __global__ __launch_bounds__(kFewWaves * kWave) void few_tokens(const T *x, int6
     const int64_t r0 = int64_t(blockIdx.y) * share, r1 = r0 + share < R ? r0 + share : R;
     const T *wr = w + (n0 + i < N ? n0 + i : N - 1) * ldw;
     const T *xr[TILES];
+#pragma unroll
     for (int t = 0; t < TILES; ++t) xr[t] = x + (16 * t + i < M ? 16 * t + i : M - 1) * ldx;
     f32x4 acc[TILES] = {};
-    for (int64_t r = r0 + wave * 64 + 16 * g; r - 16 * g < r1; r += kFewWaves * 64) {
-        const typename Mfma<T>::Frag a = eight<T, WIDE>(wr, r, r1), b = eight<T, WIDE>(wr, r + 8, r1);
-        for (int t = 0; t < TILES; ++t) {
-            acc[t] = Mfma<T>::run(a, eight<T, WIDE>(xr[t], r, r1), acc[t]);
-            acc[t] = Mfma<T>::run(b, eight<T, WIDE>(xr[t], r + 8, r1), acc[t]);
-        }
+    // several pieces are asked for before the first is used: a compute unit then has 128 KB of weights on their way
+    constexpr int kAhead = TILES == 1 ? 4 : 2;
+    for (int64_t r = r0 + wave * 64 + 16 * g; r - 16 * g < r1; r += kAhead * kFewWaves * 64) {
+        typename Mfma<T>::Frag a[kAhead][2], b[TILES][kAhead][2];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) a[k][h] = eight<T, WIDE>(wr, r + k * kFewWaves * 64 + 8 * h, r1);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) b[t][k][h] = eight<T, WIDE>(xr[t], r + k * kFewWaves * 64 + 8 * h, r1);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) acc[t] = Mfma<T>::run(a[k][h], b[t][k][h], acc[t]);
     }
+#pragma unroll
     for (int t = 0; t < TILES; ++t)
+#pragma unroll
         for (int k = 0; k < 4; ++k) sums[wave][16 * t + i][4 * g + k] = acc[t][k];
     __syncthreads();
     for (int at = threadIdx.x; at < TILES * 256; at += kFewWaves * kWave) {
@@ -542,8 +559,8 @@ Plan plan_for(const harp_ctx *ctx, int kind, int64_t P, int64_t Q, int64_t R) {
     if (kind == kForward && P <= kFewTokens) {
         p.few = true;
         const int64_t groups = (Q + 15) / 16;
-        // 8 workgroups a compute unit, of at least four pieces a wavefront
-        int64_t shares = 8 * cu / (groups > 0 ? groups : 1);
+        // 4 workgroups a compute unit, of at least four pieces a wavefront (8 of them: a second launch that costs 4 us)
+        int64_t shares = 4 * cu / (groups > 0 ? groups : 1);
         const int64_t most = R / (16 * kPiece);
         shares = shares < most ? shares : most;
         return split(p, R, shares < 16 ? shares : 16);
