@@ -18,6 +18,7 @@ namespace {
 constexpr int kBlock = 256;               // elements that share an exponent: one wavefront, four elements a lane
 constexpr int kThreads = 256;
 constexpr int kChunk = 4096;              // elements a workgroup works on
+constexpr int kAhead = 2;
 constexpr int kTopM = 15, kTopV = 31;     // largest exponent fields of the two codes
 
 struct Tensor {                           // a tensor as the kernels see it
@@ -30,7 +31,7 @@ struct Tensor {                           // a tensor as the kernels see it
     double weight_decay;
     uint64_t first_block;                 // place of its first block of 256 among all tensors' (for the rounding's hash)
     int32_t state, grad_type, copy_type;
-    int32_t wide;                         // pointers allow loads of four elements
+    int32_t wide;                         // four elements can be read and written at once
 };
 struct Chunk { uint32_t tensor, index; };  // workgroup -> elements index * kChunk .. of the tensor
 
@@ -42,14 +43,48 @@ struct Step {
     const int32_t *skip;
 };
 
-__device__ __forceinline__ float element(const void *p, int type, int64_t i) {
-    return type == HARP_F32 ? static_cast<const float *>(p)[i]
-           : type == HARP_BF16 ? to_f32(static_cast<const __bf16 *>(p)[i])
-                               : to_f32(static_cast<const _Float16 *>(p)[i]);
+// Elements i .. i + 3 of a tensor of n; `wide`: all are there and aligned.  What is not there is 0.
+template <typename T> __device__ __forceinline__ f32x4 four_of(const void *p, int64_t i, int64_t n, bool wide) {
+    const T *a = static_cast<const T *>(p) + i;
+    if (wide) return load4(a);
+    f32x4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = i + j < n ? to_f32(a[j]) : 0.0f;
+    return v;
 }
-__device__ __forceinline__ void put_copy(void *p, int type, int64_t i, float v) {
-    if (type == HARP_BF16) static_cast<__bf16 *>(p)[i] = __bf16(v);
-    else static_cast<_Float16 *>(p)[i] = _Float16(v);
+__device__ __forceinline__ f32x4 gradient(const void *p, int type, int64_t i, int64_t n, bool wide) {
+    return type == HARP_F32 ? four_of<float>(p, i, n, wide) : type == HARP_BF16 ? four_of<__bf16>(p, i, n, wide) : four_of<_Float16>(p, i, n, wide);
+}
+template <typename T> __device__ __forceinline__ void put_four(void *p, int64_t i, int64_t n, bool wide, f32x4 v) {
+    T *a = static_cast<T *>(p) + i;
+    if (wide) {
+        store4(a, v);
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i + j < n) a[j] = T(v[j]);
+}
+__device__ __forceinline__ void put_copy(void *p, int type, int64_t i, int64_t n, bool wide, f32x4 v) {
+    if (type == HARP_BF16) put_four<__bf16>(p, i, n, wide, v);
+    else put_four<_Float16>(p, i, n, wide, v);
+}
+// Four codes, the first in the lowest byte.
+__device__ __forceinline__ uint32_t codes_of(const uint8_t *a, int64_t i, int64_t n, bool wide) {
+    if (wide) return *reinterpret_cast<const uint32_t *>(a + i);
+    uint32_t c = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c |= i + j < n ? uint32_t(a[i + j]) << (8 * j) : 0;
+    return c;
+}
+__device__ __forceinline__ void put_codes(uint8_t *a, int64_t i, int64_t n, bool wide, uint32_t c) {
+    if (wide) {
+        *reinterpret_cast<uint32_t *>(a + i) = c;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i + j < n) a[i + j] = uint8_t(c >> (8 * j));
 }
 
 // The new moments and the new weight.  Every product and sum is rounded by itself (no fused multiply-add): the
@@ -101,89 +136,152 @@ __device__ __forceinline__ uint32_t encode(uint32_t bits, uint32_t exponent, int
     return exponent == 255 ? 0 : code < most ? code : most;
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-    for (int d = 32; d; d >>= 1) {
-        const uint32_t y = __shfl_xor(x, d);
-        x = x > y ? x : y;
-    }
-    return x;
-}
-
 __global__ __launch_bounds__(kThreads) void adamw_step(const Tensor *tensors, const Chunk *chunks, Step s) {
     if (s.skip && *s.skip) return;
     const Chunk c = chunks[blockIdx.x];
     const Tensor &t = tensors[c.tensor];
     const float scale = s.grad_scale ? *s.grad_scale : 1.0f;
     const float decay = float(s.lr * t.weight_decay);
-    const int64_t begin = int64_t(c.index) * kChunk;
-    const int64_t end = begin + kChunk < t.n ? begin + kChunk : t.n;
+    const int64_t begin = int64_t(c.index) * kChunk, n = t.n;
+    const int64_t end = begin + kChunk < n ? begin + kChunk : n;
     if (t.state == HARP_STATE_F32) {
-        float *m = static_cast<float *>(t.m), *v = static_cast<float *>(t.v);
-        for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
-            float p = t.p[i], mi = m[i], vi = v[i];
-            update(s, element(t.grad, t.grad_type, i) * scale, decay, p, mi, vi);
-            t.p[i] = p;
-            m[i] = mi;
-            v[i] = vi;
-            if (t.copy) put_copy(t.copy, t.copy_type, i, p);
-        }
+        // kAhead pieces of four are read before the first is worked on
+        auto piece = [&](int64_t at, bool wide) {
+            f32x4 g[kAhead], p[kAhead], m[kAhead], v[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int64_t i = at + k * 4 * kThreads;
+                g[k] = gradient(t.grad, t.grad_type, i, n, wide);
+                p[k] = four_of<float>(t.p, i, n, wide);
+                m[k] = four_of<float>(t.m, i, n, wide);
+                v[k] = four_of<float>(t.v, i, n, wide);
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const int64_t i = at + k * 4 * kThreads;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float pj = p[k][j], mj = m[k][j], vj = v[k][j];
+                    update(s, g[k][j] * scale, decay, pj, mj, vj);
+                    p[k][j] = pj;
+                    m[k][j] = mj;
+                    v[k][j] = vj;
+                }
+                put_four<float>(t.p, i, n, wide, p[k]);
+                put_four<float>(t.m, i, n, wide, m[k]);
+                put_four<float>(t.v, i, n, wide, v[k]);
+                if (t.copy) put_copy(t.copy, t.copy_type, i, n, wide, p[k]);
+            }
+        };
+        if (t.wide && begin + kChunk <= n)
+            for (int64_t i = begin + 4 * threadIdx.x; i < end; i += kAhead * 4 * kThreads) piece(i, true);
+        else
+            for (int64_t i = begin + 4 * threadIdx.x; i < end; i += kAhead * 4 * kThreads) piece(i, false);
         return;
     }
-    uint8_t *m = static_cast<uint8_t *>(t.m), *v = static_cast<uint8_t *>(t.v);
+    uint8_t *tm = static_cast<uint8_t *>(t.m), *tv = static_cast<uint8_t *>(t.v);
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    for (int64_t at = begin + wave * kBlock; at < end; at += kThreads / kWave * kBlock) {
-        const int64_t b = at / kBlock;
-        const uint32_t em = t.m_exp[b], ev = t.v_exp[b];
-        const float um = block_unit(em, kTopM), uv = block_unit(ev, kTopV);
-        float mi[4] = {0, 0, 0, 0}, vi[4] = {0, 0, 0, 0};
-        uint32_t most_m = 0, most_v = 0;
-        for (int j = 0; j < 4; ++j) {
-            const int64_t i = at + 4 * lane + j;
-            if (i >= t.n) continue;
-            const uint32_t cm = m[i], cv = v[i];
-            mi[j] = decode(cm & 127, um);
-            if (cm & 128) mi[j] = -mi[j];
-            vi[j] = decode(cv, uv);
-            float p = t.p[i];
-            update(s, element(t.grad, t.grad_type, i) * scale, decay, p, mi[j], vi[j]);
-            t.p[i] = p;
-            if (t.copy) put_copy(t.copy, t.copy_type, i, p);
-            const uint32_t am = __float_as_uint(mi[j]) & 0x7FFFFFFFu, av = __float_as_uint(vi[j]) & 0x7FFFFFFFu;
-            most_m = most_m > am ? most_m : am;
-            most_v = most_v > av ? most_v : av;
+    constexpr int kStep = kThreads / kWave * kBlock;       // to a wavefront's next block
+    auto blocks = [&](int64_t first, bool wide) {
+        uint32_t cm[kAhead], cv[kAhead], em[kAhead], ev[kAhead];
+        f32x4 g[kAhead], p[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t at = first + k * kStep, i = at + 4 * lane, b = (at < end ? at : first) / kBlock;
+            cm[k] = codes_of(tm, i, n, wide);
+            cv[k] = codes_of(tv, i, n, wide);
+            g[k] = gradient(t.grad, t.grad_type, i, n, wide);
+            p[k] = four_of<float>(t.p, i, n, wide);
+            em[k] = t.m_exp[b];
+            ev[k] = t.v_exp[b];
         }
-        const uint32_t nm = block_exponent(wave_max(most_m)), nv = block_exponent(wave_max(most_v));
-        const uint64_t pair = ((t.first_block + b) * kBlock + 4 * lane) / 2;
-        const uint64_t h[2] = {hash_pair(s.seed, pair), hash_pair(s.seed, pair + 1)};
-        for (int j = 0; j < 4; ++j) {
-            const int64_t i = at + 4 * lane + j;
-            if (i >= t.n) continue;
-            const uint32_t r = uint32_t(h[j >> 1] >> (32 * (j & 1)));
-            const uint32_t bm = __float_as_uint(mi[j]);
-            m[i] = uint8_t(encode(bm, nm, kTopM, r & 0xFFFF) | (bm >> 24 & 128));
-            v[i] = uint8_t(encode(__float_as_uint(vi[j]), nv, kTopV, r >> 16));
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t at = first + k * kStep, i = at + 4 * lane, b = at / kBlock;
+            if (at >= end) break;
+            const float um = block_unit(em[k], kTopM), uv = block_unit(ev[k], kTopV);
+            float m[4], v[4];
+            uint32_t most_m = 0, most_v = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a = cm[k] >> (8 * j) & 255;
+                m[j] = decode(a & 127, um);
+                m[j] = a & 128 ? -m[j] : m[j];
+                v[j] = decode(cv[k] >> (8 * j) & 255, uv);
+                float pj = p[k][j];
+                update(s, g[k][j] * scale, decay, pj, m[j], v[j]);
+                p[k][j] = pj;
+                if (wide || i + j < n) {                   // what is not there has no say in the block's exponent
+                    most_m = larger(most_m, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+                    most_v = larger(most_v, __float_as_uint(v[j]) & 0x7FFFFFFFu);
+                }
+            }
+            const uint32_t nm = block_exponent(wave_max(most_m)), nv = block_exponent(wave_max(most_v));
+            const uint64_t pair = ((t.first_block + b) * kBlock + 4 * lane) / 2;
+            uint32_t out_m = 0, out_v = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint64_t bits = hash_pair(s.seed, pair + h);
+#pragma unroll
+                for (int j = 2 * h; j < 2 * h + 2; ++j) {
+                    const uint32_t r = uint32_t(bits >> (32 * (j & 1))), bm = __float_as_uint(m[j]);
+                    out_m |= (encode(bm, nm, kTopM, r & 0xFFFF) | (bm >> 24 & 128)) << (8 * j);
+                    out_v |= encode(__float_as_uint(v[j]), nv, kTopV, r >> 16) << (8 * j);
+                }
+            }
+            put_four<float>(t.p, i, n, wide, p[k]);
+            if (t.copy) put_copy(t.copy, t.copy_type, i, n, wide, p[k]);
+            put_codes(tm, i, n, wide, out_m);
+            put_codes(tv, i, n, wide, out_v);
+            if (lane == 0) {
+                t.m_exp[b] = uint8_t(nm);
+                t.v_exp[b] = uint8_t(nv);
+            }
         }
-        if (lane == 0) {
-            t.m_exp[b] = uint8_t(nm);
-            t.v_exp[b] = uint8_t(nv);
-        }
-    }
+    };
+    if (t.wide && begin + kChunk <= n)
+        for (int64_t at = begin + wave * kBlock; at < end; at += kAhead * kStep) blocks(at, true);
+    else
+        for (int64_t at = begin + wave * kBlock; at < end; at += kAhead * kStep) blocks(at, false);
 }
 
 __global__ __launch_bounds__(kThreads) void adamw_read(const Tensor *tensors, const Chunk *chunks) {
     const Chunk c = chunks[blockIdx.x];
     const Tensor &t = tensors[c.tensor];
     if (t.state != HARP_STATE_8BIT) return;
-    const int64_t begin = int64_t(c.index) * kChunk;
-    const int64_t end = begin + kChunk < t.n ? begin + kChunk : t.n;
-    const uint8_t *m = static_cast<const uint8_t *>(t.m), *v = static_cast<const uint8_t *>(t.v);
-    for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
-        if (t.m_seen) {
-            const float x = decode(m[i] & 127, block_unit(t.m_exp[i / kBlock], kTopM));
-            t.m_seen[i] = __bf16(m[i] & 128 ? -x : x);
+    const int64_t begin = int64_t(c.index) * kChunk, n = t.n;
+    const int64_t end = begin + kChunk < n ? begin + kChunk : n;
+    const uint8_t *tm = static_cast<const uint8_t *>(t.m), *tv = static_cast<const uint8_t *>(t.v);
+    auto pieces = [&](int64_t first, bool wide) {
+        uint32_t cm[2 * kAhead], cv[2 * kAhead], em[2 * kAhead], ev[2 * kAhead];
+#pragma unroll
+        for (int k = 0; k < 2 * kAhead; ++k) {
+            const int64_t i = first + k * 4 * kThreads, b = (i < end ? i : first) / kBlock;
+            cm[k] = codes_of(tm, i, n, wide);
+            cv[k] = codes_of(tv, i, n, wide);
+            em[k] = t.m_exp[b];
+            ev[k] = t.v_exp[b];
         }
-        if (t.v_seen) t.v_seen[i] = __bf16(decode(v[i], block_unit(t.v_exp[i / kBlock], kTopV)));
-    }
+#pragma unroll
+        for (int k = 0; k < 2 * kAhead; ++k) {
+            const int64_t i = first + k * 4 * kThreads;
+            const float um = block_unit(em[k], kTopM), uv = block_unit(ev[k], kTopV);
+            f32x4 m, v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a = cm[k] >> (8 * j) & 255;
+                m[j] = decode(a & 127, um);
+                m[j] = a & 128 ? -m[j] : m[j];
+                v[j] = decode(cv[k] >> (8 * j) & 255, uv);
+            }
+            if (t.m_seen) put_four<__bf16>(t.m_seen, i, n, wide, m);
+            if (t.v_seen) put_four<__bf16>(t.v_seen, i, n, wide, v);
+        }
+    };
+    static_assert(kChunk == 2 * kAhead * 4 * kThreads, "one round of a workgroup is a chunk");
+    if (begin + 4 * int(threadIdx.x) >= end) return;
+    if (t.wide && begin + kChunk <= n) pieces(begin + 4 * threadIdx.x, true);
+    else pieces(begin + 4 * threadIdx.x, false);
 }
 
 const char *tensor_fault(const harp_adamw_tensor &t) {
@@ -283,6 +381,8 @@ int harp_adamw_plan(harp_ctx *ctx, const harp_adamw_tensor *tensors, int32_t n_t
         d.state = a.state;
         d.grad_type = a.grad_type;
         d.copy_type = a.copy_type;
+        d.wide = aligned(a.p, 16) && aligned(a.grad, 4 * size_t(type_bytes(a.grad_type))) && aligned(a.copy, 8) && aligned(a.m_seen, 8) &&
+                 aligned(a.v_seen, 8) && aligned(a.m, a.state == HARP_STATE_F32 ? 16 : 4) && aligned(a.v, a.state == HARP_STATE_F32 ? 16 : 4);
         t[i] = d;
         block += uint64_t(a.n + kBlock - 1) / kBlock;
         for (int64_t k = 0; k * kChunk < a.n; ++k) *c++ = Chunk{uint32_t(i), uint32_t(k)};

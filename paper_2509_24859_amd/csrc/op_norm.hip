@@ -92,18 +92,6 @@ __device__ __forceinline__ void load_vector(const float *p, int cols, float othe
     }
 }
 
-// Sum over 16 lanes, the same bits in each: a tree of rotations.
-template <int CTRL> __device__ __forceinline__ float rotated(float x) {
-    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), CTRL, 0xF, 0xF, true));
-}
-__device__ __forceinline__ float sum16(float x) {
-    x += rotated<0x128>(x);      // row_ror:8, 4, 2, 1
-    x += rotated<0x124>(x);
-    x += rotated<0x122>(x);
-    return x + rotated<0x121>(x);
-}
-__device__ __forceinline__ float lane_of(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
-
 // N sums over the workgroup, the same in every thread.  `turn` alternates between two buffers, so that one barrier a
 // round is enough: a buffer is written again only after everybody has passed the next round's barrier.
 struct Exchange {

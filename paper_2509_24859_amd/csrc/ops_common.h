@@ -33,6 +33,30 @@ template <typename T> __device__ __forceinline__ void store4(T *p, f32x4 v) {
     *reinterpret_cast<typename Vec4<T>::type *>(p) = o;
 }
 
+// A value of 16 lanes that a rotation of theirs brings (DPP), and one lane's value for all.
+template <int CTRL> __device__ __forceinline__ uint32_t rotated(uint32_t x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 0xF, 0xF, true); }
+template <int CTRL> __device__ __forceinline__ float rotated(float x) { return __uint_as_float(rotated<CTRL>(__float_as_uint(x))); }
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+__device__ __forceinline__ float lane_of(float x, int lane) { return __uint_as_float(lane_of(__float_as_uint(x), lane)); }
+constexpr int kRotate8 = 0x128, kRotate4 = 0x124, kRotate2 = 0x122, kRotate1 = 0x121;      // row_ror
+
+// Sum over 16 lanes, the same bits in each: a tree of rotations.
+__device__ __forceinline__ float sum16(float x) {
+    x += rotated<kRotate8>(x);
+    x += rotated<kRotate4>(x);
+    x += rotated<kRotate2>(x);
+    return x + rotated<kRotate1>(x);
+}
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+// Largest of a wavefront's values.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+    x = larger(x, rotated<kRotate8>(x));
+    x = larger(x, rotated<kRotate4>(x));
+    x = larger(x, rotated<kRotate2>(x));
+    x = larger(x, rotated<kRotate1>(x));
+    return larger(larger(lane_of(x, 0), lane_of(x, 16)), larger(lane_of(x, 32), lane_of(x, 48)));
+}
+
 // Bytes of an element, 0 for a type that there is none of.
 inline int type_bytes(int type) { return type == HARP_F32 ? 4 : type == HARP_BF16 || type == HARP_F16 ? 2 : 0; }
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
