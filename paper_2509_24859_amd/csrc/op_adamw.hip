@@ -87,6 +87,12 @@ __device__ __forceinline__ void put_codes(uint8_t *a, int64_t i, int64_t n, bool
         if (i + j < n) a[i + j] = uint8_t(c >> (8 * j));
 }
 
+// Square root within a unit of the last place, also of numbers so small that the instruction alone is not.
+__device__ __forceinline__ float root(float v) {
+    const bool small = v < 0x1p-96f;
+    return __builtin_amdgcn_sqrtf(small ? v * 0x1p32f : v) * (small ? 0x1p-16f : 1.0f);
+}
+
 // The new moments and the new weight.  Every product and sum is rounded by itself (no fused multiply-add): the
 // moments in 8 bits are then the same whoever computes them from the formula in 32 bits.  What is taken off the weight
 // is summed up first, decay included: 1 - lr weight_decay as a factor would cost the weight two more roundings.
@@ -94,13 +100,14 @@ __device__ __forceinline__ void update(const Step &s, float g, float decay, floa
 #pragma clang fp contract(off)
     m = m * s.beta1 + g * s.one_minus_beta1;
     v = v * s.beta2 + (g * g) * s.one_minus_beta2;
-    p = p - (p * decay + s.step_size * m / (sqrtf(v) * s.inv_sqrt_c2 + s.eps));
+    p = p - (p * decay + s.step_size * m * __builtin_amdgcn_rcpf(root(v) * s.inv_sqrt_c2 + s.eps));
 }
 
-// 64 random bits for elements 2 k and 2 k + 1 of all tensors' blocks (splitmix64: Steele, Lea, Flood 2014).  Of the
-// lower 32 the lower 16 round m of the even element and the upper its v, of the upper 32 those of the odd one.
-__device__ __forceinline__ uint64_t hash_pair(uint64_t seed, uint64_t k) {
-    uint64_t z = k * 0x9E3779B97F4A7C15ull + seed;
+// 64 random bits for elements 2 k and 2 k + 1 of all tensors' blocks, from z = k kGamma + seed (splitmix64: Steele, Lea,
+// Flood 2014).  Of the lower 32 the lower 16 round m of the even element and the upper its v, of the upper 32 those of
+// the odd one.
+constexpr uint64_t kGamma = 0x9E3779B97F4A7C15ull;
+__device__ __forceinline__ uint64_t hash(uint64_t z) {
     z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
     z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
     return z ^ (z >> 31);
@@ -180,8 +187,9 @@ __global__ __launch_bounds__(kThreads) void adamw_step(const Tensor *tensors, co
         return;
     }
     uint8_t *tm = static_cast<uint8_t *>(t.m), *tv = static_cast<uint8_t *>(t.v);
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / kWave);
     constexpr int kStep = kThreads / kWave * kBlock;       // to a wavefront's next block
+    const uint64_t lane_part = uint64_t(2 * lane) * kGamma;
     auto blocks = [&](int64_t first, bool wide) {
         uint32_t cm[kAhead], cv[kAhead], em[kAhead], ev[kAhead];
         f32x4 g[kAhead], p[kAhead];
@@ -217,11 +225,12 @@ __global__ __launch_bounds__(kThreads) void adamw_step(const Tensor *tensors, co
                 }
             }
             const uint32_t nm = block_exponent(wave_max(most_m)), nv = block_exponent(wave_max(most_v));
-            const uint64_t pair = ((t.first_block + b) * kBlock + 4 * lane) / 2;
+            // k = (element's place) / 2: the block's part is the same for the wavefront
+            const uint64_t z = (t.first_block + b) * (kBlock / 2) * kGamma + s.seed + lane_part;
             uint32_t out_m = 0, out_v = 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const uint64_t bits = hash_pair(s.seed, pair + h);
+                const uint64_t bits = hash(z + h * kGamma);
 #pragma unroll
                 for (int j = 2 * h; j < 2 * h + 2; ++j) {
                     const uint32_t r = uint32_t(bits >> (32 * (j & 1))), bm = __float_as_uint(m[j]);
