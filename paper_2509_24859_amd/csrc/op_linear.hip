@@ -121,10 +121,13 @@ __global__ __launch_bounds__(256) void join(const float *partial, int shares, in
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < P * across; i += int64_t(gridDim.x) * 256) {
         const int64_t p = i / across, q = i % across * 4;
         f32x4 d = {0, 0, 0, 0};
-        for (int s = 0; s < shares; ++s) {
-            const float *o = partial + (s * P + p) * Q + q;
-            for (int k = 0; k < 4; ++k)
-                if (q + k < Q) d[k] += o[k];
+        if (Q % 4 == 0) {
+#pragma unroll 4
+            for (int s = 0; s < shares; ++s) d += load4(partial + (s * P + p) * Q + q);
+        } else {
+            for (int s = 0; s < shares; ++s)
+                for (int k = 0; k < 4; ++k)
+                    if (q + k < Q) d[k] += partial[(s * P + p) * Q + q + k];
         }
         finish4<T>(e, p, q, Q, d);
     }
@@ -409,6 +412,9 @@ template <typename T, bool WIDE> __device__ __forceinline__ typename Mfma<T>::Fr
     typename Mfma<T>::Frag v = {};
     if (WIDE) {
         if (r < R) v = *reinterpret_cast<const typename Mfma<T>::Frag *>(row + r);
+    } else if (r + 8 <= R) {
+        typedef typename Mfma<T>::Frag Loose __attribute__((aligned(sizeof(T))));       // where it lies
+        v = *reinterpret_cast<const Loose *>(row + r);
     } else {
         for (int k = 0; k < 8; ++k)
             if (r + k < R) v[k] = row[r + k];
@@ -565,9 +571,26 @@ Plan plan_for(const harp_ctx *ctx, int kind, int64_t P, int64_t Q, int64_t R) {
         shares = shares < most ? shares : most;
         return split(p, R, shares < 16 ? shares : 16);
     }
-    p.big = tiles(P, Q, 256) >= cu;
-    const int64_t n = tiles(P, Q, p.big ? 256 : 128), slots = p.big ? cu : 2 * cu;
-    return split(p, R, n > 0 && n < slots ? slots / n : 1);
+    // Microseconds by what was measured (4,096 x 16,384 x 4,096 and 1,537 x 1,224 x 4,904): a round of workgroups takes 0.74 for
+    // 32 of r and 13 around them with tiles of 256 x 256, one to a compute unit; 0.5 and 8 with tiles of 128 x 128, two to a
+    // compute unit.  Shares of r cost a launch, and their sums' way through memory.
+    double best = 1e300;
+    for (int big = 0; big < 2; ++big) {
+        const int64_t n = tiles(P, Q, big ? 256 : 128), slots = big ? cu : 2 * cu;
+        for (int64_t shares = 1; shares <= 16; ++shares) {
+            if (shares > 1 && (n * shares > slots || R < shares * 4 * kPiece)) break;
+            Plan t = {};
+            t.big = big;
+            t = split(t, R, shares);
+            double us = double((n * t.shares + slots - 1) / slots) * (double(t.share < R ? t.share : R) / 32 * (big ? 0.74 : 0.5) + (big ? 13 : 8));
+            if (t.shares > 1) us += 4 + double(t.shares) * double(P) * double(Q) * 8 / 4e6;
+            if (us < best) {
+                best = us;
+                p = t;
+            }
+        }
+    }
+    return p;
 }
 
 size_t packed_bytes(int64_t rows, int64_t cols) { return round_up(size_t(rows) * round_up(size_t(cols), 8) * 2, 256); }
