@@ -57,6 +57,12 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
     return larger(larger(lane_of(x, 0), lane_of(x, 16)), larger(lane_of(x, 32), lane_of(x, 48)));
 }
 
+// The same, past the caches: for what is larger than they are.
+template <typename T> __device__ __forceinline__ void store4_past(T *p, f32x4 v) {
+    typename Vec4<T>::type o = {T(v.x), T(v.y), T(v.z), T(v.w)};
+    __builtin_nontemporal_store(o, reinterpret_cast<typename Vec4<T>::type *>(p));
+}
+
 // Bytes of an element, 0 for a type that there is none of.
 inline int type_bytes(int type) { return type == HARP_F32 ? 4 : type == HARP_BF16 || type == HARP_F16 ? 2 : 0; }
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
