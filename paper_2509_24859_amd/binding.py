@@ -182,6 +182,7 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU visible: the planner has no CPU path")
         self.device = torch.device("cuda", device_ordinal)
+        self.index = device_ordinal
         h = C.c_void_p()
         rc = self.lib.harp_create(C.byref(h), device_ordinal)
         if rc != OK:

@@ -63,7 +63,7 @@ __device__ __forceinline__ float slope(float z, int act) {
 // What becomes of D[p][q].
 enum { kForward, kInput, kWeight };
 struct Epilogue {
-    int kind, act, accumulate, out_f32, wide;
+    int kind, act, accumulate, out_f32;
     int past;                        // results are stored past the caches
     void *out;
     const void *bias, *residual;     // residual: [p][q]
@@ -93,9 +93,9 @@ template <typename O> __device__ __forceinline__ void put4(const Epilogue &e, O 
     if (e.past) store4_past(o, d);
     else store4(o, d);
 }
-// The same for q .. q + 3.  `wide`: all of it is there and aligned.
+// The same for q .. q + 3.
 template <typename T> __device__ __forceinline__ void finish4(const Epilogue &e, int64_t p, int64_t q, int64_t Q, f32x4 d) {
-    if (!e.wide) {
+    if (q + 4 > Q) {
 #pragma unroll 1
         for (int k = 0; k < 4 && q < Q; ++k, ++q) {
             finish<T>(e, p, q, d.x);
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256) void join(const float *partial, int shares, in
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < P * across; i += int64_t(gridDim.x) * 256) {
         const int64_t p = i / across, q = i % across * 4;
         f32x4 d = {0, 0, 0, 0};
-        if (Q % 4 == 0) {
+        if (q + 4 <= Q) {
 #pragma unroll 4
             for (int s = 0; s < shares; ++s) d += load4(partial + (s * P + p) * Q + q);
         } else {
@@ -146,8 +146,14 @@ __global__ __launch_bounds__(256) void pack(const T *from, int64_t ld, int64_t r
     const int64_t across = ldto / 8;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < rows * across; i += int64_t(gridDim.x) * 256) {
         const int64_t row = i / across, c = i % across * 8;
-        typename Mfma<T>::Frag v;
-        for (int k = 0; k < 8; ++k) v[k] = c + k < cols ? from[row * ld + c + k] : T(0.0f);
+        typedef typename Mfma<T>::Frag Loose __attribute__((aligned(sizeof(T))));
+        typename Mfma<T>::Frag v = {};
+        if (c + 8 <= cols) {
+            v = *reinterpret_cast<const Loose *>(from + row * ld + c);
+        } else {
+            for (int k = 0; k < 8; ++k)
+                if (c + k < cols) v[k] = from[row * ld + c + k];
+        }
         *reinterpret_cast<typename Mfma<T>::Frag *>(to + row * ldto + c) = v;
     }
 }
@@ -392,7 +398,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
     // hold, and rows are stored in whole lines.  What the epilogue reads of the next 16 p is asked for before the current
     // ones are worked on (4,096 x 16,384 x 4,096 forward with bias, tanh GELU and Z kept 515 us without, 497 so); not of a
     // weight gradient to add to, where reads and writes of 32 bits contend for memory (508 us without, 540 so).
-    if (partial) e = Epilogue{kWeight, HARP_ACT_NONE, 0, 1, Q % 4 == 0, 0, partial + int64_t(blockIdx.y) * P * Q, nullptr, nullptr, nullptr, nullptr, Q, 0, 0};
+    if (partial) e = Epilogue{kWeight, HARP_ACT_NONE, 0, 1, 0, partial + int64_t(blockIdx.y) * P * Q, nullptr, nullptr, nullptr, nullptr, Q, 0, 0};
     constexpr int kCols = BQ / WQ, kPitch = kCols + 4, kLanes = kCols / 4, kRows = kWave / kLanes, kParts = 16 / kRows;
     static_assert(WP * WQ * 16 * kPitch * 4 <= kBuffers * BP * kDeep * 2, "the wavefronts' rows have to fit into the first operand's LDS");
     float *rows = reinterpret_cast<float *>(&la[0][0]) + wave * 16 * kPitch;
@@ -441,7 +447,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
             __builtin_amdgcn_wave_barrier();
         }
     };
-    if (A_ACROSS || !e.wide) {
+    if (A_ACROSS || (q0 + BQ > Q && Q % 4 != 0)) {       // some lane's four q are not all there
 #pragma unroll
         for (int i = 0; i < kP; ++i) {
             through_lds(i);
@@ -735,9 +741,6 @@ template <typename T>
 void launch_product(const harp_ctx *ctx, Given a, Given b, int64_t P, int64_t Q, int64_t R, Epilogue e, void *workspace, hipStream_t st) {
     const Plan plan = plan_for(ctx, e.kind, P, Q, R);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
-    const size_t out = e.out_f32 ? 16 : 8;
-    e.wide = Q % 4 == 0 && e.ldo % 4 == 0 && aligned(e.out, out) && aligned(e.bias, 8) && aligned(e.residual, 8) && aligned(e.slope_at, 8) &&
-             aligned(e.keep, 8) && (!e.residual || e.ldr % 4 == 0) && ((!e.slope_at && !e.keep) || e.ldz % 4 == 0);
     // Compute units finish their tiles together; what they then store at once has to leave the L2 caches of 32 MiB at the
     // fabric's pace.  Past the caches 4,096 x 16,384 x 4,096 takes 440 us where it took 473 (32-bit results).
     e.past = size_t(P) * size_t(Q) * (e.out_f32 ? 4 : 2) >= size_t(32) << 20;
@@ -788,7 +791,7 @@ int harp_linear_forward(harp_ctx *ctx, const harp_linear *g, void *workspace, si
                         {"residual", g->residual, g->ldr, g->N, 2, false}, {"Y", g->Y, g->ldy, g->N, 2, some}, {"Z", g->Z, g->ldz, g->N, 2, false}};
     const int rc = check(ctx, g->M, g->N, g->K, g->type, g->act, m, 6, workspace, workspace_bytes);
     if (rc != HARP_OK || !some) return rc;
-    const Epilogue e = {kForward, g->act, 0, 0, 0, 0, g->Y, g->bias, g->residual, nullptr, g->Z, g->ldy, g->ldr, g->ldz};
+    const Epilogue e = {kForward, g->act, 0, 0, 0, g->Y, g->bias, g->residual, nullptr, g->Z, g->ldy, g->ldr, g->ldz};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (g->type == HARP_BF16) launch_product<__bf16>(ctx, {g->X, g->ldx, g->M, g->K}, {g->W, g->ldw, g->N, g->K}, g->M, g->N, g->K, e, workspace, st);
     else launch_product<_Float16>(ctx, {g->X, g->ldx, g->M, g->K}, {g->W, g->ldw, g->N, g->K}, g->M, g->N, g->K, e, workspace, st);
@@ -804,7 +807,7 @@ int harp_linear_grad_input(harp_ctx *ctx, const harp_linear_input *g, void *work
                         {"residual", g->residual, g->ldr, g->K, 2, false}, {"dX", g->dX, g->lddx, g->K, 2, some}};
     const int rc = check(ctx, g->M, g->N, g->K, g->type, g->act, m, 5, workspace, workspace_bytes);
     if (rc != HARP_OK || !some) return rc;
-    const Epilogue e = {kInput, g->act, 0, 0, 0, 0, g->dX, nullptr, g->residual, g->act != HARP_ACT_NONE ? g->Z : nullptr, nullptr, g->lddx, g->ldr, g->ldz};
+    const Epilogue e = {kInput, g->act, 0, 0, 0, g->dX, nullptr, g->residual, g->act != HARP_ACT_NONE ? g->Z : nullptr, nullptr, g->lddx, g->ldr, g->ldz};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (g->type == HARP_BF16) launch_product<__bf16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->W, g->ldw, g->N, g->K}, g->M, g->K, g->N, e, workspace, st);
     else launch_product<_Float16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->W, g->ldw, g->N, g->K}, g->M, g->K, g->N, e, workspace, st);
@@ -821,7 +824,7 @@ int harp_linear_grad_weight(harp_ctx *ctx, const harp_linear_weight *g, void *wo
     const int rc = check(ctx, g->M, g->N, g->K, g->type, HARP_ACT_NONE, m, 4, workspace, workspace_bytes);
     if (rc != HARP_OK) return rc;
     if (!some && g->accumulate) return HARP_OK;
-    const Epilogue e = {kWeight, HARP_ACT_NONE, g->accumulate, g->dw_type == HARP_F32, 0, 0, g->dW, nullptr, nullptr, nullptr, nullptr, g->lddw, 0, 0};
+    const Epilogue e = {kWeight, HARP_ACT_NONE, g->accumulate, g->dw_type == HARP_F32, 0, g->dW, nullptr, nullptr, nullptr, nullptr, g->lddw, 0, 0};
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (g->type == HARP_BF16) launch_product<__bf16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->X, g->ldx, g->M, g->K}, g->N, g->K, g->M, e, workspace, st);
     else launch_product<_Float16>(ctx, {g->dY, g->lddy, g->M, g->N}, {g->X, g->ldx, g->M, g->K}, g->N, g->K, g->M, e, workspace, st);

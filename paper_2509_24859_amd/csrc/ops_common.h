@@ -20,17 +20,24 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__bf16 x) { return float(x); }
 __device__ __forceinline__ float to_f32(_Float16 x) { return float(x); }
 
-template <typename T> struct Vec4 {                   // 4 elements of 2 bytes as one load
+template <typename T> struct Vec4 {                   // 4 elements as one load, where an element may lie
     typedef T type __attribute__((ext_vector_type(4)));
+    typedef type loose __attribute__((aligned(sizeof(T))));
 };
 
+// Four neighbouring elements.  Memory takes them at any alignment of the elements, with the same instruction.
 template <typename T> __device__ __forceinline__ f32x4 load4(const T *p) {
-    const typename Vec4<T>::type v = *reinterpret_cast<const typename Vec4<T>::type *>(p);
+    const typename Vec4<T>::type v = *reinterpret_cast<const typename Vec4<T>::loose *>(p);
     return f32x4{to_f32(v.x), to_f32(v.y), to_f32(v.z), to_f32(v.w)};
 }
 template <typename T> __device__ __forceinline__ void store4(T *p, f32x4 v) {
     typename Vec4<T>::type o = {T(v.x), T(v.y), T(v.z), T(v.w)};
-    *reinterpret_cast<typename Vec4<T>::type *>(p) = o;
+    *reinterpret_cast<typename Vec4<T>::loose *>(p) = o;
+}
+// The same, past the caches: for what is larger than they are.
+template <typename T> __device__ __forceinline__ void store4_past(T *p, f32x4 v) {
+    typename Vec4<T>::type o = {T(v.x), T(v.y), T(v.z), T(v.w)};
+    __builtin_nontemporal_store(o, reinterpret_cast<typename Vec4<T>::loose *>(p));
 }
 
 // A value of 16 lanes that a rotation of theirs brings (DPP), and one lane's value for all.
@@ -55,12 +62,6 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
     x = larger(x, rotated<kRotate2>(x));
     x = larger(x, rotated<kRotate1>(x));
     return larger(larger(lane_of(x, 0), lane_of(x, 16)), larger(lane_of(x, 32), lane_of(x, 48)));
-}
-
-// The same, past the caches: for what is larger than they are.
-template <typename T> __device__ __forceinline__ void store4_past(T *p, f32x4 v) {
-    typename Vec4<T>::type o = {T(v.x), T(v.y), T(v.z), T(v.w)};
-    __builtin_nontemporal_store(o, reinterpret_cast<typename Vec4<T>::type *>(p));
 }
 
 // Bytes of an element, 0 for a type that there is none of.

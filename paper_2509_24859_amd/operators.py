@@ -43,7 +43,7 @@ def _vector(ctx, t, n, dtype, name):
     """The address of a contiguous vector of n elements, or None."""
     if t is None:
         return None
-    if t.get_device() != ctx.device.index:
+    if t.get_device() != ctx.index:
         raise _elsewhere(ctx, t, name)
     if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
         raise HarpError(ERR_SHAPE, "%s: %d contiguous elements of %s are wanted, got %s of %s"
@@ -64,23 +64,31 @@ def _matrix(ctx, t, shape, dtype, name):
     """(address, leading dimension) of a matrix whose rows are contiguous; (None, columns) for None."""
     if t is None:
         return None, shape[1]
-    if t.get_device() != ctx.device.index:
+    if t.get_device() != ctx.index:
         raise _elsewhere(ctx, t, name)
     if t.dtype is not dtype or t.shape != shape:
         raise HarpError(ERR_SHAPE, "%s: %s of %s is wanted, got %s of %s" % (name, tuple(shape), dtype, tuple(t.shape), t.dtype))
-    rows, cols = shape
+    cols = shape[1]
+    if t.is_contiguous():
+        return t.data_ptr(), cols
+    rows = shape[0]
     row, col = t.stride()
     if (col != 1 and cols > 1) or (row < cols and rows > 1):
         raise HarpError(ERR_SHAPE, "%s: rows must be contiguous and apart, its strides are %s" % (name, (row, col)))
     return t.data_ptr(), row if row > cols else cols
 
 
+def _current(ctx: Context) -> int:
+    """The handle of torch's current stream."""
+    raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)      # without an object around it
+    return raw(ctx.index) if raw else int(_torch().cuda.current_stream(ctx.device).cuda_stream)
+
+
 def _stream(ctx: Context, stream, tensors):
     """The stream's handle.  Tensors used on another stream than torch's current one are recorded there, so that
     their memory is not handed out again before the call has run."""
     if stream is None:
-        raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)      # the handle without an object around it
-        return raw(ctx.device.index) if raw else int(_torch().cuda.current_stream(ctx.device).cuda_stream)
+        return _current(ctx)
     if stream != _torch().cuda.current_stream(ctx.device):
         for t in tensors:
             if t is not None:
@@ -91,7 +99,7 @@ def _stream(ctx: Context, stream, tensors):
 def _workspace(ctx, w):
     if w is None:
         return None, 0
-    if w.get_device() != ctx.device.index:
+    if w.get_device() != ctx.index:
         raise _elsewhere(ctx, w, "the workspace")
     return w.data_ptr(), w.numel() * w.element_size()
 
