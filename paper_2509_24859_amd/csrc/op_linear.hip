@@ -159,8 +159,9 @@ __global__ __launch_bounds__(256) void pack(const T *from, int64_t ld, int64_t r
 }
 
 // ---------------------------------------------------------------------------------------------- tiles
-// A workgroup makes a tile of BP x BQ of D, 32 of r at a time.  Both operands go from memory straight into LDS, three
-// steps before they are multiplied (four buffers).
+// A workgroup makes a tile of BP x BQ of D, 32 of r at a time.  Both operands go from memory straight into LDS, three or four
+// steps before they are multiplied (five buffers, all of LDS for tiles of 256 x 256).  Two steps are sent for at once: where r
+// is contiguous they are the two halves of lines of 128 bytes.
 //
 // LDS holds pieces of 16 bytes.  Where r is contiguous in memory a row of the tile is 4 pieces of 8 r, piece c of row
 // `row` at place c ^ (row / 2 & 3): the 8 rows that a wavefront reads at once then lie in 8 different places of 128 bytes.
@@ -209,10 +210,20 @@ template <typename T, bool ACROSS, int B, int THREADS> struct Side {
             off[i] = uint32_t(ACROSS ? depth(i) * ld + at : at * ld + depth(i)) * uint32_t(sizeof(T));
         }
     }
+    // The next step, or the next two: one after the other, each piece's two halves of a line together.
     __device__ __forceinline__ void load(T *lds) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) load_to_lds(base, off[i], target(lds, i));
         base += step;
+    }
+    __device__ __forceinline__ void load_two(T *lds, T *after) {
+        const char *next = base + step;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            load_to_lds(base, off[i], target(lds, i));
+            load_to_lds(next, off[i], target(after, i));
+        }
+        base = next + step;
     }
     // The last, partial step of `left` r: what is beyond is read from the last r there are, and made zeros by clear() when
     // it has arrived.  Rows of r that are not a multiple of 8 long have zeros up to there.
@@ -276,10 +287,12 @@ __device__ __forceinline__ void tile_of(int id, int tiles_p, int tiles_q, int &t
 
 // WP x WQ wavefronts, each a part of BP / WP x BQ / WQ of the tile.  With `partial` the sums of blockIdx.y's share of r go
 // there, [share][P][Q], instead of through the epilogue.
-template <typename T, bool A_ACROSS, bool B_ACROSS, int BP, int BQ, int WP, int WQ, int kBuffers>
+template <typename T, bool A_ACROSS, bool B_ACROSS, int BP, int BQ, int WP, int WQ>
 __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t lda, const T *b, int64_t ldb, int64_t P, int64_t Q, int64_t R,
                                                            int tiles_p, int tiles_q, int64_t share, float *partial, Epilogue e) {
     constexpr int kThreads = WP * WQ * kWave, kP = BP / WP / 16, kQ = BQ / WQ / 16;
+    constexpr bool kPairs = !(A_ACROSS && B_ACROSS);
+    constexpr int kBuffers = kPairs ? 5 : 4;
     __shared__ __align__(16) T la[kBuffers][BP * kDeep];
     __shared__ __align__(16) T lb[kBuffers][BQ * kDeep];
     int tp, tq;
@@ -299,13 +312,18 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
     f32x4 acc[kP][kQ] = {};
     typedef typename Mfma<T>::Frag Frag;
     const int steps = int((r1 - r0 + kDeep - 1) / kDeep), odd = int((r1 - r0) % kDeep);     // odd: r of a partial last step
-    auto bring = [&](int i) {
-        if (i + 1 < steps || odd == 0) {
-            sa.load(la[i % kBuffers]);
-            sb.load(lb[i % kBuffers]);
+    // An operand of a step, whole or not; of two steps where r is contiguous and they share lines.
+    auto bring = [&](auto &side, auto *lds, int i) {
+        if (i >= steps) return;
+        if (i + 1 < steps || odd == 0) side.load(lds[i % kBuffers]);
+        else side.load_partial(lds[i % kBuffers], odd);
+    };
+    auto bring_two = [&](auto &side, auto *lds, int i) {
+        if (i + 2 < steps || (i + 2 == steps && odd == 0)) {
+            side.load_two(lds[i % kBuffers], lds[(i + 1) % kBuffers]);
         } else {
-            sa.load_partial(la[i % kBuffers], odd);
-            sb.load_partial(lb[i % kBuffers], odd);
+            bring(side, lds, i);
+            bring(side, lds, i + 1);
         }
     };
     auto barrier = [] {
@@ -313,19 +331,20 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
         asm volatile("" ::: "memory");
     };
     // Step i is in LDS for everybody, and nobody reads the buffer of step i - 1 any more.  Loads into LDS are counted by
-    // vmcnt, which a barrier alone does not wait for; they arrive in order, so those of later steps may be out still.
-    constexpr int kLoads = decltype(sa)::kLoads + decltype(sb)::kLoads;
+    // vmcnt, which a barrier alone does not wait for; they arrive in order, so what was sent for after step i may be out
+    // still: of an operand that comes in pairs the next pair of steps, of the other kBuffers - 2 steps.  At the end there is
+    // less, and the wait is for more than has to be.
+    constexpr int kA = decltype(sa)::kLoads, kB = decltype(sb)::kLoads;
+    constexpr int kOut = (kPairs && !A_ACROSS ? 2 : kBuffers - 2) * kA + (kPairs && !B_ACROSS ? 2 : kBuffers - 2) * kB;
     auto arrived = [&](int i) {
-        if (i + kBuffers - 2 < steps) {
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kBuffers - 2) * kLoads) : "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            if (i + 1 == steps && odd) {
-                sa.clear(la[i % kBuffers], odd);
-                sb.clear(lb[i % kBuffers], odd);
-            }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (i + kBuffers - 2 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kOut) : "memory");
+        else if (i + 2 < steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kA + kB) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (i + 1 == steps && odd) {
+            sa.clear(la[i % kBuffers], odd);
+            sb.clear(lb[i % kBuffers], odd);
         }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         barrier();
     };
     auto read = [&](int buffer, Frag (&x)[kP], Frag (&y)[kQ]) {
@@ -354,26 +373,37 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
     };
     Frag x[2][kP], y[2][kQ];
     if (steps > 0) {
-        for (int i = 0; i < kBuffers && i < steps; ++i) bring(i);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (steps <= kBuffers && odd) {
-            sa.clear(la[steps - 1], odd);
-            sb.clear(lb[steps - 1], odd);
+        // First what steps 0 and 1 need, then the rest that the buffers hold, in an order in which no step's loads lie among
+        // the last kOut when it is waited for.
+        static_assert(!A_ACROSS || B_ACROSS, "only the second operand comes in pairs: the order would have to be another");
+        if (kPairs && !A_ACROSS) bring_two(sa, la, 0);
+        else { bring(sa, la, 0); bring(sa, la, 1); }
+        if (kPairs && !B_ACROSS) bring_two(sb, lb, 0);
+        else { bring(sb, lb, 0); bring(sb, lb, 1); }
+        if (kPairs) bring_two(sa, la, 2);
+        if (kPairs && !B_ACROSS) bring_two(sb, lb, 2);
+        for (int i = 2; i < kBuffers; ++i) {
+            if (!kPairs) bring(sa, la, i);
+            if (!kPairs || B_ACROSS) bring(sb, lb, i);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (steps >= kBuffers + 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kOut) : "memory");
+        else arrived(steps - 1);                         // few steps: all of them
         barrier();
         read(0, x[0], y[0]);
-        // Step i has its operands in registers.  Behind its barrier step i + 1 has arrived, and the buffer of step i is free
-        // for step i + kBuffers.  Several steps at a time while all that they bring is whole: buffers are known then.
-        int i = 0;
+        // Step i has its operands in registers.  Behind its barrier step i + 1 has arrived, and the buffers of step i and of
+        // the one before are free: for step i + kBuffers, and for pairs every other time, for steps i + 4 and i + 5.  A round
+        // of steps at a time while all that they bring is whole: buffers are known then.
         constexpr int kRound = kBuffers % 2 ? 2 * kBuffers : kBuffers;
+        int i = 0;
         for (; i + kRound + kBuffers < steps; i += kRound) {
 #pragma unroll
             for (int k = 0; k < kRound; ++k) {
-                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kBuffers - 2) * kLoads) : "memory");
+                asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(kOut) : "memory");
                 barrier();
-                sa.load(la[k % kBuffers]);
-                sb.load(lb[k % kBuffers]);
+                if (!(kPairs && !A_ACROSS)) sa.load(la[k % kBuffers]);
+                else if (k % 2 == 0) sa.load_two(la[(k + 4) % kBuffers], la[k % kBuffers]);
+                if (!(kPairs && !B_ACROSS)) sb.load(lb[k % kBuffers]);
+                else if (k % 2 == 0) sb.load_two(lb[(k + 4) % kBuffers], lb[k % kBuffers]);
                 __builtin_amdgcn_sched_barrier(0);
                 read((k + 1) % kBuffers, x[(k + 1) % 2], y[(k + 1) % 2]);
                 multiply(x[k % 2], y[k % 2]);
@@ -382,7 +412,10 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
         }
         for (; i + 1 < steps; ++i) {
             arrived(i + 1);
-            if (i + kBuffers < steps) bring(i + kBuffers);
+            if (!(kPairs && !A_ACROSS)) bring(sa, la, i + kBuffers);
+            else if (i % 2 == 0) bring_two(sa, la, i + 4);
+            if (!(kPairs && !B_ACROSS)) bring(sb, lb, i + kBuffers);
+            else if (i % 2 == 0) bring_two(sb, lb, i + 4);
             read((i + 1) % kBuffers, x[1], y[1]);
             multiply(x[0], y[0]);
 #pragma unroll
@@ -723,8 +756,8 @@ void launch_tiles(const Plan &plan, const Given &a, const Given &b, int64_t P, i
     const int tp = int((P + side - 1) / side), tq = int((Q + side - 1) / side);
     const dim3 grid(uint32_t(tp) * uint32_t(tq), uint32_t(plan.shares));
     const T *pa = static_cast<const T *>(a.a), *pb = static_cast<const T *>(b.a);
-    if (plan.big) product<T, A_ACROSS, B_ACROSS, 256, 256, 2, 4, 4><<<grid, dim3(512), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
-    else product<T, A_ACROSS, B_ACROSS, 128, 128, 2, 2, 4><<<grid, dim3(256), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
+    if (plan.big) product<T, A_ACROSS, B_ACROSS, 256, 256, 2, 4><<<grid, dim3(512), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
+    else product<T, A_ACROSS, B_ACROSS, 128, 128, 2, 2><<<grid, dim3(256), 0, st>>>(pa, a.ld, pb, b.ld, P, Q, R, tp, tq, plan.share, partial, e);
 }
 
 template <typename T, bool WIDE>
