@@ -89,10 +89,6 @@ template <typename T> __device__ __forceinline__ void finish(const Epilogue &e, 
     }
 }
 
-template <typename O> __device__ __forceinline__ void put4(const Epilogue &e, O *o, f32x4 d) {
-    if (e.past) store4_past(o, d);
-    else store4(o, d);
-}
 // The same for q .. q + 3.
 template <typename T> __device__ __forceinline__ void finish4(const Epilogue &e, int64_t p, int64_t q, int64_t Q, f32x4 d) {
     if (q + 4 > Q) {
@@ -105,7 +101,7 @@ template <typename T> __device__ __forceinline__ void finish4(const Epilogue &e,
     }
     if (e.kind == kForward) {
         if (e.bias) d += load4(static_cast<const T *>(e.bias) + q);
-        if (e.keep) put4(e, static_cast<T *>(e.keep) + p * e.ldz + q, d);
+        if (e.keep) store4(static_cast<T *>(e.keep) + p * e.ldz + q, d, e.past);
         for (int k = 0; k < 4; ++k) d[k] = activate(d[k], e.act);
     } else if (e.kind == kInput && e.act != HARP_ACT_NONE) {
         const f32x4 z = load4(static_cast<const T *>(e.slope_at) + p * e.ldz + q);
@@ -114,10 +110,10 @@ template <typename T> __device__ __forceinline__ void finish4(const Epilogue &e,
     if (e.residual) d += load4(static_cast<const T *>(e.residual) + p * e.ldr + q);
     if (e.out_f32) {
         float *o = static_cast<float *>(e.out) + p * e.ldo + q;
-        put4(e, o, e.accumulate ? d + load4(o) : d);
+        store4(o, e.accumulate ? d + load4(o) : d, e.past);
     } else {
         T *o = static_cast<T *>(e.out) + p * e.ldo + q;
-        put4(e, o, e.accumulate ? d + load4(o) : d);
+        store4(o, e.accumulate ? d + load4(o) : d, e.past);
     }
 }
 
@@ -466,7 +462,7 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
                 if (p >= P || q >= Q) continue;
                 f32x4 d = from_lds(k) + bias;
                 if (e.kind == kForward) {
-                    if (e.keep) put4(e, static_cast<T *>(e.keep) + p * e.ldz + q, d);
+                    if (e.keep) store4(static_cast<T *>(e.keep) + p * e.ldz + q, d, e.past);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) d[j] = activate(d[j], act);
                 } else if (act != HARP_ACT_NONE) {
@@ -474,8 +470,8 @@ __global__ __launch_bounds__(WP * WQ * kWave) void product(const T *a, int64_t l
                     for (int j = 0; j < 4; ++j) d[j] *= slope(z[i % 2][k][j], act);
                 }
                 if (e.residual) d += more[i % 2][k];
-                if (e.out_f32) put4(e, static_cast<float *>(e.out) + p * e.ldo + q, d);
-                else put4(e, static_cast<T *>(e.out) + p * e.ldo + q, d);
+                if (e.out_f32) store4(static_cast<float *>(e.out) + p * e.ldo + q, d, e.past);
+                else store4(static_cast<T *>(e.out) + p * e.ldo + q, d, e.past);
             }
             __builtin_amdgcn_wave_barrier();
         }
@@ -775,7 +771,7 @@ void launch_product(const harp_ctx *ctx, Given a, Given b, int64_t P, int64_t Q,
     const Plan plan = plan_for(ctx, e.kind, P, Q, R);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     // Compute units finish their tiles together; what they then store at once has to leave the L2 caches of 32 MiB at the
-    // fabric's pace.  Past the caches 4,096 x 16,384 x 4,096 takes 440 us where it took 473 (32-bit results).
+    // fabric's pace.  Past the caches the gradients of 4,096 tokens take 1,010 us where they took 1,033.
     e.past = size_t(P) * size_t(Q) * (e.out_f32 ? 4 : 2) >= size_t(32) << 20;
     if (!plan.few) {
         a = packed<T>(a, ws, st);

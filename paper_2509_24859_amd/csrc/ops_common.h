@@ -30,14 +30,22 @@ template <typename T> __device__ __forceinline__ f32x4 load4(const T *p) {
     const typename Vec4<T>::type v = *reinterpret_cast<const typename Vec4<T>::loose *>(p);
     return f32x4{to_f32(v.x), to_f32(v.y), to_f32(v.z), to_f32(v.w)};
 }
-template <typename T> __device__ __forceinline__ void store4(T *p, f32x4 v) {
-    typename Vec4<T>::type o = {T(v.x), T(v.y), T(v.z), T(v.w)};
-    *reinterpret_cast<typename Vec4<T>::loose *>(p) = o;
+// `past`: not kept in the caches, for what is larger than they are.  The empty statements keep the compiler from making one
+// store of the two, which it does by dropping what tells them apart.
+template <int ALIGN, typename V> __device__ __forceinline__ void store_as(void *to, V v, bool past) {
+    typedef V Loose __attribute__((aligned(ALIGN)));
+    Loose *p = static_cast<Loose *>(to);
+    if (past) {
+        asm volatile("");
+        __builtin_nontemporal_store(v, p);
+        asm volatile("");
+    } else {
+        *p = v;
+    }
 }
-// The same, past the caches: for what is larger than they are.
-template <typename T> __device__ __forceinline__ void store4_past(T *p, f32x4 v) {
-    typename Vec4<T>::type o = {T(v.x), T(v.y), T(v.z), T(v.w)};
-    __builtin_nontemporal_store(o, reinterpret_cast<typename Vec4<T>::loose *>(p));
+template <typename T> __device__ __forceinline__ void store4(T *p, f32x4 v, bool past = false) {
+    const typename Vec4<T>::type o = {T(v.x), T(v.y), T(v.z), T(v.w)};
+    store_as<int(sizeof(T))>(p, o, past);
 }
 
 // A value of 16 lanes that a rotation of theirs brings (DPP), and one lane's value for all.

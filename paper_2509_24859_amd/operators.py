@@ -192,6 +192,10 @@ class harp_adamw_hyper(C.Structure):
                 ("step", C.c_int64), ("seed", C.c_uint64), ("grad_scale", C.c_void_p), ("skip", C.c_void_p)]
 
 
+_ADAMW_NEEDED = frozenset(("p", "grad", "m", "v"))
+_ADAMW_KNOWN = _ADAMW_NEEDED | {"copy", "m_exp", "v_exp", "m_seen", "v_seen", "weight_decay"}
+
+
 class AdamW:
     """harp_adamw_plan / harp_adamw_step / harp_adamw_read_state / harp_adamw_release.
 
@@ -206,37 +210,35 @@ class AdamW:
 
     def __init__(self, ctx: Context, tensors, stream=None):
         torch = _torch()
+        f32, u8, bf16 = torch.float32, torch.uint8, torch.bfloat16
         self.ctx, self.handle = ctx, None
         self.tensors = [dict(t) for t in tensors]
         array = (harp_adamw_tensor * max(len(self.tensors), 1))()
-        held = []
         for a, t in zip(array, self.tensors):
-            unknown = set(t) - {"p", "grad", "m", "v", "copy", "m_exp", "v_exp", "m_seen", "v_seen", "weight_decay"}
-            if unknown or not {"p", "grad", "m", "v"} <= set(t):
+            if not (_ADAMW_NEEDED <= t.keys() <= _ADAMW_KNOWN):
                 raise HarpError(ERR_INVALID_ARG, "a tensor's entry needs p, grad, m and v, and knows no %s"
-                                % (", ".join(sorted(unknown)) or "other"))
-            n = t["p"].numel()
-            eight = t["m"].dtype == torch.uint8
-            kind = torch.uint8 if eight else torch.float32
-            a.n, a.state = n, STATE_8BIT if eight else STATE_F32
-            a.p = _vector(ctx, t["p"], n, torch.float32, "p")
-            a.grad_type = _type(t["grad"])
-            a.grad = _vector(ctx, t["grad"], n, t["grad"].dtype, "grad")
-            a.m, a.v = _vector(ctx, t["m"], n, kind, "m"), _vector(ctx, t["v"], n, kind, "v")
+                                % (", ".join(sorted(t.keys() - _ADAMW_KNOWN)) or "other"))
+            get = t.get
+            p, grad, m, copy = t["p"], t["grad"], t["m"], get("copy")
+            n = a.n = p.numel()
+            eight = m.dtype is u8
+            kind, a.state = (u8, STATE_8BIT) if eight else (f32, STATE_F32)
+            a.p = _vector(ctx, p, n, f32, "p")
+            a.grad_type = _type(grad)
+            a.grad = _vector(ctx, grad, n, grad.dtype, "grad")
+            a.m, a.v = _vector(ctx, m, n, kind, "m"), _vector(ctx, t["v"], n, kind, "v")
             if eight:
                 blocks = -(-n // ADAMW_BLOCK)
-                if t.get("m_exp") is None or t.get("v_exp") is None:
+                if get("m_exp") is None or get("v_exp") is None:
                     raise HarpError(ERR_INVALID_ARG, "8-bit moments need m_exp and v_exp")
-                a.m_exp = _vector(ctx, t["m_exp"], blocks, torch.uint8, "m_exp")
-                a.v_exp = _vector(ctx, t["v_exp"], blocks, torch.uint8, "v_exp")
-            if t.get("copy") is not None:
-                a.copy_type = _type(t["copy"], (BF16, F16))
-                a.copy = _vector(ctx, t["copy"], n, t["copy"].dtype, "copy")
-            a.m_seen = _vector(ctx, t.get("m_seen"), n, torch.bfloat16, "m_seen")
-            a.v_seen = _vector(ctx, t.get("v_seen"), n, torch.bfloat16, "v_seen")
-            a.weight_decay = float(t.get("weight_decay", 0.0))
-            held += [x for x in t.values() if isinstance(x, torch.Tensor)]
-        self.held = held
+                a.m_exp = _vector(ctx, t["m_exp"], blocks, u8, "m_exp")
+                a.v_exp = _vector(ctx, t["v_exp"], blocks, u8, "v_exp")
+            if copy is not None:
+                a.copy_type = _type(copy, (BF16, F16))
+                a.copy = _vector(ctx, copy, n, copy.dtype, "copy")
+            a.m_seen = _vector(ctx, get("m_seen"), n, bf16, "m_seen")
+            a.v_seen = _vector(ctx, get("v_seen"), n, bf16, "v_seen")
+            a.weight_decay = get("weight_decay", 0.0)
         nbytes = ctx.lib.harp_adamw_plan_bytes(array, len(self.tensors))
         self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=ctx.device)
         h = C.c_void_p()
@@ -261,7 +263,8 @@ class AdamW:
     def _on_stream(self, stream, *more):
         if stream is None:
             return _stream(self.ctx, None, ())
-        return _stream(self.ctx, stream, [self.buf, *self.held, *more])
+        held = [x for t in self.tensors for x in t.values() if hasattr(x, "record_stream")]
+        return _stream(self.ctx, stream, [self.buf, *held, *more])
 
     def release(self):
         if self.handle:
