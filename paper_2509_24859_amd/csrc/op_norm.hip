@@ -4,6 +4,10 @@
 // A row's channels lie in the registers of one workgroup, eight to a thread, so that every tensor is read once and
 // written once: the pass is bound by memory.  A workgroup takes rows in turn and keeps what belongs to its channels
 // (weights, biases, scale, and in the backward pass the sums over rows) in registers throughout.
+//
+// Measured, bfloat16, RMS norms on both sides, one gate, a scale: forward of 4,096 x 8,192 63 us, 4.2 TB/s, backward 109 us, 3.7
+// TB/s (a copy reaches 4.9); one row 4.5 us in the kernel.  A workgroup of 1,024 threads has a compute unit to itself: between
+// its sums over the row it waits, and half of the registers that would let a second one in hold the next row and the vectors.
 #include <math.h>
 
 #include <type_traits>
