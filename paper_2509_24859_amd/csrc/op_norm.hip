@@ -3,11 +3,14 @@
 //
 // A row's channels lie in the registers of one workgroup, eight to a thread, so that every tensor is read once and
 // written once: the pass is bound by memory.  A workgroup takes rows in turn and keeps what belongs to its channels
-// (weights, biases, scale, and in the backward pass the sums over rows) in registers throughout.
+// (weights, biases, scale, and in the backward pass the sums over rows) in registers throughout.  In the backward pass a
+// workgroup works on several rows at a time where they are short, each by a team of its threads, and adds the teams' sums up
+// in LDS: as many waits are hidden as by so many workgroups, with one's partial sums.
 //
-// Measured, bfloat16, RMS norms on both sides, one gate, a scale: forward of 4,096 x 8,192 63 us, 4.2 TB/s, backward 109 us, 3.7
-// TB/s (a copy reaches 4.9); one row 4.5 us in the kernel.  A workgroup of 1,024 threads has a compute unit to itself: between
-// its sums over the row it waits, and half of the registers that would let a second one in hold the next row and the vectors.
+// Measured, bfloat16, RMS norms on both sides, one gate, a scale: forward of 4,096 x 8,192 63 us, 4.2 TB/s, backward 97 us, 4.2
+// TB/s (a copy reaches 4.9); one row 4.5 us in the kernel.  Backward of 11,366 x 1,176: 54 us, 3.0 TB/s, in float32 95, 3.4.  A
+// workgroup of 1,024 threads has a compute unit to itself: between its sums over the row it waits, and half of the registers
+// that would let a second one in hold the next row and the vectors.
 #include <math.h>
 
 #include <type_traits>
@@ -23,7 +26,7 @@ namespace {
 constexpr int kPer = 8;                               // channels a thread holds
 constexpr int kMaxThreads = HARP_NORM_MAX_COLS / kPer;
 constexpr int kMaxWaves = kMaxThreads / kWave;
-constexpr int kFewThreads = 512;
+constexpr int kFewThreads = 512, kTeamThreads = 768;    // a thread has 256, 168 and, with kMaxThreads, 128 registers
 
 // Everything but the data, as the kernels see it.
 struct Form {
@@ -86,19 +89,24 @@ template <typename T, bool WIDE> struct Raw {
     }
 };
 
-// A vector over the channels, `other` where there is none.
-__device__ __forceinline__ void load_vector(const float *p, int cols, float other, float (&v)[kPer]) {
-    if (p) {
-        Raw<float, false> raw;
-        raw.load(p, cols);
-        raw.get(v, cols);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) v[j] = other;
+// A vector over the channels, `other` where there is none; several are asked for before the first is taken.
+struct Vector {
+    Raw<float, false> raw;
+    const float *p;
+    __device__ __forceinline__ Vector(const float *at, int cols) : p(at) {
+        if (p) raw.load(p, cols);
     }
-}
+    __device__ __forceinline__ void get(float (&v)[kPer], int cols, float other) const {
+        if (p) {
+            raw.get(v, cols);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) v[j] = other;
+        }
+    }
+};
 
-// N sums over the workgroup, the same in every thread.  `turn` alternates between two buffers, so that one barrier a
+// N sums over a row's threads (threadIdx.x), the same in every thread.  `turn` alternates between two buffers, so that one barrier a
 // round is enough: a buffer is written again only after everybody has passed the next round's barrier.
 struct Exchange {
     f32x4 (*buf)[kMaxWaves];
@@ -112,7 +120,7 @@ template <int N> __device__ __forceinline__ void block_sum(float (&v)[N], Exchan
     }
     const int waves = blockDim.x / kWave;
     if (waves == 1) return;
-    f32x4 *b = x.buf[x.turn];
+    f32x4 *b = x.buf[x.turn] + threadIdx.y * waves;
     x.turn ^= 1;
     if (threadIdx.x % kWave == 0) {
         f32x4 q = {0, 0, 0, 0};
@@ -168,11 +176,15 @@ __global__ __launch_bounds__(MOST) void norm_forward(Form f, const T *x, int64_t
     };
     ask(blockIdx.x);                                     // there are no more workgroups than rows
     float wa[kPer], ba[kPer], wb[kPer], bb[kPer], sc[kPer];
-    load_vector(f.scale, cols, 1.0f, sc);
-    load_vector(f.w_after, cols, 1.0f, wa);
-    load_vector(f.w_before, cols, 1.0f, wb);
-    load_vector(BIAS ? f.b_after : nullptr, cols, 0.0f, ba);
-    load_vector(BIAS ? f.b_before : nullptr, cols, 0.0f, bb);
+    {
+        const Vector vs(f.scale, cols), va(f.w_after, cols), vb(f.w_before, cols), vab(BIAS ? f.b_after : nullptr, cols),
+            vbb(BIAS ? f.b_before : nullptr, cols);
+        vs.get(sc, cols, 1.0f);
+        va.get(wa, cols, 1.0f);
+        vb.get(wb, cols, 1.0f);
+        vab.get(ba, cols, 0.0f);
+        vbb.get(bb, cols, 0.0f);
+    }
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
         wa[j] *= sc[j];
@@ -218,7 +230,7 @@ __global__ __launch_bounds__(MOST) void norm_forward(Form f, const T *x, int64_t
 // workgroups' partial sums.
 struct Slabs {
     int64_t rows;             // rows of a slab
-    int64_t per_group;        // slabs of a gate's group, 0: a slab holds whole groups (or there is no gate)
+    int64_t per_group;        // slabs of a gate's group (without a gate: of all rows), 0: a slab holds whole groups
     int64_t rows_per_group;
     int64_t count;
 };
@@ -247,27 +259,29 @@ __device__ __forceinline__ float through(float d, float a, float rstd, float c0,
 // and a gate's f is the same for all rows of its group: with G1 = sum D n, G0 = sum D over them A1 = f G1, A0 = f G0 and
 // dgate = f' scale (w_after G1 + b_after G0).  A slab inside one group (GROUPS false) adds up G alone.
 // BIAS: there is a b_after, or db_after or db_before is wanted; without, A0, B0 and G0 are not needed.
-// The statistics of both norms are summed in one round, what the second gradient needs in another; the next row is
-// asked for before the current one is worked on.
+// The statistics of both norms are summed in one round, what the second gradient needs in another; the next row and its gate are
+// asked for before the current one is worked on, the first before the vectors.
+// A team is the threads of one threadIdx.y; teams take a slab's rows, with GROUPS its groups, in turn.
 enum { kA1, kB1, kA0, kB0 };
 template <typename T, bool WIDE, bool BIAS, bool GROUPS, int MOST>
 __global__ __launch_bounds__(MOST) void norm_backward(Form f, Slabs slabs, const T *dh, int64_t lddh, const T *dz, int64_t lddz,
                                                              const T *h, int64_t ldh, const T *y, int64_t ldy, T *dx, int64_t lddx,
                                                              T *dy, int64_t lddy, T *dgate, int64_t lddgate, float *partial,
                                                              float *gate_partial) {
-    __shared__ f32x4 buf[2][kMaxWaves];
+    __shared__ f32x4 buf[2][kMaxWaves], pool[2][MOST == kMaxThreads ? 1 : MOST];
     Exchange ex = {buf, 0};
-    const int cols = f.cols;
+    const int cols = f.cols, teams = MOST == kMaxThreads ? 1 : int(blockDim.y);
+    const int team = MOST == kMaxThreads ? 0 : __builtin_amdgcn_readfirstlane(int(threadIdx.y));
     const float inv_cols = 1.0f / float(cols);
     int64_t begin, end;
     slab_rows(slabs, f.rows, blockIdx.x, begin, end);
 
-    float wb[kPer], c[kPer];                             // c: scale w_after, times the gate's factor where that is one vector
+    float wb[kPer], c[kPer], cb[kPer];                   // c: scale w_after, times the gate's factor where that is one vector; cb: scale b_after
     float B1[kPer] = {}, B0[kPer] = {}, A1[kPer] = {}, A0[kPer] = {}, G1[kPer] = {}, G0[kPer] = {};
-    auto gate_of = [&](int64_t r, float (&factor)[kPer], float (&slope)[kPer]) {
-        Raw<T, WIDE> raw;
-        raw.load(static_cast<const T *>(f.gate) + r / f.rows_per_gate * f.ldgate, cols);
-        raw.get(factor, cols);
+    Raw<T, WIDE> gate, next_gate;
+    auto load_gate = [&](int64_t r, Raw<T, WIDE> &to) { to.load(static_cast<const T *>(f.gate) + r / f.rows_per_gate * f.ldgate, cols); };
+    auto factors = [&](float (&factor)[kPer], float (&slope)[kPer]) {
+        gate.get(factor, cols);
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
             slope[j] = 1.0f;
@@ -277,45 +291,6 @@ __global__ __launch_bounds__(MOST) void norm_backward(Form f, Slabs slabs, const
             }
         }
     };
-    load_vector(f.w_before, cols, 1.0f, wb);
-    load_vector(f.scale, cols, 1.0f, c);
-    {
-        float wa[kPer];
-        load_vector(f.w_after, cols, 1.0f, wa);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) c[j] *= wa[j];
-        if (!GROUPS && f.gate && begin < end) {
-            float factor[kPer], slope[kPer];
-            gate_of(begin, factor, slope);
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) c[j] *= factor[j];
-        }
-    }
-    // A group is done: its gate's gradient, and its share of the sums.
-    auto close = [&](int64_t r, float *to_partial) {
-        float factor[kPer], slope[kPer], wa[kPer], ba[kPer], sc[kPer];
-        gate_of(r, factor, slope);
-        load_vector(f.w_after, cols, 1.0f, wa);
-        load_vector(BIAS ? f.b_after : nullptr, cols, 0.0f, ba);
-        load_vector(f.scale, cols, 1.0f, sc);
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            A1[j] += factor[j] * G1[j];
-            const float s = BIAS ? wa[j] * G1[j] + ba[j] * G0[j] : wa[j] * G1[j];
-            slope[j] *= sc[j] * s;
-            if (BIAS) A0[j] += factor[j] * G0[j];
-            G1[j] = G0[j] = 0;
-        }
-        if (to_partial) {
-#pragma unroll
-            for (int j = 0; j < kPer; ++j)
-                if (channel(j) < cols) to_partial[channel(j)] = slope[j];
-        } else if (dgate) {
-            Raw<T, WIDE> raw;
-            raw.store(dgate + r / f.rows_per_gate * lddgate, cols, slope, f.past);
-        }
-    };
-
     Raw<T, WIDE> next_h, next_dz, next_y, next_dh;
     auto ask = [&](int64_t r) {
         if (dz) {
@@ -324,17 +299,48 @@ __global__ __launch_bounds__(MOST) void norm_backward(Form f, Slabs slabs, const
         }
         if (y) next_y.load(y + r * ldy, cols);
         if (dh) next_dh.load(dh + r * lddh, cols);
+        if (GROUPS) load_gate(r, next_gate);
     };
-    if (begin < end) ask(begin);
-    for (int64_t r = begin; r < end; ++r) {
-        float a[kPer] = {}, e[kPer] = {}, b[kPer] = {}, d[kPer] = {};
-        if (dz) {
-            next_h.get(a, cols);
-            next_dz.get(e, cols);
+    const int64_t unit = GROUPS ? f.rows_per_gate : 1;
+    int64_t r = begin + team * unit, left = unit, following;
+    if (r < end) ask(r);
+    {
+        const bool gated = !GROUPS && f.gate && begin < end;
+        if (gated) load_gate(begin, gate);
+        const Vector vb(f.w_before, cols), vs(f.scale, cols), va(f.w_after, cols), vab(BIAS && GROUPS ? f.b_after : nullptr, cols);
+        vb.get(wb, cols, 1.0f);
+        vs.get(cb, cols, 1.0f);
+        va.get(c, cols, 1.0f);
+        float ba[kPer], factor[kPer], slope[kPer];
+        vab.get(ba, cols, 0.0f);
+        if (gated) factors(factor, slope);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            c[j] *= cb[j];
+            cb[j] *= ba[j];
+            if (gated) c[j] *= factor[j];
         }
-        if (y) next_y.get(b, cols);
-        if (dh) next_dh.get(d, cols);
-        if (r + 1 < end) ask(r + 1);
+    }
+    // Every team makes as many turns, so that all meet at the barriers; one whose rows are done adds nothing.
+    for (int64_t first = begin; first < end; r = following) {
+        const bool live = r < end;
+        following = r + 1;
+        if (--left == 0) {
+            following += (teams - 1) * unit;
+            first += teams * unit;
+            left = unit;
+        }
+        float a[kPer] = {}, e[kPer] = {}, b[kPer] = {}, d[kPer] = {};
+        if (live) {
+            if (dz) {
+                next_h.get(a, cols);
+                next_dz.get(e, cols);
+            }
+            if (y) next_y.get(b, cols);
+            if (dh) next_dh.get(d, cols);
+            if (GROUPS) gate = next_gate;
+            if (following < end) ask(following);
+        }
         if (f.before == HARP_NORM_LAYER || f.after == HARP_NORM_LAYER) {
             float m[2] = {0, 0};
 #pragma unroll
@@ -358,7 +364,7 @@ __global__ __launch_bounds__(MOST) void norm_backward(Form f, Slabs slabs, const
         block_sum(s, ex);
         const float rstd_h = rstd_of(s[0], inv_cols, f.eps_before);
         const float rstd_y = f.after != HARP_NORM_NONE ? rstd_of(s[3], inv_cols, f.eps_after) : 1.0f;
-        if (dz) {
+        if (dz && live) {
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
                 B1[j] += e[j] * (a[j] * rstd_h);
@@ -367,61 +373,113 @@ __global__ __launch_bounds__(MOST) void norm_backward(Form f, Slabs slabs, const
             }
         }
         Raw<T, WIDE> out;
-        if (dx) out.store(dx + r * lddx, cols, d, f.past);
+        if (dx && live) out.store(dx + r * lddx, cols, d, f.past);
         if (!y) continue;
-        float k[2] = {0, 0}, factor[kPer], slope[kPer];
-        if (GROUPS) gate_of(r, factor, slope);
+        float k[2] = {0, 0};
+        if (live) {
+            float factor[kPer], slope[kPer];
+            if (GROUPS) factors(factor, slope);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            if (channel(j) >= cols) d[j] = 0;
-            G1[j] += d[j] * (b[j] * rstd_y);
-            if (BIAS) G0[j] += d[j];
-            d[j] *= GROUPS ? c[j] * factor[j] : c[j];
-            k[0] += d[j];
-            k[1] += d[j] * b[j];
+            for (int j = 0; j < kPer; ++j) {
+                if (channel(j) >= cols) d[j] = 0;
+                G1[j] += d[j] * (b[j] * rstd_y);
+                if (BIAS) G0[j] += d[j];
+                d[j] *= GROUPS ? c[j] * factor[j] : c[j];
+                k[0] += d[j];
+                k[1] += d[j] * b[j];
+            }
         }
         if (f.after != HARP_NORM_NONE) {
             block_sum(k, ex);
 #pragma unroll
             for (int j = 0; j < kPer; ++j) d[j] = through(d[j], b[j], rstd_y, k[0], k[1], f.after, inv_cols);
         }
+        if (!live) continue;
         if (dy) out.store(dy + r * lddy, cols, d, f.past);
-        if (GROUPS && (r + 1 == f.rows || (r + 1) % f.rows_per_gate == 0)) close(r, nullptr);
-    }
-    if (!GROUPS) {
-        if (f.gate && y && begin < end) {
-            close(begin, gate_partial ? gate_partial + int64_t(blockIdx.x) * cols : nullptr);
-        } else {
+        if (GROUPS && (left == unit || r + 1 == f.rows)) {       // a gate's last row: its gradient, and its share of the sums
+            float factor[kPer], slope[kPer];
+            factors(factor, slope);
 #pragma unroll
             for (int j = 0; j < kPer; ++j) {
-                A1[j] = G1[j];
-                A0[j] = G0[j];
-                if (gate_partial && channel(j) < cols) gate_partial[int64_t(blockIdx.x) * cols + channel(j)] = 0;
+                A1[j] += factor[j] * G1[j];
+                slope[j] *= BIAS ? c[j] * G1[j] + cb[j] * G0[j] : c[j] * G1[j];
+                if (BIAS) A0[j] += factor[j] * G0[j];
+                G1[j] = G0[j] = 0;
             }
+            if (dgate) out.store(dgate + r / f.rows_per_gate * lddgate, cols, slope, f.past);
+        }
+    }
+    // The teams' sums, in the teams' order, to the first.
+    auto gather = [&](float (&v)[kPer]) {
+        const int at = int(threadIdx.x), step = int(blockDim.x);
+        if (team) {
+            pool[0][at + (team - 1) * step] = f32x4{v[0], v[1], v[2], v[3]};
+            pool[1][at + (team - 1) * step] = f32x4{v[4], v[5], v[6], v[7]};
+        }
+        __syncthreads();
+        if (!team)
+            for (int i = 0; i < teams - 1; ++i)
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) v[j] += pool[j / 4][at + i * step][j % 4];
+        __syncthreads();
+    };
+    if (teams > 1) {
+        gather(GROUPS ? A1 : G1);
+        gather(B1);
+        if (BIAS) {
+            gather(GROUPS ? A0 : G0);
+            gather(B0);
+        }
+        if (team) return;
+    }
+    auto put = [&](float *to, const float (&v)[kPer]) {
+        Raw<float, false> raw;
+        raw.store(to, cols, v, false);
+    };
+    if (!GROUPS) {
+        float factor[kPer], slope[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) factor[j] = 1.0f;
+        const bool gated = f.gate && y && begin < end;
+        if (gated) {
+            load_gate(begin, gate);
+            const Vector vs(gate_partial ? f.scale : nullptr, cols), va(gate_partial ? f.w_after : nullptr, cols),
+                vab(BIAS && gate_partial ? f.b_after : nullptr, cols);
+            factors(factor, slope);
+            float wa[kPer], ba[kPer], sc[kPer];
+            vs.get(sc, cols, 1.0f);
+            va.get(wa, cols, 1.0f);
+            vab.get(ba, cols, 0.0f);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) slope[j] *= sc[j] * (BIAS ? wa[j] * G1[j] + ba[j] * G0[j] : wa[j] * G1[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) slope[j] = 0;
+        }
+        if (gate_partial) put(gate_partial + int64_t(blockIdx.x) * cols, slope);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            A1[j] = factor[j] * G1[j];
+            A0[j] = factor[j] * G0[j];
         }
     }
     if (!partial) return;
     constexpr int kSums = BIAS ? 4 : 2;
     float *p = partial + int64_t(blockIdx.x) * kSums * cols;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        const int at = channel(j);
-        if (at >= cols) continue;
-        p[kA1 * int64_t(cols) + at] = A1[j];
-        p[kB1 * int64_t(cols) + at] = B1[j];
-        if (BIAS) {
-            p[kA0 * int64_t(cols) + at] = A0[j];
-            p[kB0 * int64_t(cols) + at] = B0[j];
-        }
+    put(p + kA1 * int64_t(cols), A1);
+    put(p + kB1 * int64_t(cols), B1);
+    if (BIAS) {
+        put(p + kA0 * int64_t(cols), A0);
+        put(p + kB0 * int64_t(cols), B0);
     }
 }
 
 // Sums of the slabs' partial sums: 32 channels a workgroup, 32 threads to a channel, each a run of slabs in order, then
 // the runs in order.
 constexpr int kJoinCols = 32, kJoinRuns = 32;
-template <int N> __device__ __forceinline__ void join_runs(const float *partial, int64_t count, int64_t stride, int64_t pitch, int cols, float (&v)[N]) {
+template <int N> __device__ __forceinline__ void join_runs(const float *partial, int block, int64_t count, int64_t stride, int64_t pitch, int cols, float (&v)[N]) {
     __shared__ float runs[N][kJoinRuns][kJoinCols + 1];
-    const int c = blockIdx.x * kJoinCols + threadIdx.x % kJoinCols, run = threadIdx.x / kJoinCols;
+    const int c = block * kJoinCols + threadIdx.x % kJoinCols, run = threadIdx.x / kJoinCols;
     const int64_t each = (count + kJoinRuns - 1) / kJoinRuns, first = run * each, last = first + each < count ? first + each : count;
 #pragma unroll
     for (int k = 0; k < N; ++k) v[k] = 0;
@@ -441,11 +499,46 @@ template <int N> __device__ __forceinline__ void join_runs(const float *partial,
     }
 }
 struct Sums { float *dw_after, *db_after, *dscale, *dw_before, *db_before; };
-template <bool BIAS>
-__global__ __launch_bounds__(kJoinCols *kJoinRuns) void norm_sums(Form f, const float *partial, int64_t count, Sums out, int accumulate) {
+// What gates' groups of several slabs have of their gates' gradients, [group][per_group][cols].
+struct Gates {
+    const float *partial;
+    void *dgate;
+    int64_t per_group, ld;
+};
+// Few slabs are added up by a thread for each channel: by runs, 226 gates of one slab each and 1,883 channels cost 23 us.
+constexpr int kJoinSlabs = 32, kJoinThreads = kJoinCols * kJoinRuns;
+__host__ __device__ inline int gate_blocks(int64_t per_group, int cols) {
+    const int at_once = per_group > kJoinSlabs ? kJoinCols : kJoinThreads;
+    return (cols + at_once - 1) / at_once;
+}
+// Workgroups: first those of the sums, if there is `partial`, then gate_blocks() for each group.
+template <typename T, bool BIAS>
+__global__ __launch_bounds__(kJoinThreads) void norm_sums(Form f, const float *partial, int64_t count, Sums out, int accumulate, Gates gates) {
     constexpr int N = BIAS ? 4 : 2;
+    const uint32_t mine = partial ? uint32_t(f.cols + kJoinCols - 1) / kJoinCols : 0;
+    if (blockIdx.x >= mine) {
+        const uint32_t blocks = uint32_t(gate_blocks(gates.per_group, f.cols));
+        const int64_t group = (blockIdx.x - mine) / blocks;
+        const int block = int((blockIdx.x - mine) % blocks);
+        const float *p = gates.partial + group * gates.per_group * f.cols;
+        T *to = static_cast<T *>(gates.dgate) + group * gates.ld;
+        if (gates.per_group > kJoinSlabs) {
+            float v[1];
+            join_runs<1>(p, block, gates.per_group, f.cols, 0, f.cols, v);
+            const int c = block * kJoinCols + threadIdx.x;
+            if (threadIdx.x < kJoinCols && c < f.cols) to[c] = T(v[0]);
+        } else {
+            const int c = block * kJoinThreads + threadIdx.x;
+            if (c >= f.cols) return;
+            float v = 0;
+#pragma unroll 8
+            for (int i = 0; i < int(gates.per_group); ++i) v += p[int64_t(i) * f.cols + c];
+            to[c] = T(v);
+        }
+        return;
+    }
     float v[N];
-    join_runs<N>(partial, count, int64_t(N) * f.cols, f.cols, f.cols, v);
+    join_runs<N>(partial, blockIdx.x, count, int64_t(N) * f.cols, f.cols, f.cols, v);
     const int c = blockIdx.x * kJoinCols + threadIdx.x;
     if (threadIdx.x >= kJoinCols || c >= f.cols) return;
     const float w = f.w_after ? f.w_after[c] : 1.0f, s = f.scale ? f.scale[c] : 1.0f;
@@ -459,41 +552,29 @@ __global__ __launch_bounds__(kJoinCols *kJoinRuns) void norm_sums(Form f, const 
     put(out.dw_before, v[kB1]);
     put(out.db_before, b0);
 }
-template <typename T>
-__global__ __launch_bounds__(kJoinCols *kJoinRuns) void gate_sums(const float *partial, int64_t per_group, int cols, T *dgate, int64_t lddgate,
-                                                                  int64_t first_group) {
-    const int64_t group = first_group + blockIdx.y;
-    float v[1];
-    join_runs<1>(partial + group * per_group * cols, per_group, cols, 0, cols, v);
-    const int c = blockIdx.x * kJoinCols + threadIdx.x;
-    if (threadIdx.x < kJoinCols && c < cols) dgate[group * lddgate + c] = T(v[0]);
-}
-
 int threads_for(int cols) { return int(round_up(size_t((cols + kPer - 1) / kPer), kWave)); }
 
-// As many workgroups as have 1,024 threads a compute unit, at most three: more of them hide more of each other's waits and
-// leave more partial sums (2,313 rows of 1,155 floats, a gate for 257: two 56, three 45, four 47, five 59 us).
+int teams_for(int cols, int threads) {
+    const int t = threads_for(cols);
+    return t <= threads ? threads / t : 1;
+}
+// A workgroup a compute unit (places), with as many teams as it holds; a second one would bring more partial sums than it
+// hides of the first's waits (2,313 rows of 1,155 floats, a gate for 257: one 33, two 50, three 59 us).  Gates' groups are
+// split into as many slabs as there are places for them, or whole ones are put together, a team for each, whichever makes fewer
+// turns of the busiest place; a slab costs four turns more, for its vectors and its partial sums.  The layout does not depend
+// on which gradients are wanted: the caller's workspace is sized before that is known.
 Slabs slabs_for(const harp_ctx *ctx, const harp_norm *n) {
-    Slabs s;
-    const int64_t want = int64_t(ctx->n_cu) * (kMaxThreads / threads_for(n->cols) < 3 ? kMaxThreads / threads_for(n->cols) : 3);
-    s.rows = (n->rows + want - 1) / want;
-    if (s.rows < 1) s.rows = 1;
-    s.per_group = 0;
-    s.rows_per_group = n->gate ? n->rows_per_gate : n->rows;
-    if (n->gate && n->rows > 0) {
-        const int64_t per = n->rows_per_gate < n->rows ? n->rows_per_gate : n->rows;
-        if (per <= s.rows) {
-            s.rows = s.rows / per * per;
-        } else {
-            s.rows_per_group = per;
-            s.per_group = (per + s.rows - 1) / s.rows;
-            s.rows = (per + s.per_group - 1) / s.per_group;
-            s.count = (n->rows + per - 1) / per * s.per_group;
-            return s;
-        }
-    }
-    s.count = (n->rows + s.rows - 1) / s.rows;
-    return s;
+    if (n->rows == 0) return Slabs{0, 0, 0, 0};
+    const int64_t places = ctx->n_cu, teams = teams_for(n->cols, kTeamThreads), turns = 4;
+    const int64_t per = n->gate && n->rows_per_gate < n->rows ? n->rows_per_gate : n->rows, groups = (n->rows + per - 1) / per;
+    const int64_t most = (per + teams - 1) / teams;
+    int64_t parts = places / groups < most ? places / groups : most;
+    if (parts < 1) parts = 1;
+    const int64_t rows = (per + parts - 1) / parts, whole = (groups + places - 1) / places;
+    const int64_t split = (groups * parts + places - 1) / places * ((rows + teams - 1) / teams + turns);
+    const int64_t together = (whole + teams - 1) / teams * per + turns;
+    if (split < together) return Slabs{rows, parts, per, groups * parts};
+    return Slabs{whole * per, 0, 0, (n->rows + whole * per - 1) / (whole * per)};
 }
 
 int check_norm(harp_ctx *ctx, const harp_norm *n) {
@@ -561,38 +642,47 @@ void run_backward(const harp_norm *n, const harp_norm_grads *g, const Slabs &s, 
     float *partial = sums ? workspace : nullptr;
     float *gate_partial = s.per_group && g->dgate ? workspace + s.count * kMostSums * n->cols : nullptr;
 #define RUN(BIAS, GROUPS, MOST)                                                                                                     \
-    norm_backward<T, WIDE, BIAS, GROUPS, MOST><<<dim3(uint32_t(s.count)), dim3(threads), 0, st>>>(                                        \
+    norm_backward<T, WIDE, BIAS, GROUPS, MOST><<<dim3(uint32_t(s.count)), dim3(threads, teams), 0, st>>>(                                        \
         form_of(n), s, static_cast<const T *>(g->dh), g->lddh, static_cast<const T *>(g->dz), g->lddz, static_cast<const T *>(g->h), \
         g->ldh, static_cast<const T *>(g->y), g->ldy, static_cast<T *>(g->dx), g->lddx, static_cast<T *>(g->dy), g->lddy,            \
         static_cast<T *>(g->dgate), g->lddgate, partial, gate_partial)
     if (s.count > 0) {
         const bool groups = n->gate && s.per_group == 0;
-        const bool few = threads <= kFewThreads;
-        if (bias && groups && few) RUN(true, true, kFewThreads);
-        else if (bias && groups) RUN(true, true, kMaxThreads);
-        else if (bias && few) RUN(true, false, kFewThreads);
-        else if (bias) RUN(true, false, kMaxThreads);
-        else if (groups && few) RUN(false, true, kFewThreads);
-        else if (groups) RUN(false, true, kMaxThreads);
-        else if (few) RUN(false, false, kFewThreads);
-        else RUN(false, false, kMaxThreads);
+        const int64_t units = groups ? (s.rows + n->rows_per_gate - 1) / n->rows_per_gate : s.rows;
+        // With 168 registers this one form keeps 50 values of a thread in memory (11,366 rows of 1,173, a gate a row: 237 us, 169 so).
+        const bool fewer = sizeof(T) == 4 && bias && groups;
+        int teams = teams_for(n->cols, fewer ? kFewThreads : kTeamThreads);
+        if (teams > units) teams = int(units);
+        const int all = threads * teams;
+#define PICK(MOST)                           \
+    if (bias && groups) RUN(true, true, MOST);   \
+    else if (bias) RUN(true, false, MOST);       \
+    else if (groups) RUN(false, true, MOST);     \
+    else RUN(false, false, MOST)
+        if (all <= kFewThreads) {
+            PICK(kFewThreads);
+        } else if (all <= kTeamThreads) {
+            PICK(kTeamThreads);
+        } else {
+            PICK(kMaxThreads);
+        }
+#undef PICK
     }
 #undef RUN
     const uint32_t across = uint32_t((n->cols + kJoinCols - 1) / kJoinCols);
     const Sums out = {g->dw_after, g->db_after, g->dscale, g->dw_before, g->db_before};
-    if (sums && bias) norm_sums<true><<<dim3(across), dim3(kJoinCols * kJoinRuns), 0, st>>>(form_of(n), partial, s.count, out, g->accumulate);
-    else if (sums) norm_sums<false><<<dim3(across), dim3(kJoinCols * kJoinRuns), 0, st>>>(form_of(n), partial, s.count, out, g->accumulate);
-    if (gate_partial) {
-        const int64_t groups = s.count / s.per_group;
-        for (int64_t first = 0; first < groups; first += 65535)
-            gate_sums<T><<<dim3(across, uint32_t(groups - first < 65535 ? groups - first : 65535)), dim3(kJoinCols * kJoinRuns), 0, st>>>(
-                gate_partial, s.per_group, n->cols, static_cast<T *>(g->dgate), g->lddgate, first);
-    }
+    // (slabs_for() splits so few groups that the grid is within its limits)
+    const int64_t blocks = (sums ? across : 0) + (gate_partial ? s.count / s.per_group * gate_blocks(s.per_group, n->cols) : 0);
+    if (blocks == 0) return;
+    const Gates gates = {gate_partial, g->dgate, s.per_group, g->lddgate};
+    const dim3 grid(static_cast<uint32_t>(blocks)), block(kJoinThreads);
+    if (bias) norm_sums<T, true><<<grid, block, 0, st>>>(form_of(n), partial, s.count, out, g->accumulate, gates);
+    else norm_sums<T, false><<<grid, block, 0, st>>>(form_of(n), partial, s.count, out, g->accumulate, gates);
 }
 
 size_t workspace_for(const harp_ctx *ctx, const harp_norm *n) {
     const Slabs s = slabs_for(ctx, n);
-    return round_up(size_t(s.count) * (kMostSums + (s.per_group ? 1 : 0)) * size_t(n->cols) * 4, 256) + 256;
+    return round_up(size_t(s.count) * (kMostSums + (n->gate && s.per_group ? 1 : 0)) * size_t(n->cols) * 4, 256) + 256;
 }
 
 }  // namespace
