@@ -558,6 +558,9 @@ int teams_for(int cols, int threads) {
     const int t = threads_for(cols);
     return t <= threads ? threads / t : 1;
 }
+// Rows of a gate's group that there are: the kernels make a turn for each.
+int64_t group_rows(const harp_norm *n) { return n->gate && n->rows_per_gate < n->rows ? n->rows_per_gate : n->rows; }
+
 // A workgroup a compute unit (places), with as many teams as it holds; a second one would bring more partial sums than it
 // hides of the first's waits (2,313 rows of 1,155 floats, a gate for 257: one 33, two 50, three 59 us).  Gates' groups are
 // split into as many slabs as there are places for them, or whole ones are put together, a team for each, whichever makes fewer
@@ -566,7 +569,7 @@ int teams_for(int cols, int threads) {
 Slabs slabs_for(const harp_ctx *ctx, const harp_norm *n) {
     if (n->rows == 0) return Slabs{0, 0, 0, 0};
     const int64_t places = ctx->n_cu, teams = teams_for(n->cols, kTeamThreads), turns = 4;
-    const int64_t per = n->gate && n->rows_per_gate < n->rows ? n->rows_per_gate : n->rows, groups = (n->rows + per - 1) / per;
+    const int64_t per = group_rows(n), groups = (n->rows + per - 1) / per;
     const int64_t most = (per + teams - 1) / teams;
     int64_t parts = places / groups < most ? places / groups : most;
     if (parts < 1) parts = 1;
@@ -611,7 +614,7 @@ int check_operands(harp_ctx *ctx, const harp_norm *n, const Operand *o, int coun
 }
 
 Form form_of(const harp_norm *n) {
-    return Form{n->rows, n->gate ? n->rows_per_gate : 1, n->ldgate, n->cols, n->after, n->before, n->gate_act, n->eps_after, n->eps_before,
+    return Form{n->rows, n->gate ? group_rows(n) : 1, n->ldgate, n->cols, n->after, n->before, n->gate_act, n->eps_after, n->eps_before,
                 n->w_after, n->b_after, n->w_before, n->b_before, n->scale, n->gate,
                 // results larger than the L2 caches: forward of 4,096 x 8,192 65.3 us through them, 63.8 past them
                 size_t(n->rows) * size_t(n->cols) * size_t(type_bytes(n->type)) >= size_t(32) << 20};
@@ -648,7 +651,7 @@ void run_backward(const harp_norm *n, const harp_norm_grads *g, const Slabs &s, 
         static_cast<T *>(g->dgate), g->lddgate, partial, gate_partial)
     if (s.count > 0) {
         const bool groups = n->gate && s.per_group == 0;
-        const int64_t units = groups ? (s.rows + n->rows_per_gate - 1) / n->rows_per_gate : s.rows;
+        const int64_t units = groups ? s.rows / group_rows(n) : s.rows;
         // With 168 registers this one form keeps 50 values of a thread in memory (11,366 rows of 1,173, a gate a row: 237 us, 169 so).
         const bool fewer = sizeof(T) == 4 && bias && groups;
         int teams = teams_for(n->cols, fewer ? kFewThreads : kTeamThreads);

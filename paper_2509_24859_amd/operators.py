@@ -328,7 +328,7 @@ def norm_workspace(ctx: Context, rows: int, cols: int, rows_per_gate: int = 0):
     """What harp_norm_backward needs for these sizes; rows_per_gate 0: no gate."""
     n = harp_norm(rows, cols, F32)
     if rows_per_gate:
-        n.gate, n.ldgate, n.rows_per_gate = 256, cols, rows_per_gate     # only whether there is a gate counts
+        n.gate, n.ldgate, n.rows_per_gate = 256, cols, rows_per_gate     # of its place only that there is one counts
     size = ctx.lib.harp_norm_workspace_bytes(ctx.handle, C.byref(n))
     if size == 0:
         raise HarpError(ERR_SHAPE, ctx.lib.harp_last_error(ctx.handle).decode())

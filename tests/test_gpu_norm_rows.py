@@ -63,3 +63,24 @@ def test_rows_at_a_time(harp, c, biases):
         whole = name in ("dx", "dy", "dgate")
         _within(value, *want[name], 300 + (0 if name in ("dx", "dy") else c["rows"]), UNIT[c["type"]] if whole else 0.0, name)
     ctx.close()
+
+
+@pytest.mark.parametrize("rows", (1, 2, 13, 300))
+def test_a_gate_for_more_rows_than_there_are(harp, rows):
+    """One gate for everything, however many rows it would be for: the same bits as for as many as there are."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    gate = torch.randn(1, 72, device="cuda")
+    dh, dz, h, y = (torch.randn(rows, 72, device="cuda") for _ in range(4))
+    got = []
+    for per in (rows, rows + 1, 2 ** 62, 2 ** 63 - 1):
+        out = [torch.full((rows, 72), -7.0, device="cuda") for _ in range(3)]
+        dgate, dscale = torch.full((1, 72), -7.0, device="cuda"), torch.full((72,), -7.0, device="cuda")
+        ops.harp_norm_forward(ctx, h, y, out[0], torch.empty_like(h), gate=gate, rows_per_gate=per)
+        ops.harp_norm_backward(ctx, dh, dz, h, y, out[1], out[2], gate=gate, rows_per_gate=per, dgate=dgate, dscale=dscale,
+                               workspace=ops.norm_workspace(ctx, rows, 72, per))
+        got.append(out + [dgate, dscale])
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+    ctx.close()
