@@ -29,8 +29,11 @@ template <> struct Mfma<_Float16> {
     static __device__ __forceinline__ f32x4 run(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
 
-// x / (1 + exp(-x)) and the like by way of the logistic function: a quotient of hardware reciprocal and exponential,
-// within a few units of 2^-24, where results are rounded to 2^-8 or 2^-11.
+// x / (1 + exp(-x)) and the like by way of the logistic function: a quotient of hardware reciprocal and exponential.
+// Every form keeps its relative accuracy where the result is small: (1 + erf(u)) / 2 is taken as erfc(-u) / 2, whose two parts
+// do not cancel below zero (1 + erff(u) is 4% off at z = -5 and 0 at z = -6).  What is left is the rounding of the
+// exponential's and erfc's arguments, up to z^2 units of 2^-24 of the result and a few more for the tanh form's cube:
+// under 2^-14 of it down to z = -8, where results of 16 bits are rounded to 2^-8 or 2^-11.
 __device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 constexpr float kTanhA = 1.5957691216057308f;             // 2 sqrt(2 / pi): (1 + tanh(u)) / 2 = logistic(2 u)
 constexpr float kTanhB = 0.044715f;
@@ -38,7 +41,7 @@ constexpr float kTanhB = 0.044715f;
 __device__ __forceinline__ float activate(float z, int act) {
     switch (act) {
         case HARP_ACT_RELU: return z > 0 ? z : z != z ? z : 0.0f;
-        case HARP_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678f));
+        case HARP_ACT_GELU: return 0.5f * z * erfcf(z * -0.70710678f);
         case HARP_ACT_GELU_TANH: return z * logistic(kTanhA * z * (1.0f + kTanhB * z * z));
         case HARP_ACT_SILU: return z * logistic(z);
         default: return z;
@@ -47,7 +50,7 @@ __device__ __forceinline__ float activate(float z, int act) {
 __device__ __forceinline__ float slope(float z, int act) {
     switch (act) {
         case HARP_ACT_RELU: return z > 0 ? 1.0f : 0.0f;
-        case HARP_ACT_GELU: return 0.5f * (1.0f + erff(z * 0.70710678f)) + z * 0.39894228f * __expf(-0.5f * z * z);
+        case HARP_ACT_GELU: return 0.5f * erfcf(z * -0.70710678f) + z * 0.39894228f * __expf(-0.5f * z * z);
         case HARP_ACT_GELU_TANH: {
             const float s = logistic(kTanhA * z * (1.0f + kTanhB * z * z));
             return s + z * s * (1.0f - s) * kTanhA * (1.0f + 3.0f * kTanhB * z * z);
