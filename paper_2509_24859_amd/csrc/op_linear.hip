@@ -52,8 +52,9 @@ __device__ __forceinline__ float slope(float z, int act) {
         case HARP_ACT_RELU: return z > 0 ? 1.0f : 0.0f;
         case HARP_ACT_GELU: return 0.5f * erfcf(z * -0.70710678f) + z * 0.39894228f * __expf(-0.5f * z * z);
         case HARP_ACT_GELU_TANH: {
-            const float s = logistic(kTanhA * z * (1.0f + kTanhB * z * z));
-            return s + z * s * (1.0f - s) * kTanhA * (1.0f + 3.0f * kTanhB * z * z);
+            // beyond 16 it is 1 or 0 in 32 bits; a z z without end would make NaN of the zero s (1 - s)
+            const float square = fminf(z * z, 256.0f), s = logistic(kTanhA * z * (1.0f + kTanhB * square));
+            return s + z * s * (1.0f - s) * kTanhA * (1.0f + 3.0f * kTanhB * square);
         }
         case HARP_ACT_SILU: {
             const float s = logistic(z);

@@ -80,3 +80,42 @@ def test_tails_of_a_slope_alone(harp, act, kind):
     ops.harp_act_grad(ctx, torch.ones_like(x), x, dz, act)
     _close(dz, np.vectorize(lambda v: _exact(v, act)[1], otypes=[float])(z), kind, "slope")
     ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("kind", ["float32", "bfloat16"])
+def test_slopes_of_huge_arguments(harp, act, kind):
+    """One above and zero below, also where the argument's square or cube is beyond 32 bits; NaN stays NaN (the derivative
+    of max(z, 0) is taken to be zero wherever z is not above zero)."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    t = getattr(torch, kind)
+    large = [100.0, 1e6, 1e13, 1e18, 5e18, 1e19, 6e19, 1e20, 1e30, 3e38]
+    z = torch.tensor([large, [-v for v in large]], dtype=t, device="cuda")
+    dz = torch.full_like(z, -7.0)
+    ops.harp_act_grad(ctx, torch.ones_like(z), z, dz, act)
+    assert (dz[0] == 1).all() and (dz[1] == 0).all(), dz.tolist()
+    z.fill_(math.nan)
+    ops.harp_act_grad(ctx, torch.ones_like(z), z, dz, act)
+    assert (dz == 0).all() if act == "relu" else torch.isnan(dz).all()
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("copies", [1, 80], ids=["few_tokens", "tiles"])
+def test_huge_arguments_in_a_product(harp, copies):
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    z = torch.tensor([[1e20] * 8, [-1e20] * 8, [3e38] * 8, [-3e38] * 8], device="cuda").bfloat16().repeat(copies, 1)
+    eye, ones = torch.eye(8, device="cuda").bfloat16(), torch.ones_like(z)
+    ws = ops.linear_workspace(ctx, z.shape[0], 8, 8)
+    for act in ("relu", "gelu", "gelu_tanh", "silu"):
+        y, dx = torch.empty_like(z), torch.empty_like(z)
+        ops.harp_linear_forward(ctx, z, eye, y, act=act, workspace=ws)
+        ops.harp_linear_grad_input(ctx, ones, eye, dx, act=act, z=z, workspace=ws)
+        assert torch.equal(y, z.clamp(min=0)), act
+        assert torch.equal(dx, (z > 0).to(dx.dtype)), act
+    ctx.close()
