@@ -241,6 +241,7 @@ class AdamW:
             a.weight_decay = get("weight_decay", 0.0)
         nbytes = ctx.lib.harp_adamw_plan_bytes(array, len(self.tensors))
         self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=ctx.device)
+        self.home = _current(ctx)           # the stream that buf is handed out again on
         h = C.c_void_p()
         ctx.check(ctx.lib.harp_adamw_plan(ctx.handle, array, len(self.tensors), self.buf.data_ptr(),
                                           self.buf.numel(), C.byref(h), _stream(ctx, stream, [self.buf])))
@@ -261,10 +262,18 @@ class AdamW:
         self.ctx.check(self.ctx.lib.harp_adamw_read_state(self.ctx.handle, self.handle, self._on_stream(stream)))
 
     def _on_stream(self, stream, *more):
-        if stream is None:
-            return _stream(self.ctx, None, ())
-        held = [x for t in self.tensors for x in t.values() if hasattr(x, "record_stream")]
-        return _stream(self.ctx, stream, [self.buf, *held, *more])
+        """The stream's handle.  On another stream than the current one, or than the one that the plan's memory comes from,
+        that memory and the tensors are recorded there: the object may be dropped before the call has run."""
+        current = _current(self.ctx)
+        handle = current if stream is None else int(stream.cuda_stream)
+        if handle != current or handle != self.home:
+            if stream is None:
+                stream = _torch().cuda.current_stream(self.ctx.device)
+            held = [x for t in self.tensors for x in t.values() if hasattr(x, "record_stream")]
+            for t in (self.buf, *held, *more):
+                if t is not None:
+                    t.record_stream(stream)
+        return handle
 
     def release(self):
         if self.handle:
