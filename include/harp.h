@@ -418,7 +418,9 @@ int harp_measure_valu_int32(harp_ctx *ctx, int32_t blocks, int32_t iters, uint32
  * leaves it out.  All sums, statistics and moments are held in 32 bits; a result of 16 bits is rounded
  * once, to the nearest, when it is stored.  Infinities and NaN go where the formulas take them.
  * Calls are asynchronous on `hip_stream`, allocate nothing, give the same bits for the same inputs on
- * every call, and can be captured in a graph.  Outputs must not overlap inputs unless stated.
+ * every call, and can be captured in a graph, whose replays repeat the call with the arguments and scalars
+ * that it was captured with (harp_adamw_plan, which waits, cannot).  Outputs must not overlap inputs
+ * unless stated.
  * ------------------------------------------------------------------------------------------------ */
 enum { HARP_F32 = 0, HARP_BF16 = 1, HARP_F16 = 2 };
 enum {
@@ -580,11 +582,14 @@ typedef struct harp_adamw harp_adamw;   /* opaque host-side view of a caller-len
 size_t harp_adamw_plan_bytes(const harp_adamw_tensor *tensors /* HOST */, int32_t n_tensors);
 /* Writes the plan (the tensors' places and how the work is split) into plan_buf, DEVICE, 256-byte aligned,
  * and waits for `hip_stream`; the tensors and the buffer must stay where they are until
- * harp_adamw_release. */
+ * harp_adamw_release.  HARP_ERR_INVALID_ARG while `hip_stream` is being captured. */
 int harp_adamw_plan(harp_ctx *ctx, const harp_adamw_tensor *tensors, int32_t n_tensors, void *plan_buf,
                     size_t plan_bytes, harp_adamw **out, void *hip_stream);
 /* For every tensor:  g = grad_scale * grad,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
- *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps). */
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps).
+ * What `hyper` holds is taken at the call, what its two pointers point to when the kernel runs: replays of a
+ * captured step all have its lr, its step's corrections and, with moments in 8 bits, its random bits, so that
+ * a program whose steps are to differ in these makes the call itself. */
 int harp_adamw_step(harp_ctx *ctx, const harp_adamw *plan, const harp_adamw_hyper *hyper, void *hip_stream);
 /* The values that the 8-bit states stand for (exact in bfloat16), into m_seen and v_seen. */
 int harp_adamw_read_state(harp_ctx *ctx, const harp_adamw *plan, void *hip_stream);

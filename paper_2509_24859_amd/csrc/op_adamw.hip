@@ -365,6 +365,14 @@ int harp_adamw_plan(harp_ctx *ctx, const harp_adamw_tensor *tensors, int32_t n_t
     if (!plan_layout(tensors, n_tensors, y, why, which)) return fail(ctx, HARP_ERR_INVALID_ARG, "tensor %d: %s", which, why);
     if (!plan_buf || !aligned(plan_buf, 256) || plan_bytes < y.bytes)
         return fail(ctx, HARP_ERR_WORKSPACE, "the plan needs %zu bytes, aligned to 256", y.bytes);
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    hipError_t e = hipSetDevice(ctx->device);
+    if (e != hipSuccess) return hip_fail(ctx, e, "hipSetDevice");
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    e = hipStreamIsCapturing(st, &capture);
+    if (e != hipSuccess) return hip_fail(ctx, e, "asking whether the stream is being captured");
+    if (capture != hipStreamCaptureStatusNone)
+        return fail(ctx, HARP_ERR_INVALID_ARG, "a plan cannot be made while the stream is being captured: it is waited for");
     harp_adamw *view = new (std::nothrow) harp_adamw;
     unsigned char *host = new (std::nothrow) unsigned char[y.bytes];
     if (!view || !host) {
@@ -400,9 +408,7 @@ int harp_adamw_plan(harp_ctx *ctx, const harp_adamw_tensor *tensors, int32_t n_t
         block += uint64_t(a.n + kBlock - 1) / kBlock;
         for (int64_t k = 0; k * kChunk < a.n; ++k) *c++ = Chunk{uint32_t(i), uint32_t(k)};
     }
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    hipError_t e = hipSetDevice(ctx->device);
-    if (e == hipSuccess) e = hipMemcpyAsync(plan_buf, host, y.bytes, hipMemcpyHostToDevice, st);
+    e = hipMemcpyAsync(plan_buf, host, y.bytes, hipMemcpyHostToDevice, st);
     if (e == hipSuccess) e = hipStreamSynchronize(st);
     delete[] host;
     if (e != hipSuccess) {

@@ -249,7 +249,8 @@ class AdamW:
 
     def step(self, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, grad_scale=None, skip=None, seed=0, stream=None):
         """One step.  grad_scale: a float32 scalar on the GPU that gradients are multiplied by; skip: an int32 one,
-        not 0 leaves everything as it is; seed: of the rounding to 8 bits, another one every step."""
+        not 0 leaves everything as it is; seed: of the rounding to 8 bits, another one every step.  In a captured graph
+        lr, step and seed are those of the capture at every replay."""
         torch = _torch()
         hyper = harp_adamw_hyper(lr, beta1, beta2, eps, step, seed & ((1 << 64) - 1),
                                  _vector(self.ctx, grad_scale, 1, torch.float32, "grad_scale"),
