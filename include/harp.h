@@ -554,7 +554,8 @@ int harp_norm_backward(harp_ctx *ctx, const harp_norm *norm, const harp_norm_gra
  * after rounding up to 3 bits of fraction, kept in 64..254 (a byte below 64 counts as 64); 255 marks a block that holds an infinity or
  * NaN and stands for NaN throughout.  A value between two codes goes up with the probability of the part
  * cut off, by a hash of hyper.seed and the element's place: moving averages whose increments are under
- * half a step would stand still otherwise.  A state of zeros is zero bytes throughout. */
+ * half a step would stand still otherwise.  A v below its first code that is not zero has that code: with
+ * zero the step of an m beside it would be m / eps.  A state of zeros is zero bytes throughout. */
 typedef struct {
     int64_t n;
     int32_t state;        /* HARP_STATE_F32 or HARP_STATE_8BIT */

@@ -136,14 +136,19 @@ __device__ __forceinline__ uint32_t block_exponent(uint32_t largest) {
     const uint32_t e = (largest + 0xFFFFFu) >> 23;
     return e < 64 ? 64 : e > 254 ? 254 : e;
 }
-// Code of a magnitude, `rnd` of 16 bits: the 20 bits below the code are cut off after rnd / 2^16 of one is added.
+// Code of a magnitude, `rnd` of 16 bits: the 20 bits below the code are cut off after rnd / 2^16 of one is added.  A v that is
+// not zero gets the smallest code at least: v begins at a thousandth of a square where the block's largest is a whole one, so
+// that an element's first v can lie below the codes while its m does not; with v zero its next step, unless a gradient as large
+// came again, would be m / eps, hundreds of lr.  The smallest code is 2^-16.5 of the block's largest gradient, the smallest of
+// m 2^-17: that step is under lr.
 __device__ __forceinline__ uint32_t encode(uint32_t bits, uint32_t exponent, int top, uint32_t rnd) {
     const uint32_t mag = bits & 0x7FFFFFFFu, field = mag >> 23;
     const uint32_t whole = (mag & 0x7FFFFFu) | (field ? 0x800000u : 0u);
     const int rel = int(field ? field : 1) - int(exponent) + top;
     const int down = 1 - rel < 31 ? 1 - rel : 31;
     const uint32_t fixed = rel >= 1 ? (uint32_t(rel - 1) << 23) + whole : whole >> down;
-    const uint32_t code = (fixed + (rnd << 4)) >> 20, most = top == kTopM ? 127 : 255;
+    const uint32_t most = top == kTopM ? 127 : 255, least = top == kTopM ? 0 : mag < 1 ? mag : 1;
+    const uint32_t code = larger((fixed + (rnd << 4)) >> 20, least);
     return exponent == 255 ? 0 : code < most ? code : most;
 }
 
