@@ -574,6 +574,7 @@ Slabs slabs_for(const harp_ctx *ctx, const harp_norm *n) {
     int64_t parts = places / groups < most ? places / groups : most;
     if (parts < 1) parts = 1;
     const int64_t rows = (per + parts - 1) / parts, whole = (groups + places - 1) / places;
+    parts = (per + rows - 1) / rows;                     // those that hold rows
     const int64_t split = (groups * parts + places - 1) / places * ((rows + teams - 1) / teams + turns);
     const int64_t together = (whole + teams - 1) / teams * per + turns;
     if (split < together) return Slabs{rows, parts, per, groups * parts};
