@@ -358,6 +358,8 @@ def harp_norm_backward(ctx: Context, dh, dz, h, y, dx, dy, after="rms", before="
     sums = dict(dw_after=dw_after, db_after=db_after, dw_before=dw_before, db_before=db_before, dscale=dscale)
     tensors = (dh, dz, h, y, dx, dy, gate, scale, w_after, b_after, w_before, b_before, dgate, workspace, *sums.values())
     n = _norm(ctx, rows, cols, dtype, after, before, eps, gate, rows_per_gate, gate_act, scale, w_after, b_after, w_before, b_before)
+    if dgate is not None and gate is None:
+        raise HarpError(ERR_INVALID_ARG, "dgate without a gate")
     g = harp_norm_grads()
     for name, t in (("dh", dh), ("dz", dz), ("h", h), ("y", y), ("dx", dx), ("dy", dy)):
         p, ld = _matrix(ctx, t, all_of, dtype, name)
