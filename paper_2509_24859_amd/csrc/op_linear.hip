@@ -173,10 +173,15 @@ __device__ __forceinline__ int swap_of(int r) { return (r & 3) << 1 | (r >> 3 & 
 
 // 16 bytes a lane, from base + off to LDS, lane after lane from `to` on (the same for the wavefront).  Written out, because
 // the compiler waits for every such load before any read of LDS that it cannot tell from the load's target; here the waits
-// are the kernel's own (vmcnt counts these loads).  There is no result register, and addresses are taken at issue.
+// are the kernel's own (vmcnt counts these loads).  There is no result register, and addresses are taken at issue.  m0 is
+// named as written so that the compiler keeps no value of its own there across the statement; that it hands m0 out to nobody
+// is what its warning, turned off here, is about.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_to_lds(const char *base, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 template <typename T> __device__ __forceinline__ uint32_t lds_address(const T *p) {
     return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void *)p));
 }
