@@ -48,7 +48,9 @@ class MlpOperator:
         n = tokens
         self.z1, self.u, self.dz1 = (torch.empty(n, f, **b) for _ in range(3))
         self.y, self.h, self.a, self.dy, self.dh, self.da = (torch.empty(n, c, **b) for _ in range(6))
-        self.ws = [ops.linear_workspace(ctx, n, f, c), ops.linear_workspace(ctx, n, c, f), ops.norm_workspace(ctx, n, c)]
+        # one workspace for all, as they run one after the other
+        self.ws = max((ops.linear_workspace(ctx, n, f, c), ops.linear_workspace(ctx, n, c, f), ops.norm_workspace(ctx, n, c)),
+                      key=lambda w: w.numel())
         self.steps = 0
         entries = []
         for k, p in self.master.items():
@@ -67,8 +69,8 @@ class MlpOperator:
     def forward(self, h, a):
         """h' and a' of the residual stream h and the normed input a; they hold until the next call."""
         ops.harp_linear_forward(self.ctx, a, self.low["w1"], self.u, bias=self.low["b1"], act="gelu_tanh", z=self.z1,
-                                workspace=self.ws[0])
-        ops.harp_linear_forward(self.ctx, self.u, self.low["w2"], self.y, bias=self.low["b2"], workspace=self.ws[1])
+                                workspace=self.ws)
+        ops.harp_linear_forward(self.ctx, self.u, self.low["w2"], self.y, bias=self.low["b2"], workspace=self.ws)
         ops.harp_norm_forward(self.ctx, h, self.y, self.h, self.a, after="rms", before="rms", scale=self.master["scale"],
                               w_after=self.master["w_after"], w_before=self.master["w_before"])
         return self.h, self.a
@@ -79,11 +81,11 @@ class MlpOperator:
         m, g = self.master, self.grad
         ops.harp_norm_backward(self.ctx, dh, da, self.h, self.y, self.dh, self.dy, after="rms", before="rms", scale=m["scale"],
                                w_after=m["w_after"], w_before=m["w_before"], dscale=g["scale"], dw_after=g["w_after"],
-                               dw_before=g["w_before"], accumulate=not first, workspace=self.ws[2])
-        ops.harp_linear_grad_weight(self.ctx, self.dy, self.u, g["w2"], dbias=g["b2"], accumulate=not first, workspace=self.ws[1])
-        ops.harp_linear_grad_input(self.ctx, self.dy, self.low["w2"], self.dz1, act="gelu_tanh", z=self.z1, workspace=self.ws[1])
-        ops.harp_linear_grad_weight(self.ctx, self.dz1, a, g["w1"], dbias=g["b1"], accumulate=not first, workspace=self.ws[0])
-        ops.harp_linear_grad_input(self.ctx, self.dz1, self.low["w1"], self.da, workspace=self.ws[0])
+                               dw_before=g["w_before"], accumulate=not first, workspace=self.ws)
+        ops.harp_linear_grad_weight(self.ctx, self.dy, self.u, g["w2"], dbias=g["b2"], accumulate=not first, workspace=self.ws)
+        ops.harp_linear_grad_input(self.ctx, self.dy, self.low["w2"], self.dz1, act="gelu_tanh", z=self.z1, workspace=self.ws)
+        ops.harp_linear_grad_weight(self.ctx, self.dz1, a, g["w1"], dbias=g["b1"], accumulate=not first, workspace=self.ws)
+        ops.harp_linear_grad_input(self.ctx, self.dz1, self.low["w1"], self.da, workspace=self.ws)
         return self.dh, self.da
 
     def step(self, lr: float):
@@ -95,6 +97,11 @@ class MlpOperator:
         count = sum(p.numel() for p in self.master.values())
         kept = 2 * self.n * (2 * self.f + 3 * self.c)                  # z1, u; y, h, a
         return count * (2 + 4 + 4 + 8 * self.bits // 32), kept, 2 * 2 * self.n * self.c
+
+    def lent(self):
+        """Bytes that the operators of a device use one after the other, however many they are: the workspace, and the
+        gradients on their way back."""
+        return sum(t.numel() * t.element_size() for t in (self.ws, self.dz1, self.dy, self.dh, self.da))
 
 
 def microseconds(call, repeat: int = 10) -> float:
@@ -148,6 +155,11 @@ def problem(forward_us: float, backward_us: float, sizes, layers: int = 80, memo
         group_ndev=np.full(2, 8, dtype=np.int32), type_mem_bytes=np.array([memory], dtype=np.int64), bw=bw)
 
 
+def planned(op: MlpOperator, forward_us: float, backward_us: float, layers: int = 80, memory=288 * GB) -> workloads.Problem:
+    """problem() of this operator on devices that have lent what its calls use in turn."""
+    return problem(forward_us, backward_us, op.bytes(), layers, memory - op.lent())
+
+
 def plan(ctx, p: workloads.Problem):
     """The best plan over both orders of the groups and all stage counts, or None."""
     orders = workloads.orderings_from_lists([(S, list(o)) for S in range(2, 17) for o in ((0, 1), (1, 0))], S_max=16)
@@ -180,9 +192,9 @@ def main():
     sizes = op.bytes()
     print("MLP operator of %d channels, %d tokens: forward %.0f us, backward %.0f us, optimizer step %.0f us"
           % (a.channels, a.tokens, forward, backward, step))
-    print("%.2f GB of weights, gradients, masters and moments (%d bits), %.2f GB kept per micro-batch, %.0f MB across a cut"
-          % (sizes[0] / 1e9, a.bits, sizes[1] / 1e9, sizes[2] / 1e6))
-    p = problem(forward, backward, sizes, a.layers)
+    print("%.2f GB of weights, gradients, masters and moments (%d bits), %.2f GB kept per micro-batch, %.0f MB across a cut, "
+          "%.2f GB lent by the device" % (sizes[0] / 1e9, a.bits, sizes[1] / 1e9, sizes[2] / 1e6, op.lent() / 1e9))
+    p = planned(op, forward, backward, a.layers)
     print("plan of %d layers on 2 x 8 GPUs: %s" % (a.layers, plan(ctx, p) or "none fits"))
     ctx.close()
 
