@@ -161,10 +161,10 @@ __device__ __forceinline__ float center(float (&v)[kPer], int kind, int cols, fl
     return rstd_of(s[0], inv_cols, eps);
 }
 
-// BIAS: there is a b_after or b_before.  MOST: threads of a workgroup at most; up to 512 of them a thread has 256 registers,
-// with 1,024 it has 128, and what does not fit goes through memory, row by row.
-template <typename T, bool WIDE, bool BIAS, int MOST>
-__global__ __launch_bounds__(MOST) void norm_forward(Form f, const T *x, int64_t ldx, const T *y, int64_t ldy, T *h,
+// BIAS: there is a b_after or b_before.  A thread has the 128 registers that workgroups of 1,024 threads leave it and needs 71 to
+// 128 of them, whatever the type and alignment: short rows are no reason for a variant of fewer threads.
+template <typename T, bool WIDE, bool BIAS>
+__global__ __launch_bounds__(kMaxThreads) void norm_forward(Form f, const T *x, int64_t ldx, const T *y, int64_t ldy, T *h,
                                                             int64_t ldh, T *z, int64_t ldz) {
     __shared__ f32x4 buf[2][kMaxWaves];
     Exchange ex = {buf, 0};
@@ -627,12 +627,9 @@ void run_forward(const harp_ctx *ctx, const harp_norm *n, const void *x, int64_t
     const int threads = threads_for(n->cols);
     const int64_t most = int64_t(ctx->n_cu) * (2048 / threads < 16 ? 2048 / threads : 16);
     const dim3 grid(uint32_t(n->rows < most ? n->rows : most)), block(threads);
-#define RUN(BIAS, MOST) norm_forward<T, WIDE, BIAS, MOST><<<grid, block, 0, st>>>(form_of(n), static_cast<const T *>(x), ldx, static_cast<const T *>(y), ldy, static_cast<T *>(h), ldh, static_cast<T *>(z), ldz)
-    const bool bias = n->b_after || n->b_before;
-    if (bias && threads <= kFewThreads) RUN(true, kFewThreads);
-    else if (bias) RUN(true, kMaxThreads);
-    else if (threads <= kFewThreads) RUN(false, kFewThreads);
-    else RUN(false, kMaxThreads);
+#define RUN(BIAS) norm_forward<T, WIDE, BIAS><<<grid, block, 0, st>>>(form_of(n), static_cast<const T *>(x), ldx, static_cast<const T *>(y), ldy, static_cast<T *>(h), ldh, static_cast<T *>(z), ldz)
+    if (n->b_after || n->b_before) RUN(true);
+    else RUN(false);
 #undef RUN
 }
 
