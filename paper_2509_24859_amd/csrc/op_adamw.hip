@@ -3,8 +3,8 @@
 // Nothing is reused and nothing is summed over the tensors, so the step is bound by what it streams: 28 bytes a
 // parameter with moments in 32 bits (gradient 2, master, m and v 4 + 4 each, copy 2), 16 with moments in 8.
 //
-// Measured, bfloat16 gradients and copies: 201 million parameters of 10 tensors 1,068 us, 5.3 TB/s (a copy reaches 4.9); 50 million with
-// moments in 8 bits 213 us, 3.8 TB/s: decoding, two hashes and encoding are some 400 vector instructions for four elements;
+// Measured, bfloat16 gradients and copies: 201 million parameters of 10 tensors 1,065 us, 5.3 TB/s (a copy reaches 4.9); 50 million with
+// moments in 8 bits 218 us, 3.7 TB/s: decoding, two hashes and encoding are some 400 vector instructions for four elements;
 // 400 tensors of 1,400 elements on average 9 us.
 #include <math.h>
 #include <string.h>

@@ -292,9 +292,10 @@ __device__ __forceinline__ void tile_of(int id, int tiles_p, int tiles_q, int &t
 
 // Measured: X [4096][4096], W [16384][4096], bfloat16, bias, tanh GELU, Z kept: 478 us, 1,150 TFLOP/s (a plain library product
 // of these sizes reaches 1,517); the gradients of X [4096][16384], W [4096][16384] through GELU, weights' added to 32 bits:
-// 1,010 us with the bias's, 1,090.  Matrix units are busy 51 to 61% of the cycles.  What bounds it: bringing the operands into
+// 1,021 us with the bias's, 1,080.  Matrix units are busy 51 to 61% of the cycles.  What bounds it: bringing the operands into
 // LDS (20%: with the loads taken out of the loop the probe ran 376 us of 472) and the epilogue, in which every compute unit
-// stores and reads at once while none multiplies (11%).  Tiles of 256 x 256 read each operand least; two workgroups a compute
+// stores and reads at once while none multiplies (11%; its code, some 50 KB straight for one activation, is part of that, how
+// much has not been told apart).  Tiles of 256 x 256 read each operand least; two workgroups a compute
 // unit with 256 x 128, which would cover each other's epilogues, need half as much again from L2 and took 632 us of 433; four
 // wavefronts of 128 x 128 each, which would read LDS a third less, 544: one to a SIMD, they wait at every barrier.
 // WP x WQ wavefronts, each a part of BP / WP x BQ / WQ of the tile.  With `partial` the sums of blockIdx.y's share of r go
@@ -788,7 +789,8 @@ void launch_product(const harp_ctx *ctx, Given a, Given b, int64_t P, int64_t Q,
     const Plan plan = plan_for(ctx, e.kind, P, Q, R);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     // Compute units finish their tiles together; what they then store at once has to leave the L2 caches of 32 MiB at the
-    // fabric's pace.  Past the caches the gradients of 4,096 tokens take 1,010 us where they took 1,033.
+    // fabric's pace.  Past the caches the gradients of 4,096 tokens take 1,010 us where they took 1,033; the
+    // products that read such results next pay some of it back (an MLP of 4,096 channels and tokens forward 960 us for 966).
     e.past = size_t(P) * size_t(Q) * (e.out_f32 ? 4 : 2) >= size_t(32) << 20;
     if (!plan.few) {
         a = packed<T>(a, ws, st);

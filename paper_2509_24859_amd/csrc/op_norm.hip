@@ -7,7 +7,7 @@
 // workgroup works on several rows at a time where they are short, each by a team of its threads, and adds the teams' sums up
 // in LDS: as many waits are hidden as by so many workgroups, with one's partial sums.
 //
-// Measured, bfloat16, RMS norms on both sides, one gate, a scale: forward of 4,096 x 8,192 63 us, 4.2 TB/s, backward 97 us, 4.2
+// Measured, bfloat16, RMS norms on both sides, one gate, a scale: forward of 4,096 x 8,192 63 us, 4.2 TB/s, backward 97 us, 4.1
 // TB/s (a copy reaches 4.9); one row 4.5 us in the kernel.  Backward of 11,366 x 1,176: 54 us, 3.0 TB/s, in float32 95, 3.4.  A
 // workgroup of 1,024 threads has a compute unit to itself: between its sums over the row it waits, and half of the registers
 // that would let a second one in hold the next row and the vectors.
