@@ -412,6 +412,9 @@ int harp_measure_valu_int32(harp_ctx *ctx, int32_t blocks, int32_t iters, uint32
  *   harp_norm_*     the norm after a block, its gate and residual scale, the residual sum, the norm
  *                   before the next block, and their gradients
  *   harp_adamw_*    one AdamW step over many tensors, with moments in 32 bits or in 8
+ * and those of its attention operator and of a gated MLP:
+ *   harp_rotary*    rotary positions of queries and keys, and their gradients
+ *   harp_gated_*    two projections, an activation and a product, and the way back through them
  *
  * Matrices are row-major; a leading dimension (ld) is the distance between rows in elements, at least
  * the number of columns.  Pointers inside the structs are DEVICE; a NULL pointer to something optional
@@ -595,6 +598,87 @@ int harp_adamw_step(harp_ctx *ctx, const harp_adamw *plan, const harp_adamw_hype
 /* The values that the 8-bit states stand for (exact in bfloat16), into m_seen and v_seen. */
 int harp_adamw_read_state(harp_ctx *ctx, const harp_adamw *plan, void *hip_stream);
 void harp_adamw_release(harp_adamw *plan);
+
+/* Rotary positions.  A head's first `turned` channels are pairs (a, b) of channels i and i + turned / 2 (HARP_ROTARY_HALF) or
+ * 2 i and 2 i + 1 (HARP_ROTARY_INTERLEAVED); of token t at position p, pair i becomes
+ *   a' = magnitude (a cos(p f_i) - b sin(p f_i)),   b' = magnitude (b cos(p f_i) + a sin(p f_i)),
+ * its other channels stay.  inverse not 0: the angle the other way round, which is the gradient of that.
+ * X and Y of `type` (any), element (t, h, c) at t * token + h * step + c; Y may be X (then with the same distances).  positions:
+ * p of every token, or NULL: first + t, with period > 0 first + t % period.  frequency: f_i, radians per position; angles are
+ * taken in 64 bits, so that they are as exact at position 10^6 as at 1.  Y's elements must not overlap one another; in X a
+ * distance may be 0.
+ * 0 <= tokens < 2^31, 1 <= heads < 2^16, 2 <= turned <= head < 2^16, turned even. */
+enum { HARP_ROTARY_HALF = 0, HARP_ROTARY_INTERLEAVED = 1 };
+typedef struct {
+    int64_t tokens;
+    int32_t heads, head, turned;
+    int32_t type, layout, inverse;
+    float magnitude;
+    const void *X;
+    int64_t x_token, x_step;
+    void *Y;
+    int64_t y_token, y_step;
+    const double *frequency;  /* DEVICE [turned / 2] */
+    const int64_t *positions; /* DEVICE [tokens] or NULL */
+    int64_t first, period;
+} harp_rotary_args;
+int harp_rotary(harp_ctx *ctx, const harp_rotary_args *args, void *hip_stream);
+
+/* The frequencies of `turned` channels, base^(-2 i / turned), and what they become where contexts are longer than those
+ * trained on, by `factor` >= 1:
+ *   LINEAR    f / factor
+ *   NTK       the base times factor^(turned / (turned - 2)): the last pair as LINEAR, the first as it was
+ *   BY_PARTS  f ((1 - g) / factor + g), g = (r - low) / (high - low) kept in 0 .. 1, r = original f / (2 pi): pairs that turn more
+ *             than `high` times in `original` positions stay, those of fewer than `low` turns are as LINEAR; magnitude
+ *             0.1 ln(factor) + 1 (else 1)
+ * frequency: HOST [turned / 2]; magnitude: HOST, or NULL.  Host code: no device is touched. */
+enum { HARP_SCALING_NONE = 0, HARP_SCALING_LINEAR = 1, HARP_SCALING_NTK = 2, HARP_SCALING_BY_PARTS = 3 };
+int harp_rotary_frequencies(int32_t turned, double base, int32_t scaling, double factor, double original, double low,
+                            double high, double *frequency, float *magnitude);
+
+/* The first half of a gated MLP block:  Z = X W^T + bias,  H = act(Z's first F columns) * Z's last F columns.
+ * X [M][K], W [2 F][K]: rows 0 .. F - 1 make the gate, the others what it is multiplied with; bias [2 F], H [M][F], Z [M][2 F], all of
+ * `type`, HARP_BF16 or HARP_F16.  Z NULL: not stored (the backward pass wants it).  H is taken of Z before it is rounded.
+ * 0 <= M < 2^31, 1 <= F, K < 2^21. */
+typedef struct {
+    int64_t M, F, K;
+    int32_t type, act;
+    const void *X;
+    int64_t ldx;
+    const void *W;
+    int64_t ldw;
+    const void *bias;
+    void *H;
+    int64_t ldh;
+    void *Z;
+    int64_t ldz;
+} harp_gated;
+/* Bytes of DEVICE workspace, 256-byte aligned, that harp_gated_forward (X [M][K]) and harp_gated_grad (dY [M][K]) need, whatever
+ * the strides and alignment (0 on sizes out of range). */
+size_t harp_gated_workspace_bytes(harp_ctx *ctx, int64_t M, int64_t F, int64_t K);
+int harp_gated_forward(harp_ctx *ctx, const harp_gated *args, void *workspace, size_t workspace_bytes,
+                       void *hip_stream);
+/* The way back through the product behind the block, Y = H W^T with W [N][F], and through the gate:
+ *   dH = dY W,   dZ's first F columns = dH * Z's last F * act'(Z's first F),   its last F = dH * act(Z's first F)
+ * and H again, for that product's weight gradient, so that it need not be kept (H NULL: not wanted).  W NULL: dY [M][F] is dH (N
+ * unused).  Then harp_linear_grad_input and harp_linear_grad_weight of dZ with the block's W [2 F][K] and X give the rest.
+ * dY [M][N], Z and dZ [M][2 F], H [M][F] of `type`; dZ may be Z. */
+typedef struct {
+    int64_t M, F, N;
+    int32_t type, act;
+    const void *dY;
+    int64_t lddy;
+    const void *W;
+    int64_t ldw;
+    const void *Z;
+    int64_t ldz;
+    void *dZ;
+    int64_t lddz;
+    void *H;
+    int64_t ldh;
+} harp_gated_grads;
+int harp_gated_grad(harp_ctx *ctx, const harp_gated_grads *args, void *workspace, size_t workspace_bytes,
+                    void *hip_stream);
 
 #ifdef __cplusplus
 }

@@ -35,6 +35,8 @@ EXPORTS = (
     "harp_linear_workspace_bytes", "harp_linear_forward", "harp_linear_grad_input", "harp_linear_grad_weight", "harp_act_grad",
     "harp_adamw_plan_bytes", "harp_adamw_plan", "harp_adamw_step", "harp_adamw_read_state", "harp_adamw_release",
     "harp_norm_forward", "harp_norm_workspace_bytes", "harp_norm_backward",
+    "harp_rotary", "harp_rotary_frequencies",
+    "harp_gated_workspace_bytes", "harp_gated_forward", "harp_gated_grad",
 )
 
 
@@ -146,6 +148,13 @@ def load_library() -> C.CDLL:
     lib.harp_norm_workspace_bytes.argtypes = [vp, vp]
     lib.harp_norm_workspace_bytes.restype = sz
     lib.harp_norm_backward.argtypes = [vp, vp, vp, vp, sz, vp]
+    f64 = C.c_double
+    lib.harp_rotary.argtypes = [vp, vp, vp]
+    lib.harp_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp, vp]
+    lib.harp_gated_workspace_bytes.argtypes = [vp, i64, i64, i64]
+    lib.harp_gated_workspace_bytes.restype = sz
+    for name in ("harp_gated_forward", "harp_gated_grad"):
+        getattr(lib, name).argtypes = [vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 

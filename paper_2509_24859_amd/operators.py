@@ -15,9 +15,13 @@ STATE_F32, STATE_8BIT = 32, 8
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
 NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 GATE_LINEAR, GATE_SIGMOID = 0, 1
+ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
+SCALING_NONE, SCALING_LINEAR, SCALING_NTK, SCALING_BY_PARTS = range(4)
 NORM_MAX_COLS = 8192
 _ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 _NORMS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
+_LAYOUTS = {"half": ROTARY_HALF, "interleaved": ROTARY_INTERLEAVED}
+_SCALINGS = {"none": SCALING_NONE, "linear": SCALING_LINEAR, "ntk": SCALING_NTK, "by_parts": SCALING_BY_PARTS}
 _GATES = {"none": GATE_LINEAR, "linear": GATE_LINEAR, "sigmoid": GATE_SIGMOID}
 ADAMW_BLOCK = 256           # elements that share an exponent in an 8-bit state
 
@@ -370,3 +374,99 @@ def harp_norm_backward(ctx: Context, dh, dz, h, y, dx, dy, after="rms", before="
         setattr(g, name, _vector(ctx, t, cols, f32, name))
     g.accumulate = int(bool(accumulate))
     ctx.check(ctx.lib.harp_norm_backward(ctx.handle, C.byref(n), C.byref(g), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))
+
+
+def _heads(ctx, t, shape, dtype, name):
+    """(address, distance of tokens, distance of heads) of [tokens][heads][head] whose channels are contiguous; for None (None, 0, 0)."""
+    if t is None:
+        return None, 0, 0
+    if t.get_device() != ctx.index:
+        raise _elsewhere(ctx, t, name)
+    if t.dtype is not dtype or t.shape != shape:
+        raise HarpError(ERR_SHAPE, "%s: %s of %s is wanted, got %s of %s" % (name, tuple(shape), dtype, tuple(t.shape), t.dtype))
+    token, step, channel = t.stride()
+    if channel != 1 and shape[2] > 1:
+        raise HarpError(ERR_SHAPE, "%s: channels must be contiguous, its strides are %s" % (name, (token, step, channel)))
+    return t.data_ptr(), token, step
+
+
+def _three(t, name):
+    if t.dim() != 3:
+        raise HarpError(ERR_SHAPE, "%s must be [tokens][heads][head]" % name)
+
+
+class harp_rotary_args(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("heads", C.c_int32), ("head", C.c_int32), ("turned", C.c_int32), ("type", C.c_int32),
+                ("layout", C.c_int32), ("inverse", C.c_int32), ("magnitude", C.c_float), ("X", C.c_void_p), ("x_token", C.c_int64),
+                ("x_step", C.c_int64), ("Y", C.c_void_p), ("y_token", C.c_int64), ("y_step", C.c_int64), ("frequency", C.c_void_p),
+                ("positions", C.c_void_p), ("first", C.c_int64), ("period", C.c_int64)]
+
+
+def rotary_frequencies(ctx: Context, turned: int, base=10000.0, scaling="none", factor=1.0, original=0.0, low=1.0, high=32.0):
+    """(float64 [turned / 2] on the GPU, magnitude) for harp_rotary; see harp_rotary_frequencies in include/harp.h."""
+    out, magnitude = (C.c_double * max(turned // 2, 1))(), C.c_float()
+    rc = ctx.lib.harp_rotary_frequencies(turned, base, _named(scaling, _SCALINGS), factor, original, low, high, out, C.byref(magnitude))
+    if rc:
+        raise HarpError(rc, "frequencies of %s channels: base %s, scaling %s by %s, original %s, low %s, high %s"
+                        % (turned, base, scaling, factor, original, low, high))
+    return _torch().tensor(list(out), dtype=_torch().float64).to(ctx.device), magnitude.value
+
+
+def harp_rotary(ctx: Context, x, y, frequencies, positions=None, first=0, period=0, layout="half", magnitude=1.0, inverse=False, stream=None):
+    """y = x [tokens][heads][head] with its first 2 * len(frequencies) channels turned; see include/harp.h.  y may be x.
+    positions: int64 [tokens], or None: first + t, or first + t % period."""
+    _three(x, "x")
+    shape, torch = x.shape, _torch()
+    turned = 2 * frequencies.numel()
+    a = harp_rotary_args(shape[0], shape[1], shape[2], turned, _type(x), _named(layout, _LAYOUTS), int(bool(inverse)), magnitude,
+                         *_heads(ctx, x, shape, x.dtype, "x"), *_heads(ctx, y, shape, x.dtype, "y"),
+                         _vector(ctx, frequencies, turned // 2, torch.float64, "frequencies"),
+                         _vector(ctx, positions, shape[0], torch.int64, "positions"), first, period)
+    ctx.check(ctx.lib.harp_rotary(ctx.handle, C.byref(a), _stream(ctx, stream, (x, y, frequencies, positions))))
+
+
+class harp_gated(C.Structure):
+    _fields_ = [("M", C.c_int64), ("F", C.c_int64), ("K", C.c_int64), ("type", C.c_int32), ("act", C.c_int32), ("X", C.c_void_p),
+                ("ldx", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64), ("bias", C.c_void_p), ("H", C.c_void_p), ("ldh", C.c_int64),
+                ("Z", C.c_void_p), ("ldz", C.c_int64)]
+
+
+class harp_gated_grads(C.Structure):
+    _fields_ = [("M", C.c_int64), ("F", C.c_int64), ("N", C.c_int64), ("type", C.c_int32), ("act", C.c_int32), ("dY", C.c_void_p),
+                ("lddy", C.c_int64), ("W", C.c_void_p), ("ldw", C.c_int64), ("Z", C.c_void_p), ("ldz", C.c_int64), ("dZ", C.c_void_p),
+                ("lddz", C.c_int64), ("H", C.c_void_p), ("ldh", C.c_int64)]
+
+
+def gated_workspace(ctx: Context, tokens: int, width: int, channels: int):
+    """What harp_gated_forward (x [tokens][channels], w [2 width][channels]) and harp_gated_grad (dy [tokens][channels],
+    w [channels][width]) need."""
+    size = ctx.lib.harp_gated_workspace_bytes(ctx.handle, tokens, width, channels)
+    if size == 0:
+        raise HarpError(ERR_SHAPE, "sizes out of range: %s tokens, width %s, %s channels" % (tokens, width, channels))
+    return _torch().empty(size, dtype=_torch().uint8, device=ctx.device)
+
+
+def harp_gated_forward(ctx: Context, x, w, h, bias=None, act="silu", z=None, workspace=None, stream=None):
+    """Z = x w^T + bias,  h = act(Z's first half) * Z's second half; see include/harp.h.  w: [2 width][channels], the gate's rows
+    first; z: receives Z, or None."""
+    _two(x, w, "x", "w")
+    (m, k), t = x.shape, x.dtype
+    if w.shape[0] % 2:
+        raise HarpError(ERR_SHAPE, "w has an odd number of rows, %d" % w.shape[0])
+    f = w.shape[0] // 2
+    tensors = (x, w, h, bias, z, workspace)
+    a = harp_gated(m, f, k, _type(x, (BF16, F16)), _named(act, _ACTS), *_matrix(ctx, x, (m, k), t, "x"), *_matrix(ctx, w, (2 * f, k), t, "w"),
+                   _vector(ctx, bias, 2 * f, t, "bias"), *_matrix(ctx, h, (m, f), t, "h"), *_matrix(ctx, z, (m, 2 * f), t, "z"))
+    ctx.check(ctx.lib.harp_gated_forward(ctx.handle, C.byref(a), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))
+
+
+def harp_gated_grad(ctx: Context, dy, w, z, dz, act="silu", h=None, workspace=None, stream=None):
+    """dH = dy w (w [outputs][width], or None: dy is dH),  dz = dH back through the gate,  h = act(gate) * up again; see include/harp.h."""
+    _two(dy, z, "dy", "z")
+    (m, n), f, t = dy.shape, z.shape[1] // 2, dy.dtype
+    n = f if w is None else n
+    tensors = (dy, w, z, dz, h, workspace)
+    a = harp_gated_grads(m, f, n, _type(dy, (BF16, F16)), _named(act, _ACTS), *_matrix(ctx, dy, (m, n), t, "dy"),
+                         *_matrix(ctx, w, (n, f), t, "w"), *_matrix(ctx, z, (m, 2 * f), t, "z"), *_matrix(ctx, dz, (m, 2 * f), t, "dz"),
+                         *_matrix(ctx, h, (m, f), t, "h"))
+    ctx.check(ctx.lib.harp_gated_grad(ctx.handle, C.byref(a), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))

@@ -1,0 +1,164 @@
+"""Rotary positions against their formula in 64 bits, and what the call refuses.
+
+Tolerances.  The angle in turns is exact to 2^-30 (positions to 2^22), rounded once to 32 bits (at most half a turn: 2^-26), which
+moves cosine and sine by 2 pi 2^-26 < 2^-23; the functions add 4 units of 2^-24, the magnitude one.  A result is a sum of two
+products: under 16 roundings of 2^-24 of |a| + |b| times the magnitude, and half a unit of its own last place when it is stored,
+2^-8, 2^-11 or 2^-24 of it, in float16 at least 2^-25.
+"""
+import math
+
+import numpy as np
+import pytest
+
+from operator_context import HostContext, refused
+
+HALF = {"bfloat16": 2.0 ** -8, "float16": 2.0 ** -11, "float32": 2.0 ** -24}
+
+
+def _want(x, f, p, layout, magnitude, inverse):
+    """(turned x, room without the last rounding) in 64 bits."""
+    r = 2 * len(f)
+    angle = (np.asarray(p, dtype=np.float64)[:, None] * f[None, :])[:, None, :] * (-1 if inverse else 1)
+    c, s = magnitude * np.cos(angle), magnitude * np.sin(angle)
+    first, second = (slice(0, r // 2), slice(r // 2, r)) if layout == "half" else (slice(0, r, 2), slice(1, r, 2))
+    a, b, y, room = x[..., first], x[..., second], x.copy(), np.zeros_like(x)
+    y[..., first], y[..., second] = a * c - b * s, b * c + a * s
+    room[..., first] = room[..., second] = (np.abs(a) + np.abs(b)) * abs(magnitude) * 16 * 2.0 ** -24
+    return y, room
+
+
+# tokens, heads, head, turned
+SIZES = [(1, 1, 2, 2), (1, 72, 128, 128), (2, 3, 64, 32), (5, 7, 80, 80), (7, 1, 96, 72), (33, 12, 96, 10), (64, 8, 256, 256),
+         (129, 5, 33, 30), (300, 9, 128, 128), (2048, 40, 128, 64), (4099, 2, 20, 18)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("size", SIZES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("kind", ["bfloat16", "float16", "float32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("where", ["apart", "in place", "odd strides", "heads first"])
+def test_formula(harp, size, kind, layout, where):
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    (n, h, d, r), t = size, getattr(torch, kind)
+    rng = np.random.default_rng(n * 31 + h * 7 + d)
+    ctx = harp.Context(0)
+    f, _ = ops.rotary_frequencies(ctx, r, scaling="by_parts", factor=8.0, original=4096.0)
+    inverse, magnitude = bool(n % 2), 1.25
+    x = torch.from_numpy(rng.standard_normal((n, h, d))).to(t)
+    p = torch.from_numpy(rng.integers(0, 1 << 20, n))
+    lead, pad = (1, 3) if where == "odd strides" else (0, 0)
+
+    def put(values):
+        if where == "heads first":
+            buf = torch.full((h, n, d), -7.0, dtype=t, device="cuda")
+            view = buf.transpose(0, 1)
+        else:
+            buf = torch.full((lead + n * (h * d + pad),), -7.0, dtype=t, device="cuda")
+            view = buf[lead:].view(n, h * d + pad)[:, :h * d].unflatten(1, (h, d))
+        if values is not None:
+            view.copy_(values)
+        return buf, view
+
+    _, gx = put(x)
+    buf, gy = (None, gx) if where == "in place" else put(None)
+    ops.harp_rotary(ctx, gx, gy, f, positions=p.cuda(), layout=layout, magnitude=magnitude, inverse=inverse)
+    got = gy.double().cpu().numpy()
+    want, room = _want(x.double().numpy(), f.cpu().numpy(), p.numpy(), layout, magnitude, inverse)
+    off = np.abs(got - want)
+    half = HALF[kind] * (np.abs(want) + room) + (2.0 ** -25 if kind == "float16" else 0)
+    assert (off <= room + half).all(), (off - room - half).max()
+    assert (got[..., r:] == x.double().numpy()[..., r:]).all()
+    if where == "odd strides":               # nothing between and before is written
+        assert (buf[:1] == -7).all() and (buf[1:].view(n, h * d + pad)[:, h * d:] == -7).all()
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_positions_by_rule_far_away_and_below_zero(harp):
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    f, _ = ops.rotary_frequencies(ctx, 64)
+    x = torch.randn(50, 2, 64, device="cuda")
+    for first, period, p in ((0, 0, range(50)), (4000000, 0, range(4000000, 4000050)), (7, 20, [7 + t % 20 for t in range(50)]),
+                             (-49, 0, range(-49, 1))):
+        y = torch.empty_like(x)
+        ops.harp_rotary(ctx, x, y, f, first=first, period=period)
+        want, room = _want(x.double().cpu().numpy(), f.cpu().numpy(), list(p), "half", 1.0, False)
+        assert (np.abs(y.double().cpu().numpy() - want) <= room + 2.0 ** -24 * (np.abs(want) + room)).all(), (first, period)
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_its_gradient_by_differences_and_back_again(harp):
+    """The inverse is the transposed map: <R x, g> = <x, R' g>; turned there and back every value is its own again, to the 16
+    roundings of each way."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    f, _ = ops.rotary_frequencies(ctx, 24)
+    x, g = torch.randn(9, 3, 32, device="cuda"), torch.randn(9, 3, 32, device="cuda")
+    y, dx, back = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+    for layout in ("half", "interleaved"):
+        ops.harp_rotary(ctx, x, y, f, first=100, layout=layout, magnitude=1.5)
+        ops.harp_rotary(ctx, g, dx, f, first=100, layout=layout, magnitude=1.5, inverse=True)
+        a, b = (y.double() * g.double()).sum(), (x.double() * dx.double()).sum()
+        assert abs(a - b) <= 32 * 2.0 ** -24 * (y.double().abs() * g.double().abs()).sum() * 2
+        ops.harp_rotary(ctx, y, back, f, first=100, layout=layout, magnitude=1 / 1.5, inverse=True)
+        assert (back - x).abs().max() <= 64 * 2.0 ** -24 * x.abs().max() * 2
+        # differences: the map is linear
+        for at in ((0, 0, 0), (3, 1, 5), (8, 2, 23), (4, 0, 30)):
+            e = torch.zeros_like(x)
+            e[at] = 1
+            ops.harp_rotary(ctx, e, back, f, first=100, layout=layout, magnitude=1.5)
+            assert abs((back.double() * g.double()).sum() - dx[at].double()) <= 64 * 2.0 ** -24 * g.abs().max().item() * 2
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_other_streams_and_graphs(harp):
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    f, _ = ops.rotary_frequencies(ctx, 128)
+    x = torch.randn(700, 5, 128, device="cuda").bfloat16()
+    p = torch.arange(700, device="cuda")
+    want, y = torch.empty_like(x), torch.empty_like(x)
+    ops.harp_rotary(ctx, x, want, f, positions=p)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    ops.harp_rotary(ctx, x, y, f, positions=p, stream=side)
+    side.synchronize()
+    assert torch.equal(y, want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ops.harp_rotary(ctx, x, y, f, positions=p)
+    for shift in (0, 3, 1000):
+        p.copy_(torch.arange(700, device="cuda") + shift)
+        ops.harp_rotary(ctx, x, want, f, positions=p)
+        y.fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+    empty = x[:0]
+    ops.harp_rotary(ctx, empty, empty, f)
+    ctx.close()
+
+
+def test_refusals(monkeypatch):
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = HostContext()
+    x, f = torch.zeros(4, 3, 16), torch.ones(8, dtype=torch.float64)
+    wide = torch.zeros(4, 6, 32)
+    for a, k in (((x, torch.zeros(4, 3, 8), f), {}), ((x, x.half(), f), {}), ((x.int(), x.int(), f), {}), ((x[0], x[0], f), {}),
+                 ((x, x, torch.ones(9, dtype=torch.float64)), {}), ((x, x, f.float()), {}), ((x, x, f[::2]), {}), ((x, x, f[:0]), {}),
+                 ((x, x, f), dict(positions=torch.arange(3))), ((x, x, f), dict(positions=torch.arange(4).int())),
+                 ((x, x, f), dict(layout="quarter")), ((x, x, f), dict(layout=2)), ((x, x, f), dict(period=-1)),
+                 ((x, x[:1].expand(4, 3, 16), f), {}), ((x, torch.zeros(4, 1, 16).expand(4, 3, 16), f), {}),
+                 ((x, torch.zeros(3, 4, 16, 2)[..., 0].transpose(0, 1), f), {}), ((wide[:, :3, :16], wide.view(-1)[:192].view(4, 3, 16), f), {})):
+        refused(monkeypatch, ops.harp_rotary, ctx, *a, **k)
+    refused(monkeypatch, ops.rotary_frequencies, ctx, 7)
+    refused(monkeypatch, ops.rotary_frequencies, ctx, 8, scaling="twice")
+    assert math.isclose(ops.rotary_frequencies(ctx, 8)[0][0].item(), 1.0)
