@@ -414,6 +414,7 @@ int harp_measure_valu_int32(harp_ctx *ctx, int32_t blocks, int32_t iters, uint32
  *   harp_adamw_*    one AdamW step over many tensors, with moments in 32 bits or in 8
  * and those of its attention operator and of a gated MLP:
  *   harp_rotary*    rotary positions of queries and keys, and their gradients
+ *   harp_attention_*  softmax attention to keys of the same or of another length, and its gradients
  *   harp_gated_*    two projections, an activation and a product, and the way back through them
  *
  * Matrices are row-major; a leading dimension (ld) is the distance between rows in elements, at least
@@ -635,6 +636,54 @@ int harp_rotary(harp_ctx *ctx, const harp_rotary_args *args, void *hip_stream);
 enum { HARP_SCALING_NONE = 0, HARP_SCALING_LINEAR = 1, HARP_SCALING_NTK = 2, HARP_SCALING_BY_PARTS = 3 };
 int harp_rotary_frequencies(int32_t turned, double base, int32_t scaling, double factor, double original, double low,
                             double high, double *frequency, float *magnitude);
+
+/* Softmax attention.  Per sequence b, head h, query i and key j of the sequence's, with kv head h / (heads / kv_heads):
+ *   s_ij = scale q_i . k_j over the keys that i sees,  lse_i = log(sum of exp(s_ij)),  o_i = sum of exp(s_ij - lse_i) v_j
+ * Sequence b has queries q_begin[b] .. q_begin[b + 1] - 1 of tokens_q, and keys k_begin[b] .. k_begin[b + 1] - 1 of tokens_k, of
+ * which it uses the first k_count[b] (NULL: all).  Where a begin is NULL the sequences have tokens / batch each.  With Lq
+ * queries and Lk used keys, i sees all of them, or with causal not 0 those j <= i + Lk - Lq: the last query sees all.  A query
+ * that sees no key (or whose scores are all -infinity) has o = 0, lse = -infinity, and no part in any gradient.  Keys that are not
+ * used are not read into any result, whatever they hold.  A key or value that is not finite and hidden from a query by the causal
+ * order alone may make that query's results NaN.
+ * Q and O [tokens_q][heads][head], K and V [tokens_k][kv_heads][head], of `type` (HARP_BF16 or HARP_F16), element (t, h, c) at
+ * t * token + h * step + c.  lse: float [heads][tokens_q], or NULL in the forward pass.  scale > 0.
+ * Begins and counts are DEVICE int32, read when the kernels run, so that a captured call takes those of each replay; begins rise
+ * and end within tokens; whatever they hold, nothing outside the tensors is touched.  Rows of no sequence are left as they were.
+ * Scores, weights' sums and all sums over keys or queries are in 32 bits; weights and their gradients are rounded to `type`
+ * where they are multiplied with V, K, Q and dO (what the matrix instructions take; in HARP_F16 the gradients times a power
+ * of two that keeps them from both ends of its range).
+ * head a multiple of 8, at most HARP_ATTENTION_MAX_HEAD; heads a multiple of kv_heads, heads <= 2^14;
+ * 0 <= tokens < 2^31, tokens_q * heads / kv_heads < 2^31; 1 <= batch <= 2^20. */
+#define HARP_ATTENTION_MAX_HEAD 128
+typedef struct {
+    int64_t tokens_q, tokens_k;
+    int32_t batch, heads, kv_heads, head;
+    int32_t type, causal;
+    float scale;
+    const int32_t *q_begin, *k_begin; /* DEVICE [batch + 1] or NULL */
+    const int32_t *k_count;           /* DEVICE [batch] or NULL */
+    const void *Q, *K, *V;
+    int64_t q_token, q_step, k_token, k_step, v_token, v_step;
+    void *O;                          /* the backward pass reads it */
+    int64_t o_token, o_step;
+    float *lse;                       /* the backward pass reads it */
+} harp_attention;
+/* Bytes of DEVICE workspace, 256-byte aligned, that both passes need for these tokens, batch, heads, kv_heads and head
+ * (0 on sizes out of range). */
+size_t harp_attention_workspace_bytes(harp_ctx *ctx, const harp_attention *args);
+int harp_attention_forward(harp_ctx *ctx, const harp_attention *args, void *workspace, size_t workspace_bytes,
+                           void *hip_stream);
+/* With P = exp(s - lse) and D_i = sum over channels of dO_i O_i:  dV = P^T dO,  dS = P (dO V^T - D),  dQ = scale dS K,
+ * dK = scale dS^T Q, a kv head's gradients summed over the heads that share it.  dO and dQ like Q, dK and dV like K.  Keys of a
+ * sequence that it does not use get zeros.  All three are written (none is added to), each may be NULL: not wanted. */
+typedef struct {
+    const void *dO;
+    int64_t do_token, do_step;
+    void *dQ, *dK, *dV;
+    int64_t dq_token, dq_step, dk_token, dk_step, dv_token, dv_step;
+} harp_attention_grads;
+int harp_attention_backward(harp_ctx *ctx, const harp_attention *args, const harp_attention_grads *grads, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
 
 /* The first half of a gated MLP block:  Z = X W^T + bias,  H = act(Z's first F columns) * Z's last F columns.
  * X [M][K], W [2 F][K]: rows 0 .. F - 1 make the gate, the others what it is multiplied with; bias [2 F], H [M][F], Z [M][2 F], all of

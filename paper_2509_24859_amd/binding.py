@@ -36,6 +36,7 @@ EXPORTS = (
     "harp_adamw_plan_bytes", "harp_adamw_plan", "harp_adamw_step", "harp_adamw_read_state", "harp_adamw_release",
     "harp_norm_forward", "harp_norm_workspace_bytes", "harp_norm_backward",
     "harp_rotary", "harp_rotary_frequencies",
+    "harp_attention_workspace_bytes", "harp_attention_forward", "harp_attention_backward",
     "harp_gated_workspace_bytes", "harp_gated_forward", "harp_gated_grad",
 )
 
@@ -151,6 +152,10 @@ def load_library() -> C.CDLL:
     f64 = C.c_double
     lib.harp_rotary.argtypes = [vp, vp, vp]
     lib.harp_rotary_frequencies.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp, vp]
+    lib.harp_attention_workspace_bytes.argtypes = [vp, vp]
+    lib.harp_attention_workspace_bytes.restype = sz
+    lib.harp_attention_forward.argtypes = [vp, vp, vp, sz, vp]
+    lib.harp_attention_backward.argtypes = [vp, vp, vp, vp, sz, vp]
     lib.harp_gated_workspace_bytes.argtypes = [vp, i64, i64, i64]
     lib.harp_gated_workspace_bytes.restype = sz
     for name in ("harp_gated_forward", "harp_gated_grad"):

@@ -1,0 +1,922 @@
+// Softmax attention over packed or padded sequences, its gradients, and their C entry points.
+//
+// Heads that share keys are rows of one matrix: packed row r of a kv head is query r / group of head kv * group + r % group, so that
+// a tile of rows meets each key once whatever the group, and one new token of a large group fills a tile.
+//
+// Products are taken transposed where that spares a way through LDS.  S^T = K Q^T leaves a lane with 16 keys of one query (column
+// l % 32, keys 8 (i / 4) + 4 (l / 32) + i % 4 of 32): maxima and sums of a row are then within a lane and its partner 32 lanes
+// on, and P^T is the second operand of O^T = V^T P^T as it lies in the registers, the keys of a step of 16 in the order
+// 4 h .. 4 h + 3, 8 + 4 h .. 11 + 4 h for lane half h, in which V^T is read too.
+#include <math.h>
+
+#include "harp_ctx.h"
+#include "ops_common.h"
+
+using namespace harp;
+using namespace harp::ops;
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T> struct Mfma32;
+template <> struct Mfma32<__bf16> {
+    typedef bf16x8 Frag;
+    static __device__ __forceinline__ f32x16 run(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <> struct Mfma32<_Float16> {
+    typedef f16x8 Frag;
+    static __device__ __forceinline__ f32x16 run(Frag a, Frag b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kKeys = 64;            // keys of a tile in LDS
+constexpr int kDies = 8;
+
+// What the kernels know of a call.
+struct Call {
+    int64_t tokens_q, tokens_k;
+    int batch, heads, kv_heads, head, group, causal;
+    uint32_t group_magic;            // floor(2^32 / group)
+    float c;                         // scale * log2(e)
+    const int32_t *q_begin, *k_begin, *k_count;
+    int64_t q_token, q_step, k_token, k_step, v_token, v_step, o_token, o_step;
+    const void *q, *k, *v;
+    void *o;
+    float *lse;
+};
+
+// r / group for 0 <= r < 2^31: the estimate is the quotient or one less.
+__device__ __forceinline__ int query_of(const Call &a, int r) {
+    uint32_t q = __umulhi(uint32_t(r), a.group_magic);
+    if (a.group == 1) return r;
+    if (r - int(q) * a.group >= a.group) ++q;
+    return int(q);
+}
+
+struct Sequence {
+    int64_t q0, k0;                  // first tokens
+    int nq, nk, used;                // queries, keys, keys used
+};
+__device__ __forceinline__ int64_t kept(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
+__device__ __forceinline__ void span(const int32_t *begin, int64_t tokens, int batch, int b, int64_t &first, int &count) {
+    if (begin) {
+        first = kept(begin[b], 0, tokens);
+        count = int(kept(begin[b + 1], first, tokens) - first);
+    } else {
+        count = int(tokens / batch);
+        first = int64_t(b) * count;
+    }
+}
+__device__ __forceinline__ Sequence sequence(const Call &a, int b) {
+    Sequence s;
+    span(a.q_begin, a.tokens_q, a.batch, b, s.q0, s.nq);
+    span(a.k_begin, a.tokens_k, a.batch, b, s.k0, s.nk);
+    s.used = a.k_count ? int(kept(a.k_count[b], 0, s.nk)) : s.nk;
+    return s;
+}
+
+// The sequence that tile `id` of `side` rows belongs to, rows being `times` the tokens of `begin`'s spans, and its place there;
+// false behind the last.  Every wavefront looks for itself, 64 sequences at a time.
+__device__ __forceinline__ bool locate(const int32_t *begin, int64_t tokens, int batch, int times, int side, int id, int &b, int &tile) {
+    if (!begin) {
+        const int each = int((tokens / batch * times + side - 1) / side);
+        if (each == 0) return false;
+        b = id / each;
+        tile = id - b * each;
+        return b < batch;
+    }
+    const int lane = threadIdx.x % kWave;
+    for (int first = 0; first < batch; first += kWave) {
+        int tiles = 0;
+        if (first + lane < batch) {
+            int64_t at;
+            int count;
+            span(begin, tokens, batch, first + lane, at, count);
+            tiles = int((int64_t(count) * times + side - 1) / side);
+        }
+        int upto = tiles;
+#pragma unroll
+        for (int d = 1; d < kWave; d *= 2) {
+            const int below = __shfl_up(upto, d);
+            if (lane >= d) upto += below;
+        }
+        const uint64_t past = __ballot(id < upto);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            b = first + at;
+            tile = id - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at));
+            return true;
+        }
+        id -= __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    return false;
+}
+
+// Workgroups go to the 8 dies in turn, each with an L2 of its own: a die takes neighbours, which share keys.
+__device__ __forceinline__ int work_of(int id, int n) {
+    const int die = id % kDies, each = n / kDies, more = n % kDies;
+    return id / kDies + die * each + (die < more ? die : more);
+}
+
+// LDS holds rows of D elements in pieces of 16 bytes, moved within a row so that neither 8 rows read piece by piece nor 4 rows read
+// across (ds_read_tr) meet in the same 128 bytes.
+template <int D> __device__ __forceinline__ int moved(int row, int piece) {
+    return D == 96 ? piece ^ ((row >> 1 & 1) << 1 | (row >> 2 & 1)) : piece ^ ((row & 3) << 1 | (row >> 2 & 1));
+}
+// Fragment of 32 rows by 16 columns: lane l has row l % 32 and columns 16 k + 8 (l / 32) .. + 7.
+template <typename T, int D> __device__ __forceinline__ typename Mfma32<T>::Frag along(const T *lds, int row0, int k) {
+    const int lane = threadIdx.x % kWave, row = row0 + lane % 32;
+    return *reinterpret_cast<const typename Mfma32<T>::Frag *>(lds + row * D + moved<D>(row, 2 * k + lane / 32) * 8);
+}
+// Fragment of 32 columns by 16 rows, transposed: lane l has column col0 + l % 32 and, h = l / 32, rows row0 + 4 h .. + 3 and
+// row0 + 8 + 4 h .. + 3.
+template <typename T, int D> __device__ __forceinline__ typename Mfma32<T>::Frag across(const T *lds, int row0, int col0) {
+    typedef __attribute__((address_space(3))) s16x4 *Lds;
+    const int lane = threadIdx.x % kWave, i = lane % 16, col = col0 + lane / 16 % 2 * 16 + i % 4 * 4;
+    const int row = row0 + lane / 32 * 4 + i / 4;
+    const T *lo = lds + row * D + moved<D>(row, col / 8) * 8 + col % 8;
+    const T *hi = lds + (row + 8) * D + moved<D>(row + 8, col / 8) * 8 + col % 8;
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)lo), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)hi);
+    const s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(typename Mfma32<T>::Frag, v);
+}
+
+// 8 elements wherever they lie, or zeros.
+template <typename T> __device__ __forceinline__ typename Mfma32<T>::Frag eight(const T *p, bool there) {
+    typedef typename Mfma32<T>::Frag Loose __attribute__((aligned(sizeof(T))));
+    typename Mfma32<T>::Frag v = {};
+    if (there) v = *reinterpret_cast<const Loose *>(p);
+    return v;
+}
+
+// A tile of ROWS rows on its way from memory through registers into LDS.  Rows from `limit` on, and channels from `head` on, are zeros:
+// what memory holds there is not looked at.
+template <typename T, int D, int ROWS, int THREADS> struct Stage {
+    static constexpr int kAll = ROWS * (D / 8), kEach = (kAll + THREADS - 1) / THREADS;
+    typename Mfma32<T>::Frag piece[kEach];
+    template <typename At> __device__ __forceinline__ void ask(At at, int limit, int head) {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int id = i * THREADS + int(threadIdx.x), row = id / (D / 8), col = id % (D / 8) * 8;
+            const bool there = row < limit && col < head && (kAll % THREADS == 0 || id < kAll);
+            piece[i] = eight<T>(at(there ? row : 0) + (there ? col : 0), there);
+        }
+    }
+    __device__ __forceinline__ void put(T *lds) const {
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int id = i * THREADS + int(threadIdx.x), row = id / (D / 8), c = id % (D / 8);
+            if (kAll % THREADS == 0 || id < kAll) *reinterpret_cast<typename Mfma32<T>::Frag *>(lds + row * D + moved<D>(row, c) * 8) = piece[i];
+        }
+    }
+};
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+// A wavefront's 32 packed rows, one to a lane and its partner.
+struct Row {
+    int64_t token;
+    int head, limit;                 // keys before `limit` are seen; -1: no such row
+};
+__device__ __forceinline__ int limit_of(const Call &a, const Sequence &s, int query) {
+    if (!a.causal) return s.used;
+    const int seen = query + 1 + s.used - s.nq;
+    return seen < 0 ? 0 : seen;
+}
+__device__ __forceinline__ Row row_of(const Call &a, const Sequence &s, int kv, int r) {
+    if (r >= int64_t(s.nq) * a.group) return Row{0, 0, -1};
+    const int query = query_of(a, r);
+    return Row{s.q0 + query, kv * a.group + r - query * a.group, limit_of(a, s, query)};
+}
+
+// Partial results of a share of the keys: unscaled sums [share][token][head][channel], reference and sum [share][token][head].
+struct Shares {
+    int count;
+    float *sums, *stats;
+};
+
+// WAVES wavefronts of 32 rows; keys go through LDS 64 at a time, two tiles of them.
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, Shares shares) {
+    constexpr int kThreads = WAVES * kWave, kRows = WAVES * 32;
+    typedef typename Mfma32<T>::Frag Frag;
+    __shared__ __align__(16) T lk[2][kKeys * D];
+    __shared__ __align__(16) T lv[2][kKeys * D];
+    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, kv = work / shares.count / tiles;
+    int b, tile;
+    if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kRows, tiles - 1 - work / shares.count % tiles, b, tile)) return;
+    const Sequence s = sequence(a, b);
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, h = lane / 32;
+    const int r0 = tile * kRows, rows = int(int64_t(s.nq) * a.group);
+    const Row mine = row_of(a, s, kv, r0 + wave * 32 + lane % 32);
+    // keys that some row of the workgroup sees: its last row sees most
+    const int last = r0 + kRows < rows ? r0 + kRows - 1 : rows - 1, most = limit_of(a, s, query_of(a, last));
+    const int all = (most + kKeys - 1) / kKeys, first = int(int64_t(all) * share / shares.count), end = int(int64_t(all) * (share + 1) / shares.count);
+    // limits within the wavefront
+    int wave_most = mine.limit, wave_least = mine.limit < 0 ? 1 << 30 : mine.limit;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        wave_most = max(wave_most, __shfl_xor(wave_most, d));
+        wave_least = min(wave_least, __shfl_xor(wave_least, d));
+    }
+    wave_most = __builtin_amdgcn_readfirstlane(wave_most);
+    wave_least = __builtin_amdgcn_readfirstlane(wave_least);
+
+    Frag q[D / 16];
+    const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) q[k] = eight<T>(from + 16 * k + 8 * h, mine.limit >= 0 && 16 * k + 8 * h < a.head);
+    f32x16 o[D / 32] = {};
+    float top = -INFINITY, sum = 0;
+
+    const T *keys = static_cast<const T *>(a.k) + s.k0 * a.k_token + kv * a.k_step;
+    const T *values = static_cast<const T *>(a.v) + s.k0 * a.v_token + kv * a.v_step;
+    Stage<T, D, kKeys, kThreads> sk, sv;
+    auto ask = [&](int t) {
+        sk.ask([&](int row) { return keys + (int64_t(t) * kKeys + row) * a.k_token; }, s.used - t * kKeys, a.head);
+        sv.ask([&](int row) { return values + (int64_t(t) * kKeys + row) * a.v_token; }, s.used - t * kKeys, a.head);
+    };
+    if (first < end) {
+        ask(first);
+        sk.put(lk[0]);
+        sv.put(lv[0]);
+    }
+    __syncthreads();
+    for (int t = first; t < end; ++t) {
+        const int at = (t - first) % 2;
+        if (t + 1 < end) ask(t + 1);
+        if (t * kKeys < wave_most) {
+            f32x16 p[2] = {};
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) p[u] = Mfma32<T>::run(along<T, D>(lk[at], 32 * u, k), q[k], p[u]);
+            if ((t + 1) * kKeys > wave_least) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (t * kKeys + 32 * u + 8 * (i / 4) + 4 * h + i % 4 >= mine.limit) p[u][i] = -INFINITY;
+            }
+            float high = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) high = fmaxf(high, p[u][i]);
+            high = fmaxf(high, other_half(high)) * a.c;
+            // The reference that exponents are taken against follows the maximum only when that has grown by 2^8 over it:
+            // sums in 32 bits and weights of 16 have room for the factor.
+            if (__any(high > top + 8.0f)) {
+                const float next = fmaxf(high, top), shrink = top == next ? 1.0f : __builtin_amdgcn_exp2f(top - next);
+                top = next;
+                sum *= shrink;
+#pragma unroll
+                for (int m = 0; m < D / 32; ++m) o[m] *= shrink;
+            }
+            const float against = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[u][i] = __builtin_amdgcn_exp2f(fmaf(p[u][i], a.c, -against));
+                    sum += p[u][i];
+                }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    Frag w;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = T(p[u][8 * k + i]);
+#pragma unroll
+                    for (int m = 0; m < D / 32; ++m) o[m] = Mfma32<T>::run(across<T, D>(lv[at], 32 * u + 16 * k, 32 * m), w, o[m]);
+                }
+        }
+        if (t + 1 < end) {
+            sk.put(lk[1 - at]);
+            sv.put(lv[1 - at]);
+        }
+        __syncthreads();
+    }
+    if (mine.limit < 0) return;
+    sum += other_half(sum);
+    if (shares.count > 1) {
+        const int64_t at = (int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head;
+        if (h == 0) {
+            shares.stats[2 * at] = top;
+            shares.stats[2 * at + 1] = sum;
+        }
+        if (sum == 0) return;                            // nothing that the join looks at
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int col = 32 * m + 8 * i + 4 * h;
+                if (col < a.head) *reinterpret_cast<f32x4 *>(shares.sums + at * a.head + col) = f32x4{o[m][4 * i], o[m][4 * i + 1], o[m][4 * i + 2], o[m][4 * i + 3]};
+            }
+        return;
+    }
+    const float scale = sum == 0 ? 0.0f : 1.0f / sum;    // no key: zeros; scores that are NaN: NaN
+    if (a.lse && h == 0) a.lse[mine.head * a.tokens_q + mine.token] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+    T *to = static_cast<T *>(a.o) + mine.token * a.o_token + mine.head * a.o_step;
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int col = 32 * m + 8 * i + 4 * h;
+            if (col < a.head) store4(to + col, f32x4{o[m][4 * i] * scale, o[m][4 * i + 1] * scale, o[m][4 * i + 2] * scale, o[m][4 * i + 3] * scale});
+        }
+}
+
+// Shares of the keys, joined: 32 lanes a row of four channels each, rows of sequences only.
+constexpr int kJoinRows = 8;
+template <typename T> __global__ __launch_bounds__(kJoinRows * 32) void forward_join(Call a, int tiles, Shares shares) {
+    int b, tile;
+    if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kJoinRows, blockIdx.x % tiles, b, tile)) return;
+    const Sequence s = sequence(a, b);
+    const Row mine = row_of(a, s, blockIdx.x / tiles, tile * kJoinRows + threadIdx.x / 32);
+    if (mine.limit < 0) return;
+    const int64_t each = a.tokens_q * a.heads, at = mine.token * a.heads + mine.head;
+    float top = -INFINITY;
+    for (int i = 0; i < shares.count; ++i) top = fmaxf(top, shares.stats[2 * (i * each + at)]);
+    float sum = 0;
+    f32x4 o = {0, 0, 0, 0};
+    const int col = threadIdx.x % 32 * 4;
+    for (int i = 0; i < shares.count; ++i) {
+        const float *stats = shares.stats + 2 * (i * each + at);
+        if (stats[1] == 0) continue;
+        const float w = stats[0] == top ? 1.0f : __builtin_amdgcn_exp2f(stats[0] - top);
+        sum += w * stats[1];
+        if (col < a.head) o += w * load4(shares.sums + (i * each + at) * a.head + col);
+    }
+    const float scale = sum == 0 ? 0.0f : 1.0f / sum;    // no key: zeros; scores that are NaN: NaN
+    if (col < a.head) store4(static_cast<T *>(a.o) + mine.token * a.o_token + mine.head * a.o_step + col, o * scale);
+    if (a.lse && col == 0) a.lse[mine.head * a.tokens_q + mine.token] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+}
+
+// ---------------------------------------------------------------------------------------------- gradients
+struct Grads {
+    const void *d_o;
+    int64_t do_token, do_step, dq_token, dq_step, dk_token, dk_step, dv_token, dv_step;
+    void *dq, *dk, *dv;
+    float *delta;                    // [heads][tokens_q]: sum over channels of dO O
+    uint32_t *peaks;                 // HARP_F16: largest squared norms of dO's and V's rows, as bits
+    float scale;
+};
+
+// Weights and their gradients on their way into the matrix instructions.  bfloat16 has the range of 32 bits.  In float16 weights go in
+// times 2^12 (they are normal numbers down to 2^-26: 10^5 equal ones of a row are still rounded to 2^-11 of themselves), and
+// gradients times a power of two taken from the largest norms: |P (dP - D)| <= 2 |dO_i| |v_j|, which is brought to 2^14 at most.
+template <typename T> struct Range {
+    static constexpr bool kNarrow = sizeof(T) == 2 && __is_same(T, _Float16);
+    static constexpr float kShift = kNarrow ? 12.0f : 0.0f, kWeight = kNarrow ? 0.000244140625f : 1.0f;
+    float factor = 1;                // of dP - D where a weight carries 2^kShift
+    __device__ __forceinline__ explicit Range(const uint32_t *peaks) {
+        if constexpr (kNarrow) {
+            const float bound = 4 * __uint_as_float(peaks[0]) * __uint_as_float(peaks[1]);
+            int e = 0;
+            if (bound > 0 && bound < INFINITY) {
+                (void)frexpf(bound, &e);
+                factor = ldexpf(1.0f, 14 - ((e + 1) >> 1) - int(kShift));
+            }
+        }
+    }
+    __device__ __forceinline__ float less(float dp, float delta) const { return kNarrow ? fmaf(dp, factor, -delta) : dp - delta; }
+    __device__ __forceinline__ float back() const { return kNarrow ? kWeight / factor : 1.0f; }       // of what gradients are summed into
+};
+
+__global__ void no_peaks(uint32_t *peaks) { peaks[threadIdx.x] = 0; }
+// A workgroup takes 64 rows of sequences, of dO or of V, 16 lanes a row.  A maximum does not mind the order.
+constexpr int kPeakRows = 64;
+template <typename T>
+__global__ __launch_bounds__(256) void find_peaks(Call a, Grads g, int of_q) {
+    const bool q = int(blockIdx.x) < of_q;
+    const int times = q ? a.heads : a.kv_heads;
+    int b, tile;
+    if (!locate(q ? a.q_begin : a.k_begin, q ? a.tokens_q : a.tokens_k, a.batch, times, kPeakRows, q ? blockIdx.x : blockIdx.x - of_q, b, tile)) return;
+    const Sequence s = sequence(a, b);
+    const int64_t rows = int64_t(q ? s.nq : s.used) * times, first = int64_t(tile) * kPeakRows;
+    const int col = threadIdx.x % 16 * 8;
+    float peak = 0;
+#pragma unroll
+    for (int i = 0; i < kPeakRows / 16; ++i) {
+        const int64_t r = first + i * 16 + threadIdx.x / 16, token = r / times, head = r % times;
+        const bool there = r < rows && col < a.head;
+        const T *from = q ? static_cast<const T *>(g.d_o) + (s.q0 + token) * g.do_token + head * g.do_step
+                          : static_cast<const T *>(a.v) + (s.k0 + token) * a.v_token + head * a.v_step;
+        const auto x = eight<T>(from + col, there);
+        float d = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) d += to_f32(T(x[k])) * to_f32(T(x[k]));
+        d = sum16(d);
+        peak = d > peak || d != d ? d : peak;
+    }
+    const uint32_t high = wave_max(__float_as_uint(peak));
+    if (threadIdx.x % kWave == 0) atomicMax(g.peaks + (q ? 0 : 1), high);
+}
+
+// 16 lanes a row of eight channels each.
+template <typename T> __global__ __launch_bounds__(256) void deltas(Call a, Grads g) {
+    const int col = threadIdx.x % 16 * 8;
+    const bool there = col < a.head;
+    for (int64_t row = int64_t(blockIdx.x) * 16 + threadIdx.x / 16; row < a.tokens_q * a.heads; row += int64_t(gridDim.x) * 16) {
+        const int64_t token = row / a.heads;
+        const int head = int(row - token * a.heads);
+        const auto x = eight<T>(static_cast<const T *>(a.o) + token * a.o_token + head * a.o_step + (there ? col : 0), there);
+        const auto y = eight<T>(static_cast<const T *>(g.d_o) + token * g.do_token + head * g.do_step + (there ? col : 0), there);
+        float d = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d += to_f32(T(x[i])) * to_f32(T(y[i]));
+        d = sum16(d);
+        if (threadIdx.x % 16 == 0) g.delta[head * a.tokens_q + token] = d;
+    }
+}
+
+// dQ, as the forward pass goes: dQ^T = K^T dS^T, dS^T = P^T (V dO^T - delta).
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g, int tiles, Shares shares) {
+    constexpr int kThreads = WAVES * kWave, kRows = WAVES * 32;
+    typedef typename Mfma32<T>::Frag Frag;
+    __shared__ __align__(16) T lk[2][kKeys * D];
+    __shared__ __align__(16) T lv[2][kKeys * D];
+    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, kv = work / shares.count / tiles;
+    int b, tile;
+    if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kRows, tiles - 1 - work / shares.count % tiles, b, tile)) return;
+    const Sequence s = sequence(a, b);
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, h = lane / 32;
+    const int r0 = tile * kRows, rows = int(int64_t(s.nq) * a.group);
+    const Row mine = row_of(a, s, kv, r0 + wave * 32 + lane % 32);
+    const int last = r0 + kRows < rows ? r0 + kRows - 1 : rows - 1, most = limit_of(a, s, query_of(a, last));
+    const int all = (most + kKeys - 1) / kKeys, first = int(int64_t(all) * share / shares.count), end = int(int64_t(all) * (share + 1) / shares.count);
+    const bool here = mine.limit >= 0;
+    float lse = here ? a.lse[mine.head * a.tokens_q + mine.token] * kLog2e : 0;
+    const Range<T> range(g.peaks);
+    const float delta = here ? g.delta[mine.head * a.tokens_q + mine.token] * range.factor : 0;
+    const int limit = lse == -INFINITY ? 0 : mine.limit;
+    lse = lse == -INFINITY ? 0 : lse - Range<T>::kShift;
+    int wave_most = limit, wave_least = limit < 0 ? 1 << 30 : limit;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        wave_most = max(wave_most, __shfl_xor(wave_most, d));
+        wave_least = min(wave_least, __shfl_xor(wave_least, d));
+    }
+    wave_most = __builtin_amdgcn_readfirstlane(wave_most);
+    wave_least = __builtin_amdgcn_readfirstlane(wave_least);
+    Frag q[D / 16], d_o[D / 16];
+    const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
+    const T *from_do = static_cast<const T *>(g.d_o) + mine.token * g.do_token + mine.head * g.do_step;
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) {
+        q[k] = eight<T>(from + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
+        d_o[k] = eight<T>(from_do + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
+    }
+    f32x16 dq[D / 32] = {};
+    const T *keys = static_cast<const T *>(a.k) + s.k0 * a.k_token + kv * a.k_step;
+    const T *values = static_cast<const T *>(a.v) + s.k0 * a.v_token + kv * a.v_step;
+    Stage<T, D, kKeys, kThreads> sk, sv;
+    auto ask = [&](int t) {
+        sk.ask([&](int row) { return keys + (int64_t(t) * kKeys + row) * a.k_token; }, s.used - t * kKeys, a.head);
+        sv.ask([&](int row) { return values + (int64_t(t) * kKeys + row) * a.v_token; }, s.used - t * kKeys, a.head);
+    };
+    if (first < end) {
+        ask(first);
+        sk.put(lk[0]);
+        sv.put(lv[0]);
+    }
+    __syncthreads();
+    for (int t = first; t < end; ++t) {
+        const int at = (t - first) % 2;
+        if (t + 1 < end) ask(t + 1);
+        if (t * kKeys < wave_most) {
+            const bool masked = (t + 1) * kKeys > wave_least;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                f32x16 p = {}, dp = {};
+#pragma unroll
+                for (int k = 0; k < D / 16; ++k) {
+                    p = Mfma32<T>::run(along<T, D>(lk[at], 32 * u, k), q[k], p);
+                    dp = Mfma32<T>::run(along<T, D>(lv[at], 32 * u, k), d_o[k], dp);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * range.less(dp[i], delta);
+                if (masked) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (t * kKeys + 32 * u + 8 * (i / 4) + 4 * h + i % 4 >= limit) p[i] = 0;
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    Frag w;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) w[i] = T(p[8 * k + i]);
+#pragma unroll
+                    for (int m = 0; m < D / 32; ++m) dq[m] = Mfma32<T>::run(across<T, D>(lk[at], 32 * u + 16 * k, 32 * m), w, dq[m]);
+                }
+            }
+        }
+        if (t + 1 < end) {
+            sk.put(lk[1 - at]);
+            sv.put(lv[1 - at]);
+        }
+        __syncthreads();
+    }
+    if (!here) return;
+    const float scale = g.scale * range.back();
+    float *sums = shares.sums + ((int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head) * a.head;
+    T *to = static_cast<T *>(g.dq) + mine.token * g.dq_token + mine.head * g.dq_step;
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int col = 32 * m + 8 * i + 4 * h;
+            if (col >= a.head) continue;
+            const f32x4 v = f32x4{dq[m][4 * i], dq[m][4 * i + 1], dq[m][4 * i + 2], dq[m][4 * i + 3]} * scale;
+            if (shares.count > 1) *reinterpret_cast<f32x4 *>(sums + col) = v;
+            else store4(to + col, v);
+        }
+}
+
+// dK and dV of 32 keys a wavefront, whose rows come through LDS kBack at a time.  dV^T = dO^T P, dK^T = Q^T dS, where a lane has
+// 16 rows of one key.
+constexpr int kBack = 32;
+template <typename T, int D, int WAVES>
+__global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, int tiles, Shares shares) {
+    constexpr int kThreads = WAVES * kWave, kCols = WAVES * 32;
+    typedef typename Mfma32<T>::Frag Frag;
+    __shared__ __align__(16) T lq[2][kBack * D];
+    __shared__ __align__(16) T ld[2][kBack * D];
+    __shared__ __align__(16) float l_lse[2][kBack], l_delta[2][kBack];
+    __shared__ __align__(16) int l_limit[2][kBack];
+    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, kv = work / shares.count / tiles;
+    int b, tile;
+    if (!locate(a.k_begin, a.tokens_k, a.batch, 1, kCols, work / shares.count % tiles, b, tile)) return;
+    const Sequence s = sequence(a, b);
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, h = lane / 32;
+    const int key0 = tile * kCols, key = key0 + wave * 32 + lane % 32, rows = int(int64_t(s.nq) * a.group);
+    const bool used = key < s.used;
+    // rows that see none of the workgroup's keys come first, if any
+    int skip = a.causal ? key0 - (s.used - s.nq) : 0;
+    skip = skip < 0 ? 0 : skip;
+    const int64_t begin_row = int64_t(skip) * a.group;
+    const int all = key0 < s.used && begin_row < rows ? int((rows - begin_row + kBack - 1) / kBack) : 0, row_first = int(begin_row);
+    const int first = int(int64_t(all) * share / shares.count), end = int(int64_t(all) * (share + 1) / shares.count);
+    Frag k[D / 16], v[D / 16];
+    const T *from_k = static_cast<const T *>(a.k) + (s.k0 + (used ? key : 0)) * a.k_token + kv * a.k_step;
+    const T *from_v = static_cast<const T *>(a.v) + (s.k0 + (used ? key : 0)) * a.v_token + kv * a.v_step;
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+        k[i] = eight<T>(from_k + 16 * i + 8 * h, used && 16 * i + 8 * h < a.head);
+        v[i] = eight<T>(from_v + 16 * i + 8 * h, used && 16 * i + 8 * h < a.head);
+    }
+    f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+    Stage<T, D, kBack, kThreads> sq, sd;
+    const Range<T> range(g.peaks);
+    float lse = 0, delta = 0;
+    int limit = 0;
+    auto ask = [&](int t) {
+        const int r0 = row_first + t * kBack;
+        auto place = [&](int row, int64_t token, int64_t step) {
+            const int query = query_of(a, r0 + row);
+            return (s.q0 + query) * token + (kv * a.group + r0 + row - query * a.group) * step;
+        };
+        sq.ask([&](int row) { return static_cast<const T *>(a.q) + place(row, a.q_token, a.q_step); }, rows - r0, a.head);
+        sd.ask([&](int row) { return static_cast<const T *>(g.d_o) + place(row, g.do_token, g.do_step); }, rows - r0, a.head);
+        if (threadIdx.x < kBack) {
+            const Row r = row_of(a, s, kv, r0 + int(threadIdx.x));
+            const bool there = r.limit >= 0;
+            lse = there ? a.lse[r.head * a.tokens_q + r.token] * kLog2e : 0;
+            delta = there ? g.delta[r.head * a.tokens_q + r.token] * range.factor : 0;
+            limit = there && lse != -INFINITY ? r.limit : 0;
+            lse = lse == -INFINITY ? 0 : lse - Range<T>::kShift;
+        }
+    };
+    auto put = [&](int at) {
+        sq.put(lq[at]);
+        sd.put(ld[at]);
+        if (threadIdx.x < kBack) l_lse[at][threadIdx.x] = lse, l_delta[at][threadIdx.x] = delta, l_limit[at][threadIdx.x] = limit;
+    };
+    if (first < end) {
+        ask(first);
+        put(0);
+    }
+    __syncthreads();
+    for (int t = first; t < end; ++t) {
+        const int at = (t - first) % 2;
+        if (t + 1 < end) ask(t + 1);
+        f32x16 p = {}, dp = {};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+            p = Mfma32<T>::run(along<T, D>(lq[at], 0, i), k[i], p);
+            dp = Mfma32<T>::run(along<T, D>(ld[at], 0, i), v[i], dp);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = 8 * i + 4 * h;
+            const f32x4 against = *reinterpret_cast<const f32x4 *>(&l_lse[at][row]), less = *reinterpret_cast<const f32x4 *>(&l_delta[at][row]);
+            const int *seen = &l_limit[at][row];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool on = key < seen[j];
+                const float w = __builtin_amdgcn_exp2f(fmaf(p[4 * i + j], a.c, -against[j]));
+                p[4 * i + j] = on ? w : 0;
+                dp[4 * i + j] = on ? w * range.less(dp[4 * i + j], less[j]) : 0;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            Frag w, ds;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = T(p[8 * i + j]), ds[j] = T(dp[8 * i + j]);
+#pragma unroll
+            for (int m = 0; m < D / 32; ++m) {
+                dv[m] = Mfma32<T>::run(across<T, D>(ld[at], 16 * i, 32 * m), w, dv[m]);
+                dk[m] = Mfma32<T>::run(across<T, D>(lq[at], 16 * i, 32 * m), ds, dk[m]);
+            }
+        }
+        if (t + 1 < end) put(1 - at);
+        __syncthreads();
+    }
+    if (key >= s.nk) return;
+    const float scale = g.scale * range.back();
+    const int64_t token = s.k0 + key, each = a.tokens_k * a.kv_heads * a.head;
+    float *sums = shares.sums + 2 * share * each + (token * a.kv_heads + kv) * a.head;
+    T *to_k = static_cast<T *>(g.dk) + token * g.dk_token + kv * g.dk_step, *to_v = static_cast<T *>(g.dv) + token * g.dv_token + kv * g.dv_step;
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int col = 32 * m + 8 * i + 4 * h;
+            if (col >= a.head) continue;
+            const f32x4 x = f32x4{dk[m][4 * i], dk[m][4 * i + 1], dk[m][4 * i + 2], dk[m][4 * i + 3]} * scale;
+            const f32x4 y = f32x4{dv[m][4 * i], dv[m][4 * i + 1], dv[m][4 * i + 2], dv[m][4 * i + 3]} * Range<T>::kWeight;
+            if (shares.count > 1) {
+                *reinterpret_cast<f32x4 *>(sums + col) = x;
+                *reinterpret_cast<f32x4 *>(sums + each + col) = y;
+            } else {
+                if (g.dk) store4(to_k + col, x);
+                if (g.dv) store4(to_v + col, y);
+            }
+        }
+}
+
+// Sums of shares, in their order, for the rows of sequences: `rows` of them per token of begin's spans, element (token, row) of
+// sums[share * stride + ...], to `to`.
+template <typename T>
+__global__ __launch_bounds__(kJoinRows * 32) void join_sums(const int32_t *begin, int64_t tokens, int batch, int rows, int head, const float *sums, int count,
+                                                            int64_t stride, T *to, int64_t to_token, int64_t to_step) {
+    int b, tile;
+    if (!locate(begin, tokens, batch, rows, kJoinRows, blockIdx.x, b, tile)) return;
+    int64_t first;
+    int n;
+    span(begin, tokens, batch, b, first, n);
+    const int64_t r = int64_t(tile) * kJoinRows + threadIdx.x / 32;
+    const int col = threadIdx.x % 32 * 4;
+    if (r >= int64_t(n) * rows || col >= head) return;
+    const int64_t token = first + r / rows, row = r % rows;
+    const float *at = sums + (token * rows + row) * head + col;
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) x += load4(at + i * stride);
+    store4(to + token * to_token + row * to_step + col, x);
+}
+
+// ---------------------------------------------------------------------------------------------- on the host
+bool sizes_fit(const harp_attention *g) {
+    const int64_t most = (int64_t(1) << 31) - 1;
+    return g->tokens_q >= 0 && g->tokens_k >= 0 && g->tokens_q <= most && g->tokens_k <= most && g->batch >= 1 && g->batch <= 1 << 20 &&
+           g->heads >= 1 && g->heads <= 1 << 14 && g->kv_heads >= 1 && g->heads % g->kv_heads == 0 && g->head >= 8 && g->head % 8 == 0 &&
+           g->head <= HARP_ATTENTION_MAX_HEAD && g->tokens_q * (g->heads / g->kv_heads) <= most;
+}
+
+// How the passes are launched; of sizes that the host knows.  With begins on the device a pass has room for a partial tile
+// of every sequence.
+struct Plan {
+    int waves;                       // of a workgroup
+    int64_t tiles;                   // of rows, or of keys
+    int shares;                      // of what a tile goes through
+};
+int64_t tiles_of(int64_t tokens, int64_t times, int batch, int side) {
+    const int64_t whole = tokens * times / side, each = (tokens / batch * times + side - 1) / side * batch;
+    // equal lengths need `each`; begins on the device at most this
+    return whole + batch > each ? whole + batch : each;
+}
+// `through`: rows that a tile goes through on average, `least` of them a share.
+Plan plan_for(const harp_ctx *ctx, int64_t tokens, int64_t times, int batch, int kv_heads, int64_t through, int64_t least) {
+    Plan p = {};
+    p.waves = tokens * times / batch > 128 ? 8 : 4;
+    p.tiles = tiles_of(tokens, times, batch, 32 * p.waves);
+    int64_t busy = (tokens * times + 32 * p.waves - 1) / (32 * p.waves);
+    busy = (busy > batch ? busy : batch) * kv_heads;                    // workgroups that have something to do
+    int64_t shares = 2 * int64_t(ctx->n_cu) * 4 / p.waves / busy;
+    shares = shares < through / least ? shares : through / least;
+    p.shares = int(shares < 1 ? 1 : shares > 64 ? 64 : shares);
+    return p;
+}
+constexpr int kLeastKeys = 256;
+Plan plan_queries(const harp_ctx *ctx, const harp_attention *g) {
+    return plan_for(ctx, g->tokens_q, g->heads / g->kv_heads, g->batch, g->kv_heads, g->tokens_k / g->batch, kLeastKeys);
+}
+Plan plan_keys(const harp_ctx *ctx, const harp_attention *g) {
+    return plan_for(ctx, g->tokens_k, 1, g->batch, g->kv_heads, g->tokens_q / g->batch * (g->heads / g->kv_heads), kLeastKeys);
+}
+
+struct Space { size_t peaks, stats, sums, all; };        // where parts of the workspace begin, behind delta
+Space space_for(const harp_ctx *ctx, const harp_attention *g) {
+    const size_t rows = size_t(g->tokens_q) * g->heads, kv = size_t(g->tokens_k) * g->kv_heads;
+    const Plan q = plan_queries(ctx, g), k = plan_keys(ctx, g);
+    Space s = {};
+    s.peaks = round_up(rows * 4, 256);
+    s.stats = s.peaks + 256;
+    s.sums = s.stats + (q.shares > 1 ? round_up(rows * q.shares * 8, 256) : 0);
+    const size_t of_q = q.shares > 1 ? rows * q.shares * g->head * 4 : 0, of_k = k.shares > 1 ? kv * k.shares * g->head * 8 : 0;
+    s.all = s.sums + round_up(of_q > of_k ? of_q : of_k, 256) + 256;
+    return s;
+}
+
+int attention_sizes(harp_ctx *ctx, const harp_attention *g) {
+    if (!sizes_fit(g))
+        return fail(ctx, HARP_ERR_SHAPE, "tokens, batch, heads, kv_heads or head out of range: %lld and %lld tokens, batch %d, %d heads, %d of keys, head %d",
+                    (long long)g->tokens_q, (long long)g->tokens_k, g->batch, g->heads, g->kv_heads, g->head);
+    return HARP_OK;
+}
+
+struct Tensor { const char *name; const void *p; int64_t tokens, heads, token, step; bool needed, written; };
+bool clear_of_each_other(int64_t tokens, int64_t heads, int64_t head, int64_t token, int64_t step) {
+    typedef __int128 Wide;
+    const bool in_token = (heads <= 1 || step >= head) && (tokens <= 1 || token >= Wide(heads - 1) * step + head);
+    const bool in_head = (tokens <= 1 || token >= head) && (heads <= 1 || step >= Wide(tokens - 1) * token + head);
+    return in_token || in_head;
+}
+
+int check(harp_ctx *ctx, const harp_attention *g, const Tensor *t, int count, const void *workspace, size_t workspace_bytes) {
+    const int rc = attention_sizes(ctx, g);
+    if (rc != HARP_OK) return rc;
+    if (g->type != HARP_BF16 && g->type != HARP_F16) return fail(ctx, HARP_ERR_INVALID_ARG, "type must be HARP_BF16 or HARP_F16");
+    if (!(g->scale > 0) || !isfinite(g->scale)) return fail(ctx, HARP_ERR_INVALID_ARG, "scale must be positive");
+    if ((!g->q_begin && g->tokens_q % g->batch) || (!g->k_begin && g->tokens_k % g->batch))
+        return fail(ctx, HARP_ERR_SHAPE, "tokens are no multiple of the batch, and begins are missing");
+    if (!aligned(g->q_begin, 4) || !aligned(g->k_begin, 4) || !aligned(g->k_count, 4) || !aligned(g->lse, 4))
+        return fail(ctx, HARP_ERR_INVALID_ARG, "begins, counts or lse are not aligned to their elements");
+    const int64_t far = int64_t(1) << 40;
+    for (int i = 0; i < count; ++i) {
+        if (!t[i].p && t[i].needed && t[i].tokens > 0) return fail(ctx, HARP_ERR_INVALID_ARG, "null %s", t[i].name);
+        if (!t[i].p) continue;
+        if (!aligned(t[i].p, 2)) return fail(ctx, HARP_ERR_INVALID_ARG, "%s is not aligned to its elements", t[i].name);
+        if (t[i].token < 0 || t[i].step < 0 || t[i].token > far || t[i].step > far)
+            return fail(ctx, HARP_ERR_SHAPE, "%s: distances must be in 0 .. 2^40", t[i].name);
+        if (t[i].written && !clear_of_each_other(t[i].tokens, t[i].heads, g->head, t[i].token, t[i].step))
+            return fail(ctx, HARP_ERR_SHAPE, "%s: elements lie over each other", t[i].name);
+    }
+    const size_t need = space_for(ctx, g).all;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need)
+        return fail(ctx, HARP_ERR_WORKSPACE, "the workspace needs %zu bytes, aligned to 256", need);
+    const Plan q = plan_queries(ctx, g), k = plan_keys(ctx, g);
+    const int64_t grid = int64_t(1) << 23;               // a launch has less than 2^32 threads
+    const bool q_fits = q.shares == 1 || (tiles_of(g->tokens_q, g->heads, g->batch, kJoinRows) < grid &&
+                                          tiles_of(g->tokens_q, g->heads / g->kv_heads, g->batch, kJoinRows) * g->kv_heads < grid);
+    const bool k_fits = k.shares == 1 || tiles_of(g->tokens_k, g->kv_heads, g->batch, kJoinRows) < grid;
+    if (q.tiles * q.shares * g->kv_heads >= grid || k.tiles * k.shares * g->kv_heads >= grid || !q_fits || !k_fits ||
+        tiles_of(g->tokens_q, g->heads, g->batch, kPeakRows) + tiles_of(g->tokens_k, g->kv_heads, g->batch, kPeakRows) >= grid)
+        return fail(ctx, HARP_ERR_SHAPE, "too many rows for one launch");
+    const hipError_t e = hipSetDevice(ctx->device);
+    return e == hipSuccess ? HARP_OK : hip_fail(ctx, e, "hipSetDevice");
+}
+
+Call call_of(const harp_attention *g) {
+    Call a = {};
+    a.tokens_q = g->tokens_q, a.tokens_k = g->tokens_k;
+    a.batch = g->batch, a.heads = g->heads, a.kv_heads = g->kv_heads, a.head = g->head, a.group = g->heads / g->kv_heads, a.causal = g->causal;
+    a.group_magic = uint32_t((uint64_t(1) << 32) / uint32_t(a.group));
+    a.c = g->scale * kLog2e;
+    a.q_begin = g->q_begin, a.k_begin = g->k_begin, a.k_count = g->k_count;
+    a.q_token = g->q_token, a.q_step = g->q_step, a.k_token = g->k_token, a.k_step = g->k_step, a.v_token = g->v_token, a.v_step = g->v_step;
+    a.o_token = g->o_token, a.o_step = g->o_step;
+    a.q = g->Q, a.k = g->K, a.v = g->V, a.o = g->O, a.lse = g->lse;
+    return a;
+}
+
+int launched(harp_ctx *ctx) {
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? HARP_OK : hip_fail(ctx, e, "launching the attention's kernels");
+}
+
+template <typename T, int D> void launch_forward(const Plan &p, const Call &a, const Shares &shares, hipStream_t st) {
+    const dim3 grid(uint32_t(p.tiles * p.shares * a.kv_heads));
+    if (p.waves == 8) forward<T, D, 8><<<grid, dim3(512), 0, st>>>(a, int(p.tiles), shares);
+    else forward<T, D, 4><<<grid, dim3(256), 0, st>>>(a, int(p.tiles), shares);
+}
+template <typename T, int D> void launch_queries(const Plan &p, const Call &a, const Grads &g, const Shares &shares, hipStream_t st) {
+    const dim3 grid(uint32_t(p.tiles * p.shares * a.kv_heads));
+    if (p.waves == 8) grad_queries<T, D, 8><<<grid, dim3(512), 0, st>>>(a, g, int(p.tiles), shares);
+    else grad_queries<T, D, 4><<<grid, dim3(256), 0, st>>>(a, g, int(p.tiles), shares);
+}
+template <typename T, int D> void launch_keys(const Plan &p, const Call &a, const Grads &g, const Shares &shares, hipStream_t st) {
+    const dim3 grid(uint32_t(p.tiles * p.shares * a.kv_heads));
+    if (p.waves == 8) grad_keys<T, D, 8><<<grid, dim3(512), 0, st>>>(a, g, int(p.tiles), shares);
+    else grad_keys<T, D, 4><<<grid, dim3(256), 0, st>>>(a, g, int(p.tiles), shares);
+}
+
+template <typename T> void run_forward(const harp_ctx *ctx, const harp_attention *g, unsigned char *ws, hipStream_t st) {
+    const Call a = call_of(g);
+    const Plan p = plan_queries(ctx, g);
+    const Space space = space_for(ctx, g);
+    const Shares shares = {p.shares, reinterpret_cast<float *>(ws + space.sums), reinterpret_cast<float *>(ws + space.stats)};
+    if (g->head <= 64) launch_forward<T, 64>(p, a, shares, st);
+    else if (g->head <= 96) launch_forward<T, 96>(p, a, shares, st);
+    else launch_forward<T, 128>(p, a, shares, st);
+    if (p.shares > 1) {
+        const int64_t tiles = tiles_of(g->tokens_q, a.group, g->batch, kJoinRows);
+        forward_join<T><<<dim3(uint32_t(tiles * a.kv_heads)), dim3(kJoinRows * 32), 0, st>>>(a, int(tiles), shares);
+    }
+}
+
+template <typename T> void run_backward(const harp_ctx *ctx, const harp_attention *g, const harp_attention_grads *d, unsigned char *ws, hipStream_t st) {
+    const Call a = call_of(g);
+    const Space space = space_for(ctx, g);
+    const Grads grads = {d->dO, d->do_token, d->do_step, d->dq_token, d->dq_step, d->dk_token, d->dk_step, d->dv_token, d->dv_step,
+                         d->dQ, d->dK, d->dV, reinterpret_cast<float *>(ws), reinterpret_cast<uint32_t *>(ws + space.peaks), g->scale};
+    const int64_t rows = g->tokens_q * g->heads;
+    float *sums = reinterpret_cast<float *>(ws + space.sums);
+    if (rows) deltas<T><<<dim3(uint32_t(rows < (1 << 20) ? (rows + 15) / 16 : 1 << 16)), dim3(256), 0, st>>>(a, grads);
+    if (Range<T>::kNarrow) {
+        const int64_t of_q = tiles_of(g->tokens_q, g->heads, g->batch, kPeakRows), of_k = tiles_of(g->tokens_k, g->kv_heads, g->batch, kPeakRows);
+        no_peaks<<<dim3(1), dim3(2), 0, st>>>(grads.peaks);
+        find_peaks<T><<<dim3(uint32_t(of_q + of_k)), dim3(256), 0, st>>>(a, grads, int(of_q));
+    }
+    if (d->dQ && rows) {
+        const Plan p = plan_queries(ctx, g);
+        const Shares shares = {p.shares, sums, nullptr};
+        if (g->head <= 64) launch_queries<T, 64>(p, a, grads, shares, st);
+        else if (g->head <= 96) launch_queries<T, 96>(p, a, grads, shares, st);
+        else launch_queries<T, 128>(p, a, grads, shares, st);
+        if (p.shares > 1)
+            join_sums<T><<<dim3(uint32_t(tiles_of(g->tokens_q, g->heads, g->batch, kJoinRows))), dim3(kJoinRows * 32), 0, st>>>(
+                a.q_begin, a.tokens_q, a.batch, a.heads, a.head, sums, p.shares, rows * a.head, static_cast<T *>(d->dQ), d->dq_token, d->dq_step);
+    }
+    if ((d->dK || d->dV) && g->tokens_k) {
+        const Plan p = plan_keys(ctx, g);
+        const Shares shares = {p.shares, sums, nullptr};
+        if (g->head <= 64) launch_keys<T, 64>(p, a, grads, shares, st);
+        else if (g->head <= 96) launch_keys<T, 96>(p, a, grads, shares, st);
+        else launch_keys<T, 128>(p, a, grads, shares, st);
+        if (p.shares > 1) {
+            const int64_t each = a.tokens_k * a.kv_heads * a.head;
+            const dim3 grid(uint32_t(tiles_of(g->tokens_k, g->kv_heads, g->batch, kJoinRows))), block(kJoinRows * 32);
+            if (d->dK) join_sums<T><<<grid, block, 0, st>>>(a.k_begin, a.tokens_k, a.batch, a.kv_heads, a.head, sums, p.shares, 2 * each, static_cast<T *>(d->dK), d->dk_token, d->dk_step);
+            if (d->dV) join_sums<T><<<grid, block, 0, st>>>(a.k_begin, a.tokens_k, a.batch, a.kv_heads, a.head, sums + each, p.shares, 2 * each, static_cast<T *>(d->dV), d->dv_token, d->dv_step);
+        }
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t harp_attention_workspace_bytes(harp_ctx *ctx, const harp_attention *g) {
+    if (!ctx || !g || attention_sizes(ctx, g) != HARP_OK) return 0;
+    return space_for(ctx, g).all;
+}
+
+int harp_attention_forward(harp_ctx *ctx, const harp_attention *g, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    if (!ctx) return HARP_ERR_INVALID_ARG;
+    if (!g) return fail(ctx, HARP_ERR_INVALID_ARG, "null args");
+    const bool some = g->tokens_q > 0;
+    const Tensor t[] = {{"Q", g->Q, g->tokens_q, g->heads, g->q_token, g->q_step, true, false},
+                        {"K", g->K, some ? g->tokens_k : 0, g->kv_heads, g->k_token, g->k_step, true, false},
+                        {"V", g->V, some ? g->tokens_k : 0, g->kv_heads, g->v_token, g->v_step, true, false},
+                        {"O", g->O, g->tokens_q, g->heads, g->o_token, g->o_step, true, true}};
+    const int rc = check(ctx, g, t, 4, workspace, workspace_bytes);
+    if (rc != HARP_OK || !some) return rc;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (g->type == HARP_BF16) run_forward<__bf16>(ctx, g, static_cast<unsigned char *>(workspace), st);
+    else run_forward<_Float16>(ctx, g, static_cast<unsigned char *>(workspace), st);
+    return launched(ctx);
+}
+
+int harp_attention_backward(harp_ctx *ctx, const harp_attention *g, const harp_attention_grads *d, void *workspace, size_t workspace_bytes,
+                            void *hip_stream) {
+    if (!ctx) return HARP_ERR_INVALID_ARG;
+    if (!g || !d) return fail(ctx, HARP_ERR_INVALID_ARG, "null args");
+    if (!g->lse && g->tokens_q > 0) return fail(ctx, HARP_ERR_INVALID_ARG, "null lse");
+    const Tensor t[] = {{"Q", g->Q, g->tokens_q, g->heads, g->q_token, g->q_step, true, false},
+                        {"K", g->K, g->tokens_k, g->kv_heads, g->k_token, g->k_step, true, false},
+                        {"V", g->V, g->tokens_k, g->kv_heads, g->v_token, g->v_step, true, false},
+                        {"O", g->O, g->tokens_q, g->heads, g->o_token, g->o_step, true, false},
+                        {"dO", d->dO, g->tokens_q, g->heads, d->do_token, d->do_step, true, false},
+                        {"dQ", d->dQ, g->tokens_q, g->heads, d->dq_token, d->dq_step, false, true},
+                        {"dK", d->dK, g->tokens_k, g->kv_heads, d->dk_token, d->dk_step, false, true},
+                        {"dV", d->dV, g->tokens_k, g->kv_heads, d->dv_token, d->dv_step, false, true}};
+    const int rc = check(ctx, g, t, 8, workspace, workspace_bytes);
+    if (rc != HARP_OK) return rc;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (g->type == HARP_BF16) run_backward<__bf16>(ctx, g, d, static_cast<unsigned char *>(workspace), st);
+    else run_backward<_Float16>(ctx, g, d, static_cast<unsigned char *>(workspace), st);
+    return launched(ctx);
+}
+
+}  // extern "C"

@@ -18,6 +18,7 @@ GATE_LINEAR, GATE_SIGMOID = 0, 1
 ROTARY_HALF, ROTARY_INTERLEAVED = 0, 1
 SCALING_NONE, SCALING_LINEAR, SCALING_NTK, SCALING_BY_PARTS = range(4)
 NORM_MAX_COLS = 8192
+ATTENTION_MAX_HEAD = 128
 _ACTS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
 _NORMS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
 _LAYOUTS = {"half": ROTARY_HALF, "interleaved": ROTARY_INTERLEAVED}
@@ -423,6 +424,69 @@ def harp_rotary(ctx: Context, x, y, frequencies, positions=None, first=0, period
                          _vector(ctx, frequencies, turned // 2, torch.float64, "frequencies"),
                          _vector(ctx, positions, shape[0], torch.int64, "positions"), first, period)
     ctx.check(ctx.lib.harp_rotary(ctx.handle, C.byref(a), _stream(ctx, stream, (x, y, frequencies, positions))))
+
+
+class harp_attention(C.Structure):
+    _fields_ = [("tokens_q", C.c_int64), ("tokens_k", C.c_int64), ("batch", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head", C.c_int32), ("type", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float), ("q_begin", C.c_void_p),
+                ("k_begin", C.c_void_p), ("k_count", C.c_void_p), ("Q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p),
+                ("q_token", C.c_int64), ("q_step", C.c_int64), ("k_token", C.c_int64), ("k_step", C.c_int64), ("v_token", C.c_int64),
+                ("v_step", C.c_int64), ("O", C.c_void_p), ("o_token", C.c_int64), ("o_step", C.c_int64), ("lse", C.c_void_p)]
+
+
+class harp_attention_grads(C.Structure):
+    _fields_ = [("dO", C.c_void_p), ("do_token", C.c_int64), ("do_step", C.c_int64), ("dQ", C.c_void_p), ("dK", C.c_void_p),
+                ("dV", C.c_void_p), ("dq_token", C.c_int64), ("dq_step", C.c_int64), ("dk_token", C.c_int64), ("dk_step", C.c_int64),
+                ("dv_token", C.c_int64), ("dv_step", C.c_int64)]
+
+
+def attention_workspace(ctx: Context, tokens_q: int, tokens_k: int, batch: int, heads: int, kv_heads: int, head: int):
+    """What harp_attention_forward and harp_attention_backward need for Q [tokens_q][heads][head] and K [tokens_k][kv_heads][head]."""
+    a = harp_attention(tokens_q, tokens_k, batch, heads, kv_heads, head)
+    size = ctx.lib.harp_attention_workspace_bytes(ctx.handle, C.byref(a))
+    if size == 0:
+        raise HarpError(ERR_SHAPE, ctx.lib.harp_last_error(ctx.handle).decode())
+    return _torch().empty(size, dtype=_torch().uint8, device=ctx.device)
+
+
+def _attention(ctx, q, k, v, o, lse, q_begin, k_begin, k_count, batch, causal, scale):
+    for t, name in ((q, "q"), (k, "k")):
+        _three(t, name)
+    torch, t = _torch(), q.dtype
+    (tq, heads, head), (tk, kv_heads, _) = q.shape, k.shape
+    for begin, name in ((q_begin, "q_begin"), (k_begin, "k_begin")):
+        if begin is not None:
+            if batch is not None and batch != begin.numel() - 1:
+                raise HarpError(ERR_SHAPE, "%s has %d entries for %d sequences" % (name, begin.numel(), batch))
+            batch = begin.numel() - 1
+    batch = 1 if batch is None else batch
+    i32, of_k = torch.int32, (tk, kv_heads, head)
+    qp, kp, vp, op = (_heads(ctx, x, s, t, n) for x, s, n in ((q, q.shape, "q"), (k, of_k, "k"), (v, of_k, "v"), (o, q.shape, "o")))
+    return harp_attention(tq, tk, batch, heads, kv_heads, head, _type(q, (BF16, F16)), int(bool(causal)),
+                          head ** -0.5 if scale is None else scale, _vector(ctx, q_begin, batch + 1, i32, "q_begin"),
+                          _vector(ctx, k_begin, batch + 1, i32, "k_begin"), _vector(ctx, k_count, batch, i32, "k_count"),
+                          qp[0], kp[0], vp[0], *qp[1:], *kp[1:], *vp[1:], *op, _vector(ctx, lse, heads * tq, torch.float32, "lse"))
+
+
+def harp_attention_forward(ctx: Context, q, k, v, o, lse=None, q_begin=None, k_begin=None, k_count=None, batch=None, causal=False, scale=None,
+                           workspace=None, stream=None):
+    """o = softmax(scale q k^T) v per sequence and head; see include/harp.h.  q, o: [tokens][heads][head], k, v:
+    [tokens][kv heads][head]; begins: int32 [sequences + 1] on the GPU, or None: `batch` (1) sequences of equal length; k_count:
+    int32 [sequences], the keys that each uses; lse: float32 [heads][tokens], or None; scale: head^-0.5 if None."""
+    a = _attention(ctx, q, k, v, o, lse, q_begin, k_begin, k_count, batch, causal, scale)
+    tensors = (q, k, v, o, lse, q_begin, k_begin, k_count, workspace)
+    ctx.check(ctx.lib.harp_attention_forward(ctx.handle, C.byref(a), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))
+
+
+def harp_attention_backward(ctx: Context, q, k, v, o, lse, do, dq, dk, dv, q_begin=None, k_begin=None, k_count=None, batch=None, causal=False,
+                            scale=None, workspace=None, stream=None):
+    """The gradients of harp_attention_forward, given do and what that call wrote; dq, dk, dv may be None; see include/harp.h."""
+    a = _attention(ctx, q, k, v, o, lse, q_begin, k_begin, k_count, batch, causal, scale)
+    t = q.dtype
+    d = [_heads(ctx, x, s, t, n) for x, s, n in ((do, q.shape, "do"), (dq, q.shape, "dq"), (dk, k.shape, "dk"), (dv, k.shape, "dv"))]
+    g = harp_attention_grads(*d[0], d[1][0], d[2][0], d[3][0], *d[1][1:], *d[2][1:], *d[3][1:])
+    tensors = (q, k, v, o, lse, do, dq, dk, dv, q_begin, k_begin, k_count, workspace)
+    ctx.check(ctx.lib.harp_attention_backward(ctx.handle, C.byref(a), C.byref(g), *_workspace(ctx, workspace), _stream(ctx, stream, tensors)))
 
 
 class harp_gated(C.Structure):
