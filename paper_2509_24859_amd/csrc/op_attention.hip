@@ -123,28 +123,51 @@ __device__ __forceinline__ int work_of(int id, int n) {
     return id / kDies + die * each + (die < more ? die : more);
 }
 
-// LDS holds rows of D elements in pieces of 16 bytes, moved within a row so that neither 8 rows read piece by piece nor 4 rows read
-// across (ds_read_tr) meet in the same 128 bytes.
+// LDS holds rows of D elements in pieces of 16 bytes.  It gives 256 bytes a cycle: to 16 lanes that read a piece each, or to 32
+// that read half of one across (ds_read_tr: 4 rows of 4 neighbouring pieces).  Pieces are moved within a row so that neither 16
+// neighbouring rows, one piece of each, nor 4 rows, 4 pieces of each, meet at the same place of 256 bytes.
 template <int D> __device__ __forceinline__ int moved(int row, int piece) {
-    return D == 96 ? piece ^ ((row >> 1 & 1) << 1 | (row >> 2 & 1)) : piece ^ ((row & 3) << 1 | (row >> 2 & 1));
+    if (D == 128) return piece ^ ((row & 3) << 2 | (row >> 2 & 3));
+    if (D == 64) return piece ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
+    return piece ^ (row >> 2 & 3);
 }
-// Fragment of 32 rows by 16 columns: lane l has row l % 32 and columns 16 k + 8 (l / 32) .. + 7.
-template <typename T, int D> __device__ __forceinline__ typename Mfma32<T>::Frag along(const T *lds, int row0, int k) {
-    const int lane = threadIdx.x % kWave, row = row0 + lane % 32;
-    return *reinterpret_cast<const typename Mfma32<T>::Frag *>(lds + row * D + moved<D>(row, 2 * k + lane / 32) * 8);
-}
-// Fragment of 32 columns by 16 rows, transposed: lane l has column col0 + l % 32 and, h = l / 32, rows row0 + 4 h .. + 3 and
+// Fragments of 32 rows by 16 columns: lane l has row l % 32 and columns 16 k + 8 (l / 32) .. + 7.  Only the pieces' low bits are
+// moved, so that a few places do for all k, and the rest is in the instruction.
+template <typename T, int D> struct Along {
+    static constexpr int N = D == 96 ? 2 : D / 16;
+    int at[N];
+    __device__ __forceinline__ Along() {
+        const int lane = threadIdx.x % kWave, row = lane % 32;
+#pragma unroll
+        for (int j = 0; j < N; ++j) at[j] = row * D + moved<D>(row, 2 * j + lane / 32) * 8;
+    }
+    // row0 a multiple of 32
+    __device__ __forceinline__ typename Mfma32<T>::Frag read(const T *lds, int row0, int k) const {
+        return *reinterpret_cast<const typename Mfma32<T>::Frag *>(lds + at[k % N] + row0 * D + k / N * (N * 16));
+    }
+};
+// Fragments of 32 columns by 16 rows, transposed: lane l has column 32 m + l % 32 and, h = l / 32, rows row0 + 4 h .. + 3 and
 // row0 + 8 + 4 h .. + 3.
-template <typename T, int D> __device__ __forceinline__ typename Mfma32<T>::Frag across(const T *lds, int row0, int col0) {
-    typedef __attribute__((address_space(3))) s16x4 *Lds;
-    const int lane = threadIdx.x % kWave, i = lane % 16, col = col0 + lane / 16 % 2 * 16 + i % 4 * 4;
-    const int row = row0 + lane / 32 * 4 + i / 4;
-    const T *lo = lds + row * D + moved<D>(row, col / 8) * 8 + col % 8;
-    const T *hi = lds + (row + 8) * D + moved<D>(row + 8, col / 8) * 8 + col % 8;
-    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)lo), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)hi);
-    const s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-    return __builtin_bit_cast(typename Mfma32<T>::Frag, v);
-}
+template <typename T, int D> struct Across {
+    static constexpr int N = D == 96 ? 1 : D / 32;
+    int at[2][N];
+    __device__ __forceinline__ Across() {
+        const int lane = threadIdx.x % kWave, i = lane % 16, row = lane / 32 * 4 + i / 4;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int up = 0; up < 2; ++up)
+                at[up][j] = (row + 8 * up) * D + moved<D>(row + 8 * up, lane / 16 % 2 * 2 + i % 4 / 2 + 4 * j) * 8 + i % 2 * 4;
+    }
+    // row0 a multiple of 16
+    __device__ __forceinline__ typename Mfma32<T>::Frag read(const T *lds, int row0, int m) const {
+        typedef __attribute__((address_space(3))) s16x4 *Lds;
+        const T *p = lds + row0 * D + m / N * (N * 32);
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + at[0][m % N])), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + at[1][m % N]));
+        const s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_bit_cast(typename Mfma32<T>::Frag, v);
+    }
+};
 
 // 8 elements wherever they lie, or zeros.
 template <typename T> __device__ __forceinline__ typename Mfma32<T>::Frag eight(const T *p, bool there) {
@@ -159,20 +182,37 @@ template <typename T> __device__ __forceinline__ typename Mfma32<T>::Frag eight(
 template <typename T, int D, int ROWS, int THREADS> struct Stage {
     static constexpr int kAll = ROWS * (D / 8), kEach = (kAll + THREADS - 1) / THREADS;
     typename Mfma32<T>::Frag piece[kEach];
+    __device__ __forceinline__ static int row(int i) { return (i * THREADS + int(threadIdx.x)) / (D / 8); }
+    __device__ __forceinline__ static int part(int i) { return (i * THREADS + int(threadIdx.x)) % (D / 8); }
     template <typename At> __device__ __forceinline__ void ask(At at, int limit, int head) {
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
-            const int id = i * THREADS + int(threadIdx.x), row = id / (D / 8), col = id % (D / 8) * 8;
-            const bool there = row < limit && col < head && (kAll % THREADS == 0 || id < kAll);
-            piece[i] = eight<T>(at(there ? row : 0) + (there ? col : 0), there);
+            const bool there = row(i) < limit && part(i) * 8 < head && (kAll % THREADS == 0 || i * THREADS + int(threadIdx.x) < kAll);
+            piece[i] = eight<T>(at(there ? row(i) : 0) + (there ? part(i) * 8 : 0), there);
         }
     }
     __device__ __forceinline__ void put(T *lds) const {
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int id = i * THREADS + int(threadIdx.x), row = id / (D / 8), c = id % (D / 8);
-            if (kAll % THREADS == 0 || id < kAll) *reinterpret_cast<typename Mfma32<T>::Frag *>(lds + row * D + moved<D>(row, c) * 8) = piece[i];
+        for (int i = 0; i < kEach; ++i)
+            if (kAll % THREADS == 0 || i * THREADS + int(threadIdx.x) < kAll)
+                *reinterpret_cast<typename Mfma32<T>::Frag *>(lds + row(i) * D + moved<D>(row(i), part(i)) * 8) = piece[i];
+    }
+};
+// The same of rows `token` apart, tile after tile.
+template <typename T, int D, int ROWS, int THREADS> struct Stream : Stage<T, D, ROWS, THREADS> {
+    typedef Stage<T, D, ROWS, THREADS> Base;
+    const T *at;                     // of this thread's first piece
+    __device__ __forceinline__ void begin(const T *from, int64_t token) { at = from + Base::row(0) * token + Base::part(0) * 8; }
+    // `limit` rows are there, of this tile and those after it
+    __device__ __forceinline__ void ask(int64_t token, int limit, int head) {
+#pragma unroll
+        for (int i = 0; i < Base::kEach; ++i) {
+            const bool there = Base::row(i) < limit && Base::part(i) * 8 < head && (Base::kAll % THREADS == 0 || i * THREADS + int(threadIdx.x) < Base::kAll);
+            const T *p = THREADS % (D / 8) == 0 ? at + i * (THREADS / (D / 8)) * token
+                                                : at + (Base::row(i) - Base::row(0)) * token + (Base::part(i) - Base::part(0)) * 8;
+            Base::piece[i] = eight<T>(p, there);
         }
+        at += ROWS * token;
     }
 };
 
@@ -200,7 +240,7 @@ struct Shares {
     float *sums, *stats;
 };
 
-// WAVES wavefronts of 32 rows; keys go through LDS 64 at a time, two tiles of them.
+// WAVES wavefronts of 32 rows; keys go through LDS 64 at a time, two tiles of them, in steps of 32.
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, Shares shares) {
     constexpr int kThreads = WAVES * kWave, kRows = WAVES * 32;
@@ -231,78 +271,172 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
     const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) q[k] = eight<T>(from + 16 * k + 8 * h, mine.limit >= 0 && 16 * k + 8 * h < a.head);
-    f32x16 o[D / 32] = {};
-    float top = -INFINITY, sum = 0;
+    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
+    const Along<T, D> along;
+    const Across<T, D> across;
+    f32x16 o[D / 32] = {}, p = {}, n = {};
+    Frag w[2] = {};
+    float top = -INFINITY, against = 0, sum = 0, shrink = 1;
 
-    const T *keys = static_cast<const T *>(a.k) + s.k0 * a.k_token + kv * a.k_step;
-    const T *values = static_cast<const T *>(a.v) + s.k0 * a.v_token + kv * a.v_step;
-    Stage<T, D, kKeys, kThreads> sk, sv;
-    auto ask = [&](int t) {
-        sk.ask([&](int row) { return keys + (int64_t(t) * kKeys + row) * a.k_token; }, s.used - t * kKeys, a.head);
-        sv.ask([&](int row) { return values + (int64_t(t) * kKeys + row) * a.v_token; }, s.used - t * kKeys, a.head);
+    const T *keys = static_cast<const T *>(a.k) + (s.k0 + first * kKeys) * a.k_token + kv * a.k_step;
+    const T *values = static_cast<const T *>(a.v) + (s.k0 + first * kKeys) * a.v_token + kv * a.v_step;
+    Stream<T, D, kKeys, kThreads> sk, sv;
+    sk.begin(keys, a.k_token);
+    sv.begin(values, a.v_token);
+    auto ask_k = [&](int t) {
+        if (t < end) sk.ask(a.k_token, s.used - t * kKeys, a.head);
     };
+    auto ask_v = [&](int t) {
+        if (t < end) sv.ask(a.v_token, s.used - t * kKeys, a.head);
+    };
+    // Scores of half a tile of keys; weighted values of one.
+    auto scores = [&](int buffer, int half) {
+        f32x16 x = {};
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) x = Mfma32<T>::run(along.read(lk[buffer], half * 32, k), q[k], x);
+        return x;
+    };
+    auto weigh = [&](int buffer, int half) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int m = 0; m < D / 32; ++m) o[m] = Mfma32<T>::run(across.read(lv[buffer], half * 32 + 16 * k, m), w[k], o[m]);
+    };
+    // Of step i's scores p: hides what a row does not see; the reference that exponents are taken against follows the maximum only
+    // when that has grown by 2^8 over it (sums in 32 bits and weights of 16 have room for the factor), and o has then to
+    // be shrunk once the weights of the step before are in it.
+    auto hide = [&](int i, f32x16 &p) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (i * 32 + 8 * (j / 4) + 4 * h + j % 4 >= mine.limit) p[j] = -INFINITY;
+    };
+    auto refer = [&](const f32x16 &p) -> bool {
+        float high = p[0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) high = fmaxf(high, p[j]);
+        high *= a.c;
+        if (!__any(high > top + 8.0f)) return false;
+        high = fmaxf(fmaxf(high, other_half(high)), top);
+        shrink = top == high ? 1.0f : __builtin_amdgcn_exp2f(top - high);
+        top = high;
+        against = top == -INFINITY ? 0.0f : top;
+        sum *= shrink;
+        return true;
+    };
+    auto weights = [&](f32x16 &p, Frag (&x)[2]) {
+        float part = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            p[j] = __builtin_amdgcn_exp2f(fmaf(p[j], a.c, -against));
+            if (j % 2) part += p[j];
+            else sum += p[j];
+            x[j / 8][j % 8] = T(p[j]);
+        }
+        sum += part;
+    };
+    auto shrink_o = [&] {
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m) o[m] *= shrink;
+    };
+    // A step's weights, while the matrix instructions make the next step's scores and the sum of the last one's weighted values.
+    // Tile t's scores are made a step ahead, its weighted values a step behind, so K of a tile is in LDS a barrier before V.
+    const int steps = min(2 * end, (wave_most + 31) / 32);       // of this wavefront
+    // Written in the order in which it is to be issued: two matrix instructions, arithmetic that takes about as long, reads for the
+    // pair after the next; the fences keep the compiler from sorting by kind (943 TFLOP/s at 4,096 x 4,096, not causal).
+    auto step = [&](int k_buffer, int v_buffer, int half, f32x16 &now, f32x16 &next) {
+        constexpr int kPairs = D / 16, kAhead = 2;
+        Frag kf[kAhead + 1], vf[kAhead + 1], x[2];
+        auto read = [&](int j) {
+            kf[j % (kAhead + 1)] = along.read(lk[k_buffer], half * 32, j);
+            vf[j % (kAhead + 1)] = across.read(lv[v_buffer], half * 32 + j / (D / 32) * 16, j % (D / 32));
+        };
+        auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) read(j);
+        fence();
+        int grown = __builtin_amdgcn_readfirstlane(refer(now));
+        asm volatile("" : "+s"(grown));                          // so that there is one copy of what follows, not one for either case
+        float part = 0;
+        auto summed = [&](int e) {                               // of exponentials
+            if (e % 2) part += now[e];
+            else sum += now[e];
+            x[e / 8][e % 8] = T(now[e]);
+        };
+        fence();
+#pragma unroll
+        for (int j = 0; j < kPairs; ++j) {
+            const int from = 16 * j / kPairs, to = 16 * (j + 1) / kPairs, before = 16 * (j - 1) / kPairs;
+            next = Mfma32<T>::run(kf[j % (kAhead + 1)], q[j], j ? next : f32x16{});
+#pragma unroll
+            for (int e = from; e < to; ++e) now[e] = __builtin_amdgcn_exp2f(fmaf(now[e], a.c, -against));
+            fence();
+            o[j % (D / 32)] = Mfma32<T>::run(vf[j % (kAhead + 1)], w[j / (D / 32)], o[j % (D / 32)]);
+            if (j + kAhead < kPairs) read(j + kAhead);
+            if (j > 0) {
+#pragma unroll
+                for (int e = before; e < from; ++e) summed(e);
+            }
+            fence();
+        }
+#pragma unroll
+        for (int e = 16 * (kPairs - 1) / kPairs; e < 16; ++e) summed(e);
+        sum += part;
+        w[0] = x[0], w[1] = x[1];
+        asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(sum));    // here, not where they are used
+        if (grown) shrink_o();
+    };
+    auto edge = [&](int i, f32x16 &now, f32x16 &next) {          // a step that lacks one of these, or hides keys
+        if (i > steps) return;
+        if (i + 1 < steps) next = scores((i + 1) / 2 - first & 1, i + 1 & 1);
+        if (i > 2 * first) weigh((i - 1) / 2 - first & 1, i - 1 & 1);
+        if (i == steps) return;
+        if (32 * i + 32 > wave_least) hide(i, now);
+        if (refer(now)) shrink_o();
+        weights(now, w);
+    };
+    ask_k(first);
+    ask_v(first);
     if (first < end) {
-        ask(first);
         sk.put(lk[0]);
         sv.put(lv[0]);
     }
+    ask_k(first + 1);
+    ask_v(first + 1);
     __syncthreads();
-    for (int t = first; t < end; ++t) {
-        const int at = (t - first) % 2;
-        if (t + 1 < end) ask(t + 1);
-        if (t * kKeys < wave_most) {
-            f32x16 p[2] = {};
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) p[u] = Mfma32<T>::run(along<T, D>(lk[at], 32 * u, k), q[k], p[u]);
-            if ((t + 1) * kKeys > wave_least) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (t * kKeys + 32 * u + 8 * (i / 4) + 4 * h + i % 4 >= mine.limit) p[u][i] = -INFINITY;
-            }
-            float high = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) high = fmaxf(high, p[u][i]);
-            high = fmaxf(high, other_half(high)) * a.c;
-            // The reference that exponents are taken against follows the maximum only when that has grown by 2^8 over it:
-            // sums in 32 bits and weights of 16 have room for the factor.
-            if (__any(high > top + 8.0f)) {
-                const float next = fmaxf(high, top), shrink = top == next ? 1.0f : __builtin_amdgcn_exp2f(top - next);
-                top = next;
-                sum *= shrink;
-#pragma unroll
-                for (int m = 0; m < D / 32; ++m) o[m] *= shrink;
-            }
-            const float against = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    p[u][i] = __builtin_amdgcn_exp2f(fmaf(p[u][i], a.c, -against));
-                    sum += p[u][i];
-                }
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    Frag w;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = T(p[u][8 * k + i]);
-#pragma unroll
-                    for (int m = 0; m < D / 32; ++m) o[m] = Mfma32<T>::run(across<T, D>(lv[at], 32 * u + 16 * k, 32 * m), w, o[m]);
-                }
-        }
-        if (t + 1 < end) {
-            sk.put(lk[1 - at]);
-            sv.put(lv[1 - at]);
-        }
+    if (2 * first < steps) p = scores(0, 0);
+    // A tile that lies in `buffer`; the next one's K is put behind its first step, V behind the barrier.
+    auto whole = [&](int t, int buffer) {
+        step(buffer, 1 - buffer, 1, p, n);
+        sk.put(lk[1 - buffer]);
+        ask_k(t + 2);
         __syncthreads();
+        sv.put(lv[1 - buffer]);
+        ask_v(t + 2);
+        step(1 - buffer, buffer, 0, n, p);
+    };
+    auto partial = [&](int t) {
+        const int next = t + 1 - first & 1;
+        edge(2 * t, p, n);
+        if (t + 1 < end) sk.put(lk[next]);
+        ask_k(t + 2);
+        __syncthreads();
+        if (t + 1 < end) sv.put(lv[next]);
+        ask_v(t + 2);
+        edge(2 * t + 1, n, p);
+    };
+    // Loops of their own: the compiler merges what two branches of one have in common, and then nothing goes on meanwhile.  A whole
+    // tile has another behind it and hides nothing.
+    const int whole_end = min(end - 1, min((steps - 1) / 2, wave_least / kKeys));
+    int t = first;
+    if (t < end) partial(t++);
+#pragma unroll 1
+    for (; t + 1 < whole_end; t += 2) {
+        whole(t, 1);
+        whole(t + 1, 0);
     }
+#pragma unroll 1
+    for (; t < end; ++t) partial(t);
+    if (first < end) edge(2 * end, p, n);                        // the last weighted values
     if (mine.limit < 0) return;
     sum += other_half(sum);
     if (shares.count > 1) {
@@ -475,6 +609,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
         q[k] = eight<T>(from + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
         d_o[k] = eight<T>(from_do + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
     }
+    const Along<T, D> along;
+    const Across<T, D> across;
     f32x16 dq[D / 32] = {};
     const T *keys = static_cast<const T *>(a.k) + s.k0 * a.k_token + kv * a.k_step;
     const T *values = static_cast<const T *>(a.v) + s.k0 * a.v_token + kv * a.v_step;
@@ -499,8 +635,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
                 f32x16 p = {}, dp = {};
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k) {
-                    p = Mfma32<T>::run(along<T, D>(lk[at], 32 * u, k), q[k], p);
-                    dp = Mfma32<T>::run(along<T, D>(lv[at], 32 * u, k), d_o[k], dp);
+                    p = Mfma32<T>::run(along.read(lk[at], 32 * u, k), q[k], p);
+                    dp = Mfma32<T>::run(along.read(lv[at], 32 * u, k), d_o[k], dp);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * range.less(dp[i], delta);
@@ -515,7 +651,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
 #pragma unroll
                     for (int i = 0; i < 8; ++i) w[i] = T(p[8 * k + i]);
 #pragma unroll
-                    for (int m = 0; m < D / 32; ++m) dq[m] = Mfma32<T>::run(across<T, D>(lk[at], 32 * u + 16 * k, 32 * m), w, dq[m]);
+                    for (int m = 0; m < D / 32; ++m) dq[m] = Mfma32<T>::run(across.read(lk[at], 32 * u + 16 * k, m), w, dq[m]);
                 }
             }
         }
@@ -573,6 +709,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         k[i] = eight<T>(from_k + 16 * i + 8 * h, used && 16 * i + 8 * h < a.head);
         v[i] = eight<T>(from_v + 16 * i + 8 * h, used && 16 * i + 8 * h < a.head);
     }
+    const Along<T, D> along;
+    const Across<T, D> across;
     f32x16 dk[D / 32] = {}, dv[D / 32] = {};
     Stage<T, D, kBack, kThreads> sq, sd;
     const Range<T> range(g.peaks);
@@ -611,8 +749,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         f32x16 p = {}, dp = {};
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
-            p = Mfma32<T>::run(along<T, D>(lq[at], 0, i), k[i], p);
-            dp = Mfma32<T>::run(along<T, D>(ld[at], 0, i), v[i], dp);
+            p = Mfma32<T>::run(along.read(lq[at], 0, i), k[i], p);
+            dp = Mfma32<T>::run(along.read(ld[at], 0, i), v[i], dp);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -634,8 +772,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
             for (int j = 0; j < 8; ++j) w[j] = T(p[8 * i + j]), ds[j] = T(dp[8 * i + j]);
 #pragma unroll
             for (int m = 0; m < D / 32; ++m) {
-                dv[m] = Mfma32<T>::run(across<T, D>(ld[at], 16 * i, 32 * m), w, dv[m]);
-                dk[m] = Mfma32<T>::run(across<T, D>(lq[at], 16 * i, 32 * m), ds, dk[m]);
+                dv[m] = Mfma32<T>::run(across.read(ld[at], 16 * i, m), w, dv[m]);
+                dk[m] = Mfma32<T>::run(across.read(lq[at], 16 * i, m), ds, dk[m]);
             }
         }
         if (t + 1 < end) put(1 - at);
