@@ -9,6 +9,9 @@
 // 4 h .. 4 h + 3, 8 + 4 h .. 11 + 4 h for lane half h, in which V^T is read too.
 #include <math.h>
 
+#include <type_traits>
+#include <utility>
+
 #include "harp_ctx.h"
 #include "ops_common.h"
 
@@ -131,39 +134,38 @@ template <int D> __device__ __forceinline__ int moved(int row, int piece) {
     if (D == 64) return piece ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
     return piece ^ (row >> 2 & 3);
 }
-// Fragments of 32 rows by 16 columns: lane l has row l % 32 and columns 16 k + 8 (l / 32) .. + 7.  Only the pieces' low bits are
-// moved, so that a few places do for all k, and the rest is in the instruction.
+// Fragments of 32 rows by 16 columns: lane l has row l % 32 and columns 16 k + 8 (l / 32) .. + 7.  Only low bits of a place in the
+// row are moved: another k is another place by those bits, the rest is in the instruction.  refresh(): the places are not kept in
+// registers over it.
 template <typename T, int D> struct Along {
     static constexpr int N = D == 96 ? 2 : D / 16;
-    int at[N];
+    uint32_t at;                     // bytes
     __device__ __forceinline__ Along() {
         const int lane = threadIdx.x % kWave, row = lane % 32;
-#pragma unroll
-        for (int j = 0; j < N; ++j) at[j] = row * D + moved<D>(row, 2 * j + lane / 32) * 8;
+        at = uint32_t(row * D + moved<D>(row, lane / 32) * 8) * 2;
     }
+    __device__ __forceinline__ void refresh() { asm volatile("" : "+v"(at)); }
     // row0 a multiple of 32
     __device__ __forceinline__ typename Mfma32<T>::Frag read(const T *lds, int row0, int k) const {
-        return *reinterpret_cast<const typename Mfma32<T>::Frag *>(lds + at[k % N] + row0 * D + k / N * (N * 16));
+        return *reinterpret_cast<const typename Mfma32<T>::Frag *>(reinterpret_cast<const char *>(lds + row0 * D + k / N * (N * 16)) + (at ^ uint32_t(k % N * 32)));
     }
 };
 // Fragments of 32 columns by 16 rows, transposed: lane l has column 32 m + l % 32 and, h = l / 32, rows row0 + 4 h .. + 3 and
 // row0 + 8 + 4 h .. + 3.
 template <typename T, int D> struct Across {
     static constexpr int N = D == 96 ? 1 : D / 32;
-    int at[2][N];
+    uint32_t at;
     __device__ __forceinline__ Across() {
         const int lane = threadIdx.x % kWave, i = lane % 16, row = lane / 32 * 4 + i / 4;
-#pragma unroll
-        for (int j = 0; j < N; ++j)
-#pragma unroll
-            for (int up = 0; up < 2; ++up)
-                at[up][j] = (row + 8 * up) * D + moved<D>(row + 8 * up, lane / 16 % 2 * 2 + i % 4 / 2 + 4 * j) * 8 + i % 2 * 4;
+        at = uint32_t(row * D + moved<D>(row, lane / 16 % 2 * 2 + i % 4 / 2) * 8 + i % 2 * 4) * 2;
     }
-    // row0 a multiple of 16
+    __device__ __forceinline__ void refresh() { asm volatile("" : "+v"(at)); }
+    // row0 a multiple of 16; a row 8 further on has its pieces moved by 2 more
     __device__ __forceinline__ typename Mfma32<T>::Frag read(const T *lds, int row0, int m) const {
         typedef __attribute__((address_space(3))) s16x4 *Lds;
-        const T *p = lds + row0 * D + m / N * (N * 32);
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + at[0][m % N])), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + at[1][m % N]));
+        const char *p = reinterpret_cast<const char *>(lds + row0 * D + m / N * (N * 32));
+        const uint32_t lo = at ^ uint32_t(m % N * 64), hi = lo ^ 32;
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + lo)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 16 * D + hi));
         const s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         return __builtin_bit_cast(typename Mfma32<T>::Frag, v);
     }
@@ -215,6 +217,10 @@ template <typename T, int D, int ROWS, int THREADS> struct Stream : Stage<T, D, 
         at += ROWS * token;
     }
 };
+
+// call(0) .. call(N - 1) written out, the number known to the compiler.
+template <typename F, int... I> __device__ __forceinline__ void written_out(F call, std::integer_sequence<int, I...>) { (call(std::integral_constant<int, I>()), ...); }
+template <int N, typename F> __device__ __forceinline__ void written_out(F call) { written_out(call, std::make_integer_sequence<int, N>()); }
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 
@@ -609,58 +615,83 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
         q[k] = eight<T>(from + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
         d_o[k] = eight<T>(from_do + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
     }
-    const Along<T, D> along;
-    const Across<T, D> across;
+    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
+    Along<T, D> along;
+    Across<T, D> across;
     f32x16 dq[D / 32] = {};
-    const T *keys = static_cast<const T *>(a.k) + s.k0 * a.k_token + kv * a.k_step;
-    const T *values = static_cast<const T *>(a.v) + s.k0 * a.v_token + kv * a.v_step;
-    Stage<T, D, kKeys, kThreads> sk, sv;
+    const T *keys = static_cast<const T *>(a.k) + (s.k0 + first * kKeys) * a.k_token + kv * a.k_step;
+    const T *values = static_cast<const T *>(a.v) + (s.k0 + first * kKeys) * a.v_token + kv * a.v_step;
+    Stream<T, D, kKeys, kThreads> sk, sv;
+    sk.begin(keys, a.k_token);
+    sv.begin(values, a.v_token);
     auto ask = [&](int t) {
-        sk.ask([&](int row) { return keys + (int64_t(t) * kKeys + row) * a.k_token; }, s.used - t * kKeys, a.head);
-        sv.ask([&](int row) { return values + (int64_t(t) * kKeys + row) * a.v_token; }, s.used - t * kKeys, a.head);
+        if (t >= end) return;
+        sk.ask(a.k_token, s.used - t * kKeys, a.head);
+        sv.ask(a.v_token, s.used - t * kKeys, a.head);
     };
+    // A tile's matrix instructions, one operand of each from LDS, and what goes on under them:
+    //   S of the first 32 keys;  their dP, exponentials;  S of the others, dS of the first;  dP, exponentials;  dQ of the first,
+    //   dS of the others;  dQ of those.
+    constexpr int kPart = D / 16, kAhead = 2;
+    auto tile_of_keys = [&](int t, int buffer, auto masked) {
+        f32x16 p[2], dp[2];
+        Frag f[kAhead + 1], w[2][2];
+        auto read = [&](auto n) {
+            constexpr int part = n / kPart, j = n % kPart;
+            Frag &to = f[n % (kAhead + 1)];
+            if (part < 4) to = along.read(part % 2 ? lv[buffer] : lk[buffer], part / 2 * 32, j);
+            else to = across.read(lk[buffer], (part - 4) * 32 + j / (D / 32) * 16, j % (D / 32));
+        };
+        auto exponential = [&](int u, int e) { p[u][e] = __builtin_amdgcn_exp2f(fmaf(p[u][e], a.c, -lse)); };
+        auto gradient = [&](int u, int e) {
+            float ds = p[u][e] * range.less(dp[u][e], delta);
+            if (masked.value && t * kKeys + 32 * u + 8 * (e / 4) + 4 * h + e % 4 >= limit) ds = 0;
+            w[u][e / 8][e % 8] = T(ds);
+        };
+        written_out<kAhead>(read);
+        written_out<6 * kPart>([&](auto n) {
+            constexpr int part = n / kPart, j = n % kPart, from = 16 * j / kPart, to = 16 * (j + 1) / kPart;
+            const Frag &x = f[n % (kAhead + 1)];
+            if constexpr (part == 0 || part == 2) p[part / 2] = Mfma32<T>::run(x, q[j], j ? p[part / 2] : f32x16{});
+            else if constexpr (part == 1 || part == 3) dp[part / 2] = Mfma32<T>::run(x, d_o[j], j ? dp[part / 2] : f32x16{});
+            else dq[j % (D / 32)] = Mfma32<T>::run(x, w[part - 4][j / (D / 32)], dq[j % (D / 32)]);
+            if constexpr (n + kAhead < 6 * kPart) read(std::integral_constant<int, n + kAhead>());
+#pragma unroll
+            for (int e = from; e < to; ++e) {
+                if (part == 1 || part == 3) exponential(part / 2, e);
+                if (part == 2) gradient(0, e);
+                if (part == 4) gradient(1, e);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    ask(first);
     if (first < end) {
-        ask(first);
         sk.put(lk[0]);
         sv.put(lv[0]);
     }
+    ask(first + 1);
     __syncthreads();
-    for (int t = first; t < end; ++t) {
-        const int at = (t - first) % 2;
-        if (t + 1 < end) ask(t + 1);
-        if (t * kKeys < wave_most) {
-            const bool masked = (t + 1) * kKeys > wave_least;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                f32x16 p = {}, dp = {};
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) {
-                    p = Mfma32<T>::run(along.read(lk[at], 32 * u, k), q[k], p);
-                    dp = Mfma32<T>::run(along.read(lv[at], 32 * u, k), d_o[k], dp);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(p[i], a.c, -lse)) * range.less(dp[i], delta);
-                if (masked) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (t * kKeys + 32 * u + 8 * (i / 4) + 4 * h + i % 4 >= limit) p[i] = 0;
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    Frag w;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) w[i] = T(p[8 * k + i]);
-#pragma unroll
-                    for (int m = 0; m < D / 32; ++m) dq[m] = Mfma32<T>::run(across.read(lk[at], 32 * u + 16 * k, m), w, dq[m]);
-                }
-            }
-        }
+    const int whole = min(end, wave_least / kKeys);              // tiles of which nothing is hidden
+    auto turn = [&](int t, int buffer, auto masked) {
+        along.refresh();
+        across.refresh();
+        if (t * kKeys < wave_most) tile_of_keys(t, buffer, masked);
         if (t + 1 < end) {
-            sk.put(lk[1 - at]);
-            sv.put(lv[1 - at]);
+            sk.put(lk[1 - buffer]);
+            sv.put(lv[1 - buffer]);
         }
+        ask(t + 2);
         __syncthreads();
+    };
+    int t = first;
+#pragma unroll 1
+    for (; t + 1 < whole; t += 2) {
+        turn(t, 0, std::false_type());
+        turn(t + 1, 1, std::false_type());
     }
+#pragma unroll 1
+    for (; t < end; ++t) turn(t, t - first & 1, std::true_type());
     if (!here) return;
     const float scale = g.scale * range.back();
     float *sums = shares.sums + ((int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head) * a.head;
@@ -686,6 +717,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
     typedef typename Mfma32<T>::Frag Frag;
     __shared__ __align__(16) T lq[2][kBack * D];
     __shared__ __align__(16) T ld[2][kBack * D];
+    __shared__ __align__(16) T lv[kCols * D];
     __shared__ __align__(16) float l_lse[2][kBack], l_delta[2][kBack];
     __shared__ __align__(16) int l_limit[2][kBack];
     const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, kv = work / shares.count / tiles;
@@ -701,16 +733,18 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
     const int64_t begin_row = int64_t(skip) * a.group;
     const int all = key0 < s.used && begin_row < rows ? int((rows - begin_row + kBack - 1) / kBack) : 0, row_first = int(begin_row);
     const int first = int(int64_t(all) * share / shares.count), end = int(int64_t(all) * (share + 1) / shares.count);
-    Frag k[D / 16], v[D / 16];
+    Frag k[D / 16];
     const T *from_k = static_cast<const T *>(a.k) + (s.k0 + (used ? key : 0)) * a.k_token + kv * a.k_step;
-    const T *from_v = static_cast<const T *>(a.v) + (s.k0 + (used ? key : 0)) * a.v_token + kv * a.v_step;
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) {
-        k[i] = eight<T>(from_k + 16 * i + 8 * h, used && 16 * i + 8 * h < a.head);
-        v[i] = eight<T>(from_v + 16 * i + 8 * h, used && 16 * i + 8 * h < a.head);
+    for (int i = 0; i < D / 16; ++i) k[i] = eight<T>(from_k + 16 * i + 8 * h, used && 16 * i + 8 * h < a.head);
+    {   // V stays in LDS: dK and dV leave no room for it in registers
+        Stage<T, D, kCols, kThreads> sv;
+        const T *values = static_cast<const T *>(a.v) + (s.k0 + key0) * a.v_token + kv * a.v_step;
+        sv.ask([&](int row) { return values + row * a.v_token; }, s.used - key0, a.head);
+        sv.put(lv);
     }
-    const Along<T, D> along;
-    const Across<T, D> across;
+    Along<T, D> along;
+    Across<T, D> across;
     f32x16 dk[D / 32] = {}, dv[D / 32] = {};
     Stage<T, D, kBack, kThreads> sq, sd;
     const Range<T> range(g.peaks);
@@ -727,10 +761,11 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         if (threadIdx.x < kBack) {
             const Row r = row_of(a, s, kv, r0 + int(threadIdx.x));
             const bool there = r.limit >= 0;
-            lse = there ? a.lse[r.head * a.tokens_q + r.token] * kLog2e : 0;
+            // of no row, or one that saw no key: infinity, against which every weight is 0
+            lse = there ? a.lse[r.head * a.tokens_q + r.token] * kLog2e - Range<T>::kShift : INFINITY;
+            lse = lse == -INFINITY ? INFINITY : lse;
             delta = there ? g.delta[r.head * a.tokens_q + r.token] * range.factor : 0;
-            limit = there && lse != -INFINITY ? r.limit : 0;
-            lse = lse == -INFINITY ? 0 : lse - Range<T>::kShift;
+            limit = r.limit;
         }
     };
     auto put = [&](int at) {
@@ -743,41 +778,68 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         put(0);
     }
     __syncthreads();
+    // A step's matrix instructions and what goes on under them:  S;  dP, weights;  dV, their gradients;  dK.
+    constexpr int kPart = D / 16, kAhead = 2;
+    auto rows_step = [&](int at, bool masked) {
+        f32x16 p, dp;
+        Frag f[kAhead + 1], v[kAhead + 1], w[2], ds[2];
+        auto read = [&](auto n) {
+            constexpr int part = n / kPart, j = n % kPart;
+            Frag &to = f[n % (kAhead + 1)];
+            if (part < 2) to = along.read(part ? ld[at] : lq[at], 0, j);
+            else to = across.read(part == 2 ? ld[at] : lq[at], j / (D / 32) * 16, j % (D / 32));
+            if (part == 1) v[n % (kAhead + 1)] = along.read(lv, wave * 32, j);
+        };
+        written_out<kAhead>(read);
+        f32x4 against = {}, less = {};
+        written_out<4 * kPart>([&](auto n) {
+            constexpr int part = n / kPart, j = n % kPart, from = 16 * j / kPart, to = 16 * (j + 1) / kPart;
+            const Frag &x = f[n % (kAhead + 1)];
+            if constexpr (part == 2 && j == 0) {
+                if (masked) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (key >= l_limit[at][8 * (e / 4) + 4 * h + e % 4]) p[e] = 0;
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) w[e / 8][e % 8] = T(p[e]);
+            }
+            if constexpr (part == 0) p = Mfma32<T>::run(x, k[j], j ? p : f32x16{});
+            else if constexpr (part == 1) dp = Mfma32<T>::run(x, v[n % (kAhead + 1)], j ? dp : f32x16{});
+            else if constexpr (part == 2) dv[j % (D / 32)] = Mfma32<T>::run(x, w[j / (D / 32)], dv[j % (D / 32)]);
+            else dk[j % (D / 32)] = Mfma32<T>::run(x, ds[j / (D / 32)], dk[j % (D / 32)]);
+            if constexpr (n + kAhead < 4 * kPart) read(std::integral_constant<int, n + kAhead>());
+#pragma unroll
+            for (int e = from; e < to; ++e) {
+                if (part == 1) {
+                    if (e % 4 == 0) against = *reinterpret_cast<const f32x4 *>(&l_lse[at][8 * (e / 4) + 4 * h]);
+                    p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.c, -against[e % 4]));
+                }
+                if (part == 2) {
+                    if (e % 4 == 0) less = *reinterpret_cast<const f32x4 *>(&l_delta[at][8 * (e / 4) + 4 * h]);
+                    float x = p[e] * range.less(dp[e], less[e % 4]);
+                    ds[e / 8][e % 8] = T(x);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+    // Under the causal order the first rows may see none or not all of the wavefront's keys.
+    const int64_t none = a.causal ? int64_t(key0 + wave * 32 - s.used + s.nq) * a.group : 0, some = a.causal ? none + 31 * a.group : 0;
+#pragma unroll 1
     for (int t = first; t < end; ++t) {
-        const int at = (t - first) % 2;
+        const int at = t - first & 1;
         if (t + 1 < end) ask(t + 1);
-        f32x16 p = {}, dp = {};
-#pragma unroll
-        for (int i = 0; i < D / 16; ++i) {
-            p = Mfma32<T>::run(along.read(lq[at], 0, i), k[i], p);
-            dp = Mfma32<T>::run(along.read(ld[at], 0, i), v[i], dp);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = 8 * i + 4 * h;
-            const f32x4 against = *reinterpret_cast<const f32x4 *>(&l_lse[at][row]), less = *reinterpret_cast<const f32x4 *>(&l_delta[at][row]);
-            const int *seen = &l_limit[at][row];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool on = key < seen[j];
-                const float w = __builtin_amdgcn_exp2f(fmaf(p[4 * i + j], a.c, -against[j]));
-                p[4 * i + j] = on ? w : 0;
-                dp[4 * i + j] = on ? w * range.less(dp[4 * i + j], less[j]) : 0;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            Frag w, ds;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = T(p[8 * i + j]), ds[j] = T(dp[8 * i + j]);
-#pragma unroll
-            for (int m = 0; m < D / 32; ++m) {
-                dv[m] = Mfma32<T>::run(across.read(ld[at], 16 * i, m), w, dv[m]);
-                dk[m] = Mfma32<T>::run(across.read(lq[at], 16 * i, m), ds, dk[m]);
-            }
-        }
+        along.refresh();
+        across.refresh();
+        if (row_first + (t + 1) * kBack > none) rows_step(at, row_first + t * kBack < some);
         if (t + 1 < end) put(1 - at);
         __syncthreads();
+    }
+    // what keys that are not used were given has stayed in their own columns
+    if (!used) {
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m) dk[m] = dv[m] = f32x16{};
     }
     if (key >= s.nk) return;
     const float scale = g.scale * range.back();
