@@ -242,7 +242,7 @@ __device__ __forceinline__ Row row_of(const Call &a, const Sequence &s, int kv, 
 
 // Partial results of a share of the keys: unscaled sums [share][token][head][channel], reference and sum [share][token][head].
 struct Shares {
-    int count;
+    int count, paired;
     float *sums, *stats;
 };
 
@@ -253,224 +253,233 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
     typedef typename Mfma32<T>::Frag Frag;
     __shared__ __align__(16) T lk[2][kKeys * D];
     __shared__ __align__(16) T lv[2][kKeys * D];
-    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, kv = work / shares.count / tiles;
-    int b, tile;
-    if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kRows, tiles - 1 - work / shares.count % tiles, b, tile)) return;
-    const Sequence s = sequence(a, b);
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, h = lane / 32;
-    const int r0 = tile * kRows, rows = int(int64_t(s.nq) * a.group);
-    const Row mine = row_of(a, s, kv, r0 + wave * 32 + lane % 32);
-    // keys that some row of the workgroup sees: its last row sees most
-    const int last = r0 + kRows < rows ? r0 + kRows - 1 : rows - 1, most = limit_of(a, s, query_of(a, last));
-    const int all = (most + kKeys - 1) / kKeys, first = int(int64_t(all) * share / shares.count), end = int(int64_t(all) * (share + 1) / shares.count);
-    // limits within the wavefront
-    int wave_most = mine.limit, wave_least = mine.limit < 0 ? 1 << 30 : mine.limit;
+    auto one = [&](int share, int kv, int id) {
+        int b, tile;
+        if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kRows, id, b, tile)) return;
+        const Sequence s = sequence(a, b);
+        const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, h = lane / 32;
+        const int r0 = tile * kRows, rows = int(int64_t(s.nq) * a.group);
+        const Row mine = row_of(a, s, kv, r0 + wave * 32 + lane % 32);
+        // keys that some row of the workgroup sees: its last row sees most
+        const int last = r0 + kRows < rows ? r0 + kRows - 1 : rows - 1, most = limit_of(a, s, query_of(a, last));
+        const int all = (most + kKeys - 1) / kKeys, first = int(int64_t(all) * share / shares.count), end = int(int64_t(all) * (share + 1) / shares.count);
+        // limits within the wavefront
+        int wave_most = mine.limit, wave_least = mine.limit < 0 ? 1 << 30 : mine.limit;
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        wave_most = max(wave_most, __shfl_xor(wave_most, d));
-        wave_least = min(wave_least, __shfl_xor(wave_least, d));
-    }
-    wave_most = __builtin_amdgcn_readfirstlane(wave_most);
-    wave_least = __builtin_amdgcn_readfirstlane(wave_least);
-
-    Frag q[D / 16];
-    const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) q[k] = eight<T>(from + 16 * k + 8 * h, mine.limit >= 0 && 16 * k + 8 * h < a.head);
-    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
-    const Along<T, D> along;
-    const Across<T, D> across;
-    f32x16 o[D / 32] = {}, p = {}, n = {};
-    Frag w[2] = {};
-    float top = -INFINITY, against = 0, sum = 0, shrink = 1;
-
-    const T *keys = static_cast<const T *>(a.k) + (s.k0 + first * kKeys) * a.k_token + kv * a.k_step;
-    const T *values = static_cast<const T *>(a.v) + (s.k0 + first * kKeys) * a.v_token + kv * a.v_step;
-    Stream<T, D, kKeys, kThreads> sk, sv;
-    sk.begin(keys, a.k_token);
-    sv.begin(values, a.v_token);
-    auto ask_k = [&](int t) {
-        if (t < end) sk.ask(a.k_token, s.used - t * kKeys, a.head);
-    };
-    auto ask_v = [&](int t) {
-        if (t < end) sv.ask(a.v_token, s.used - t * kKeys, a.head);
-    };
-    // Scores of half a tile of keys; weighted values of one.
-    auto scores = [&](int buffer, int half) {
-        f32x16 x = {};
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) x = Mfma32<T>::run(along.read(lk[buffer], half * 32, k), q[k], x);
-        return x;
-    };
-    auto weigh = [&](int buffer, int half) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-            for (int m = 0; m < D / 32; ++m) o[m] = Mfma32<T>::run(across.read(lv[buffer], half * 32 + 16 * k, m), w[k], o[m]);
-    };
-    // Of step i's scores p: hides what a row does not see; the reference that exponents are taken against follows the maximum only
-    // when that has grown by 2^8 over it (sums in 32 bits and weights of 16 have room for the factor), and o has then to
-    // be shrunk once the weights of the step before are in it.
-    auto hide = [&](int i, f32x16 &p) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (i * 32 + 8 * (j / 4) + 4 * h + j % 4 >= mine.limit) p[j] = -INFINITY;
-    };
-    auto refer = [&](const f32x16 &p) -> bool {
-        float high = p[0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) high = fmaxf(high, p[j]);
-        high *= a.c;
-        if (!__any(high > top + 8.0f)) return false;
-        high = fmaxf(fmaxf(high, other_half(high)), top);
-        shrink = top == high ? 1.0f : __builtin_amdgcn_exp2f(top - high);
-        top = high;
-        against = top == -INFINITY ? 0.0f : top;
-        sum *= shrink;
-        return true;
-    };
-    auto weights = [&](f32x16 &p, Frag (&x)[2]) {
-        float part = 0;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            p[j] = __builtin_amdgcn_exp2f(fmaf(p[j], a.c, -against));
-            if (j % 2) part += p[j];
-            else sum += p[j];
-            x[j / 8][j % 8] = T(p[j]);
+        for (int d = 1; d < 32; d *= 2) {
+            wave_most = max(wave_most, __shfl_xor(wave_most, d));
+            wave_least = min(wave_least, __shfl_xor(wave_least, d));
         }
-        sum += part;
-    };
-    auto shrink_o = [&] {
+        wave_most = __builtin_amdgcn_readfirstlane(wave_most);
+        wave_least = __builtin_amdgcn_readfirstlane(wave_least);
+
+        Frag q[D / 16];
+        const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
 #pragma unroll
-        for (int m = 0; m < D / 32; ++m) o[m] *= shrink;
-    };
-    // A step's weights, while the matrix instructions make the next step's scores and the sum of the last one's weighted values.
-    // Tile t's scores are made a step ahead, its weighted values a step behind, so K of a tile is in LDS a barrier before V.
-    const int steps = min(2 * end, (wave_most + 31) / 32);       // of this wavefront
-    // Written in the order in which it is to be issued: two matrix instructions, arithmetic that takes about as long, reads for the
-    // pair after the next; the fences keep the compiler from sorting by kind (943 TFLOP/s at 4,096 x 4,096, not causal).
-    auto step = [&](int k_buffer, int v_buffer, int half, f32x16 &now, f32x16 &next) {
-        constexpr int kPairs = D / 16, kAhead = 2;
-        Frag kf[kAhead + 1], vf[kAhead + 1], x[2];
-        auto read = [&](int j) {
-            kf[j % (kAhead + 1)] = along.read(lk[k_buffer], half * 32, j);
-            vf[j % (kAhead + 1)] = across.read(lv[v_buffer], half * 32 + j / (D / 32) * 16, j % (D / 32));
+        for (int k = 0; k < D / 16; ++k) q[k] = eight<T>(from + 16 * k + 8 * h, mine.limit >= 0 && 16 * k + 8 * h < a.head);
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
+        const Along<T, D> along;
+        const Across<T, D> across;
+        f32x16 o[D / 32] = {}, p = {}, n = {};
+        Frag w[2] = {};
+        float top = -INFINITY, against = 0, sum = 0, shrink = 1;
+
+        const T *keys = static_cast<const T *>(a.k) + (s.k0 + first * kKeys) * a.k_token + kv * a.k_step;
+        const T *values = static_cast<const T *>(a.v) + (s.k0 + first * kKeys) * a.v_token + kv * a.v_step;
+        Stream<T, D, kKeys, kThreads> sk, sv;
+        sk.begin(keys, a.k_token);
+        sv.begin(values, a.v_token);
+        auto ask_k = [&](int t) {
+            if (t < end) sk.ask(a.k_token, s.used - t * kKeys, a.head);
         };
-        auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) read(j);
-        fence();
-        int grown = __builtin_amdgcn_readfirstlane(refer(now));
-        asm volatile("" : "+s"(grown));                          // so that there is one copy of what follows, not one for either case
-        float part = 0;
-        auto summed = [&](int e) {                               // of exponentials
-            if (e % 2) part += now[e];
-            else sum += now[e];
-            x[e / 8][e % 8] = T(now[e]);
+        auto ask_v = [&](int t) {
+            if (t < end) sv.ask(a.v_token, s.used - t * kKeys, a.head);
         };
-        fence();
+        // Scores of half a tile of keys; weighted values of one.
+        auto scores = [&](int buffer, int half) {
+            f32x16 x = {};
 #pragma unroll
-        for (int j = 0; j < kPairs; ++j) {
-            const int from = 16 * j / kPairs, to = 16 * (j + 1) / kPairs, before = 16 * (j - 1) / kPairs;
-            next = Mfma32<T>::run(kf[j % (kAhead + 1)], q[j], j ? next : f32x16{});
+            for (int k = 0; k < D / 16; ++k) x = Mfma32<T>::run(along.read(lk[buffer], half * 32, k), q[k], x);
+            return x;
+        };
+        auto weigh = [&](int buffer, int half) {
 #pragma unroll
-            for (int e = from; e < to; ++e) now[e] = __builtin_amdgcn_exp2f(fmaf(now[e], a.c, -against));
-            fence();
-            o[j % (D / 32)] = Mfma32<T>::run(vf[j % (kAhead + 1)], w[j / (D / 32)], o[j % (D / 32)]);
-            if (j + kAhead < kPairs) read(j + kAhead);
-            if (j > 0) {
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int e = before; e < from; ++e) summed(e);
+                for (int m = 0; m < D / 32; ++m) o[m] = Mfma32<T>::run(across.read(lv[buffer], half * 32 + 16 * k, m), w[k], o[m]);
+        };
+        // Of step i's scores p: hides what a row does not see; the reference that exponents are taken against follows the maximum only
+        // when that has grown by 2^8 over it (sums in 32 bits and weights of 16 have room for the factor), and o has then to
+        // be shrunk once the weights of the step before are in it.
+        auto hide = [&](int i, f32x16 &p) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (i * 32 + 8 * (j / 4) + 4 * h + j % 4 >= mine.limit) p[j] = -INFINITY;
+        };
+        auto refer = [&](const f32x16 &p) -> bool {
+            float high = p[0];
+#pragma unroll
+            for (int j = 1; j < 16; ++j) high = fmaxf(high, p[j]);
+            high *= a.c;
+            if (!__any(high > top + 8.0f)) return false;
+            high = fmaxf(fmaxf(high, other_half(high)), top);
+            shrink = top == high ? 1.0f : __builtin_amdgcn_exp2f(top - high);
+            top = high;
+            against = top == -INFINITY ? 0.0f : top;
+            sum *= shrink;
+            return true;
+        };
+        auto weights = [&](f32x16 &p, Frag (&x)[2]) {
+            float part = 0;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                p[j] = __builtin_amdgcn_exp2f(fmaf(p[j], a.c, -against));
+                if (j % 2) part += p[j];
+                else sum += p[j];
+                x[j / 8][j % 8] = T(p[j]);
             }
-            fence();
-        }
+            sum += part;
+        };
+        auto shrink_o = [&] {
 #pragma unroll
-        for (int e = 16 * (kPairs - 1) / kPairs; e < 16; ++e) summed(e);
-        sum += part;
-        w[0] = x[0], w[1] = x[1];
-        asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(sum));    // here, not where they are used
-        if (grown) shrink_o();
-    };
-    auto edge = [&](int i, f32x16 &now, f32x16 &next) {          // a step that lacks one of these, or hides keys
-        if (i > steps) return;
-        if (i + 1 < steps) next = scores((i + 1) / 2 - first & 1, i + 1 & 1);
-        if (i > 2 * first) weigh((i - 1) / 2 - first & 1, i - 1 & 1);
-        if (i == steps) return;
-        if (32 * i + 32 > wave_least) hide(i, now);
-        if (refer(now)) shrink_o();
-        weights(now, w);
-    };
-    ask_k(first);
-    ask_v(first);
-    if (first < end) {
-        sk.put(lk[0]);
-        sv.put(lv[0]);
-    }
-    ask_k(first + 1);
-    ask_v(first + 1);
-    __syncthreads();
-    if (2 * first < steps) p = scores(0, 0);
-    // A tile that lies in `buffer`; the next one's K is put behind its first step, V behind the barrier.
-    auto whole = [&](int t, int buffer) {
-        step(buffer, 1 - buffer, 1, p, n);
-        sk.put(lk[1 - buffer]);
-        ask_k(t + 2);
-        __syncthreads();
-        sv.put(lv[1 - buffer]);
-        ask_v(t + 2);
-        step(1 - buffer, buffer, 0, n, p);
-    };
-    auto partial = [&](int t) {
-        const int next = t + 1 - first & 1;
-        edge(2 * t, p, n);
-        if (t + 1 < end) sk.put(lk[next]);
-        ask_k(t + 2);
-        __syncthreads();
-        if (t + 1 < end) sv.put(lv[next]);
-        ask_v(t + 2);
-        edge(2 * t + 1, n, p);
-    };
-    // Loops of their own: the compiler merges what two branches of one have in common, and then nothing goes on meanwhile.  A whole
-    // tile has another behind it and hides nothing.
-    const int whole_end = min(end - 1, min((steps - 1) / 2, wave_least / kKeys));
-    int t = first;
-    if (t < end) partial(t++);
-#pragma unroll 1
-    for (; t + 1 < whole_end; t += 2) {
-        whole(t, 1);
-        whole(t + 1, 0);
-    }
-#pragma unroll 1
-    for (; t < end; ++t) partial(t);
-    if (first < end) edge(2 * end, p, n);                        // the last weighted values
-    if (mine.limit < 0) return;
-    sum += other_half(sum);
-    if (shares.count > 1) {
-        const int64_t at = (int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head;
-        if (h == 0) {
-            shares.stats[2 * at] = top;
-            shares.stats[2 * at + 1] = sum;
+            for (int m = 0; m < D / 32; ++m) o[m] *= shrink;
+        };
+        // A step's weights, while the matrix instructions make the next step's scores and the sum of the last one's weighted values.
+        // Tile t's scores are made a step ahead, its weighted values a step behind, so K of a tile is in LDS a barrier before V.
+        const int steps = min(2 * end, (wave_most + 31) / 32);       // of this wavefront
+        // Written in the order in which it is to be issued: two matrix instructions, arithmetic that takes about as long, reads for the
+        // pair after the next; the fences keep the compiler from sorting by kind (943 TFLOP/s at 4,096 x 4,096, not causal).
+        auto step = [&](int k_buffer, int v_buffer, int half, f32x16 &now, f32x16 &next) {
+            constexpr int kPairs = D / 16, kAhead = 2;
+            Frag kf[kAhead + 1], vf[kAhead + 1], x[2];
+            auto read = [&](int j) {
+                kf[j % (kAhead + 1)] = along.read(lk[k_buffer], half * 32, j);
+                vf[j % (kAhead + 1)] = across.read(lv[v_buffer], half * 32 + j / (D / 32) * 16, j % (D / 32));
+            };
+            auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) read(j);
+            fence();
+            int grown = __builtin_amdgcn_readfirstlane(refer(now));
+            asm volatile("" : "+s"(grown));                          // so that there is one copy of what follows, not one for either case
+            float part = 0;
+            auto summed = [&](int e) {                               // of exponentials
+                if (e % 2) part += now[e];
+                else sum += now[e];
+                x[e / 8][e % 8] = T(now[e]);
+            };
+            fence();
+#pragma unroll
+            for (int j = 0; j < kPairs; ++j) {
+                const int from = 16 * j / kPairs, to = 16 * (j + 1) / kPairs, before = 16 * (j - 1) / kPairs;
+                next = Mfma32<T>::run(kf[j % (kAhead + 1)], q[j], j ? next : f32x16{});
+#pragma unroll
+                for (int e = from; e < to; ++e) now[e] = __builtin_amdgcn_exp2f(fmaf(now[e], a.c, -against));
+                fence();
+                o[j % (D / 32)] = Mfma32<T>::run(vf[j % (kAhead + 1)], w[j / (D / 32)], o[j % (D / 32)]);
+                if (j + kAhead < kPairs) read(j + kAhead);
+                if (j > 0) {
+#pragma unroll
+                    for (int e = before; e < from; ++e) summed(e);
+                }
+                fence();
+            }
+#pragma unroll
+            for (int e = 16 * (kPairs - 1) / kPairs; e < 16; ++e) summed(e);
+            sum += part;
+            w[0] = x[0], w[1] = x[1];
+            asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(sum));    // here, not where they are used
+            if (grown) shrink_o();
+        };
+        auto edge = [&](int i, f32x16 &now, f32x16 &next) {          // a step that lacks one of these, or hides keys
+            if (i > steps) return;
+            if (i + 1 < steps) next = scores((i + 1) / 2 - first & 1, i + 1 & 1);
+            if (i > 2 * first) weigh((i - 1) / 2 - first & 1, i - 1 & 1);
+            if (i == steps) return;
+            if (32 * i + 32 > wave_least) hide(i, now);
+            if (refer(now)) shrink_o();
+            weights(now, w);
+        };
+        ask_k(first);
+        ask_v(first);
+        if (first < end) {
+            sk.put(lk[0]);
+            sv.put(lv[0]);
         }
-        if (sum == 0) return;                            // nothing that the join looks at
+        ask_k(first + 1);
+        ask_v(first + 1);
+        __syncthreads();
+        if (2 * first < steps) p = scores(0, 0);
+        // A tile that lies in `buffer`; the next one's K is put behind its first step, V behind the barrier.
+        auto whole = [&](int t, int buffer) {
+            step(buffer, 1 - buffer, 1, p, n);
+            sk.put(lk[1 - buffer]);
+            ask_k(t + 2);
+            __syncthreads();
+            sv.put(lv[1 - buffer]);
+            ask_v(t + 2);
+            step(1 - buffer, buffer, 0, n, p);
+        };
+        auto partial = [&](int t) {
+            const int next = t + 1 - first & 1;
+            edge(2 * t, p, n);
+            if (t + 1 < end) sk.put(lk[next]);
+            ask_k(t + 2);
+            __syncthreads();
+            if (t + 1 < end) sv.put(lv[next]);
+            ask_v(t + 2);
+            edge(2 * t + 1, n, p);
+        };
+        // Loops of their own: the compiler merges what two branches of one have in common, and then nothing goes on meanwhile.  A whole
+        // tile has another behind it and hides nothing.
+        const int whole_end = min(end - 1, min((steps - 1) / 2, wave_least / kKeys));
+        int t = first;
+        if (t < end) partial(t++);
+#pragma unroll 1
+        for (; t + 1 < whole_end; t += 2) {
+            whole(t, 1);
+            whole(t + 1, 0);
+        }
+#pragma unroll 1
+        for (; t < end; ++t) partial(t);
+        if (first < end) edge(2 * end, p, n);                        // the last weighted values
+        if (mine.limit < 0) return;
+        sum += other_half(sum);
+        if (shares.count > 1) {
+            const int64_t at = (int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head;
+            if (h == 0) {
+                shares.stats[2 * at] = top;
+                shares.stats[2 * at + 1] = sum;
+            }
+            if (sum == 0) return;                            // nothing that the join looks at
+#pragma unroll
+            for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int col = 32 * m + 8 * i + 4 * h;
+                    if (col < a.head) *reinterpret_cast<f32x4 *>(shares.sums + at * a.head + col) = f32x4{o[m][4 * i], o[m][4 * i + 1], o[m][4 * i + 2], o[m][4 * i + 3]};
+                }
+            return;
+        }
+        const float scale = sum == 0 ? 0.0f : 1.0f / sum;    // no key: zeros; scores that are NaN: NaN
+        if (a.lse && h == 0) a.lse[mine.head * a.tokens_q + mine.token] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+        T *to = static_cast<T *>(a.o) + mine.token * a.o_token + mine.head * a.o_step;
 #pragma unroll
         for (int m = 0; m < D / 32; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int col = 32 * m + 8 * i + 4 * h;
-                if (col < a.head) *reinterpret_cast<f32x4 *>(shares.sums + at * a.head + col) = f32x4{o[m][4 * i], o[m][4 * i + 1], o[m][4 * i + 2], o[m][4 * i + 3]};
+                if (col < a.head) store4(to + col, f32x4{o[m][4 * i] * scale, o[m][4 * i + 1] * scale, o[m][4 * i + 2] * scale, o[m][4 * i + 3] * scale});
             }
-        return;
+    };
+    // Tiles of rows that see most keys first; with shares.paired a workgroup takes one of them and one of the least in turn.
+    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, places = shares.paired ? (tiles + 1) / 2 : tiles;
+    const int kv = work / shares.count / places, place = work / shares.count % places;
+#pragma unroll 1
+    for (int turn = 0; turn < (shares.paired && place != tiles - 1 - place ? 2 : 1); ++turn) {
+        if (turn) __syncthreads();               // all have read what lies in LDS
+        one(share, kv, turn ? place : tiles - 1 - place);
     }
-    const float scale = sum == 0 ? 0.0f : 1.0f / sum;    // no key: zeros; scores that are NaN: NaN
-    if (a.lse && h == 0) a.lse[mine.head * a.tokens_q + mine.token] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
-    T *to = static_cast<T *>(a.o) + mine.token * a.o_token + mine.head * a.o_step;
-#pragma unroll
-    for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = 32 * m + 8 * i + 4 * h;
-            if (col < a.head) store4(to + col, f32x4{o[m][4 * i] * scale, o[m][4 * i + 1] * scale, o[m][4 * i + 2] * scale, o[m][4 * i + 3] * scale});
-        }
 }
 
 // Shares of the keys, joined: 32 lanes a row of four channels each, rows of sequences only.
@@ -505,20 +514,26 @@ struct Grads {
     int64_t do_token, do_step, dq_token, dq_step, dk_token, dk_step, dv_token, dv_step;
     void *dq, *dk, *dv;
     float *delta;                    // [heads][tokens_q]: sum over channels of dO O
-    uint32_t *peaks;                 // HARP_F16: largest squared norms of dO's and V's rows, as bits
+    float *peaks;                    // HARP_F16: [2][kPeaks] largest squared norms of rows of dO and of V, one from each workgroup
     float scale;
 };
 
 // Weights and their gradients on their way into the matrix instructions.  bfloat16 has the range of 32 bits.  In float16 weights go in
 // times 2^12 (they are normal numbers down to 2^-26: 10^5 equal ones of a row are still rounded to 2^-11 of themselves), and
 // gradients times a power of two taken from the largest norms: |P (dP - D)| <= 2 |dO_i| |v_j|, which is brought to 2^14 at most.
+constexpr int kPeaks = 256;
 template <typename T> struct Range {
     static constexpr bool kNarrow = sizeof(T) == 2 && __is_same(T, _Float16);
     static constexpr float kShift = kNarrow ? 12.0f : 0.0f, kWeight = kNarrow ? 0.000244140625f : 1.0f;
     float factor = 1;                // of dP - D where a weight carries 2^kShift
-    __device__ __forceinline__ explicit Range(const uint32_t *peaks) {
+    __device__ __forceinline__ explicit Range(const float *peaks) {
         if constexpr (kNarrow) {
-            const float bound = 4 * __uint_as_float(peaks[0]) * __uint_as_float(peaks[1]);
+            uint32_t high[2] = {0, 0};                           // of floats that are not negative, or NaN: as their bits
+#pragma unroll
+            for (int i = 0; i < kPeaks; i += kWave)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) high[j] = larger(high[j], __float_as_uint(peaks[j * kPeaks + i + threadIdx.x % kWave]));
+            const float bound = 4 * __uint_as_float(wave_max(high[0])) * __uint_as_float(wave_max(high[1]));
             int e = 0;
             if (bound > 0 && bound < INFINITY) {
                 (void)frexpf(bound, &e);
@@ -530,51 +545,48 @@ template <typename T> struct Range {
     __device__ __forceinline__ float back() const { return kNarrow ? kWeight / factor : 1.0f; }       // of what gradients are summed into
 };
 
-__global__ void no_peaks(uint32_t *peaks) { peaks[threadIdx.x] = 0; }
-// A workgroup takes 64 rows of sequences, of dO or of V, 16 lanes a row.  A maximum does not mind the order.
-constexpr int kPeakRows = 64;
+// Sums over channels of dO O of every row of a sequence, 16 lanes a row; in HARP_F16 the largest norms of dO's rows too, and, by as many
+// workgroups more (kPeaks), of V's.  A workgroup takes a tile of 64 rows in `groups`.
+constexpr int kMeasured = 64;
 template <typename T>
-__global__ __launch_bounds__(256) void find_peaks(Call a, Grads g, int of_q) {
-    const bool q = int(blockIdx.x) < of_q;
-    const int times = q ? a.heads : a.kv_heads;
-    int b, tile;
-    if (!locate(q ? a.q_begin : a.k_begin, q ? a.tokens_q : a.tokens_k, a.batch, times, kPeakRows, q ? blockIdx.x : blockIdx.x - of_q, b, tile)) return;
-    const Sequence s = sequence(a, b);
-    const int64_t rows = int64_t(q ? s.nq : s.used) * times, first = int64_t(tile) * kPeakRows;
-    const int col = threadIdx.x % 16 * 8;
-    float peak = 0;
+__global__ __launch_bounds__(256) void measure(Call a, Grads g, int of_q, int of_k, int groups) {
+    __shared__ uint32_t highest[4];
+    const bool q = int(blockIdx.x) < groups;
+    const int times = q ? a.heads : a.kv_heads, col = threadIdx.x % 16 * 8;
+    uint32_t high = 0;
+    for (int id = blockIdx.x % groups; id < (q ? of_q : of_k); id += groups) {
+        int b, tile;
+        if (!locate(q ? a.q_begin : a.k_begin, q ? a.tokens_q : a.tokens_k, a.batch, times, kMeasured, id, b, tile)) break;
+        const Sequence s = sequence(a, b);
+        const int64_t rows = int64_t(q ? s.nq : s.used) * times, first = int64_t(tile) * kMeasured;
 #pragma unroll
-    for (int i = 0; i < kPeakRows / 16; ++i) {
-        const int64_t r = first + i * 16 + threadIdx.x / 16, token = r / times, head = r % times;
-        const bool there = r < rows && col < a.head;
-        const T *from = q ? static_cast<const T *>(g.d_o) + (s.q0 + token) * g.do_token + head * g.do_step
-                          : static_cast<const T *>(a.v) + (s.k0 + token) * a.v_token + head * a.v_step;
-        const auto x = eight<T>(from + col, there);
-        float d = 0;
+        for (int i = 0; i < kMeasured / 16; ++i) {
+            const int64_t r = first + i * 16 + threadIdx.x / 16, token = r / times, head = r % times;
+            const bool there = r < rows && col < a.head;
+            const T *from = q ? static_cast<const T *>(g.d_o) + (s.q0 + token) * g.do_token + head * g.do_step
+                              : static_cast<const T *>(a.v) + (s.k0 + token) * a.v_token + head * a.v_step;
+            const auto x = eight<T>(from + col, there);
+            if (q) {
+                const auto y = eight<T>(static_cast<const T *>(a.o) + (s.q0 + token) * a.o_token + head * a.o_step + col, there);
+                float d = 0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) d += to_f32(T(x[k])) * to_f32(T(x[k]));
-        d = sum16(d);
-        peak = d > peak || d != d ? d : peak;
+                for (int k = 0; k < 8; ++k) d += to_f32(T(x[k])) * to_f32(T(y[k]));
+                d = sum16(d);
+                if (r < rows && threadIdx.x % 16 == 0) g.delta[head * a.tokens_q + s.q0 + token] = d;
+            }
+            if (Range<T>::kNarrow) {
+                float d = 0;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) d += to_f32(T(x[k])) * to_f32(T(x[k]));
+                high = larger(high, __float_as_uint(sum16(d)) & 0x7fffffff);
+            }
+        }
     }
-    const uint32_t high = wave_max(__float_as_uint(peak));
-    if (threadIdx.x % kWave == 0) atomicMax(g.peaks + (q ? 0 : 1), high);
-}
-
-// 16 lanes a row of eight channels each.
-template <typename T> __global__ __launch_bounds__(256) void deltas(Call a, Grads g) {
-    const int col = threadIdx.x % 16 * 8;
-    const bool there = col < a.head;
-    for (int64_t row = int64_t(blockIdx.x) * 16 + threadIdx.x / 16; row < a.tokens_q * a.heads; row += int64_t(gridDim.x) * 16) {
-        const int64_t token = row / a.heads;
-        const int head = int(row - token * a.heads);
-        const auto x = eight<T>(static_cast<const T *>(a.o) + token * a.o_token + head * a.o_step + (there ? col : 0), there);
-        const auto y = eight<T>(static_cast<const T *>(g.d_o) + token * g.do_token + head * g.do_step + (there ? col : 0), there);
-        float d = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d += to_f32(T(x[i])) * to_f32(T(y[i]));
-        d = sum16(d);
-        if (threadIdx.x % 16 == 0) g.delta[head * a.tokens_q + token] = d;
-    }
+    if (!Range<T>::kNarrow) return;
+    high = wave_max(high);
+    if (threadIdx.x % kWave == 0) highest[threadIdx.x / kWave] = high;
+    __syncthreads();
+    if (threadIdx.x == 0) g.peaks[blockIdx.x] = __uint_as_float(larger(larger(highest[0], highest[1]), larger(highest[2], highest[3])));
 }
 
 // dQ, as the forward pass goes: dQ^T = K^T dS^T, dS^T = P^T (V dO^T - delta).
@@ -584,128 +596,137 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
     typedef typename Mfma32<T>::Frag Frag;
     __shared__ __align__(16) T lk[2][kKeys * D];
     __shared__ __align__(16) T lv[2][kKeys * D];
-    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, kv = work / shares.count / tiles;
-    int b, tile;
-    if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kRows, tiles - 1 - work / shares.count % tiles, b, tile)) return;
-    const Sequence s = sequence(a, b);
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, h = lane / 32;
-    const int r0 = tile * kRows, rows = int(int64_t(s.nq) * a.group);
-    const Row mine = row_of(a, s, kv, r0 + wave * 32 + lane % 32);
-    const int last = r0 + kRows < rows ? r0 + kRows - 1 : rows - 1, most = limit_of(a, s, query_of(a, last));
-    const int all = (most + kKeys - 1) / kKeys, first = int(int64_t(all) * share / shares.count), end = int(int64_t(all) * (share + 1) / shares.count);
-    const bool here = mine.limit >= 0;
-    float lse = here ? a.lse[mine.head * a.tokens_q + mine.token] * kLog2e : 0;
-    const Range<T> range(g.peaks);
-    const float delta = here ? g.delta[mine.head * a.tokens_q + mine.token] * range.factor : 0;
-    const int limit = lse == -INFINITY ? 0 : mine.limit;
-    lse = lse == -INFINITY ? 0 : lse - Range<T>::kShift;
-    int wave_most = limit, wave_least = limit < 0 ? 1 << 30 : limit;
+    auto one = [&](int share, int kv, int id) {
+        int b, tile;
+        if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kRows, id, b, tile)) return;
+        const Sequence s = sequence(a, b);
+        const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, h = lane / 32;
+        const int r0 = tile * kRows, rows = int(int64_t(s.nq) * a.group);
+        const Row mine = row_of(a, s, kv, r0 + wave * 32 + lane % 32);
+        const int last = r0 + kRows < rows ? r0 + kRows - 1 : rows - 1, most = limit_of(a, s, query_of(a, last));
+        const int all = (most + kKeys - 1) / kKeys, first = int(int64_t(all) * share / shares.count), end = int(int64_t(all) * (share + 1) / shares.count);
+        const bool here = mine.limit >= 0;
+        float lse = here ? a.lse[mine.head * a.tokens_q + mine.token] * kLog2e : 0;
+        const Range<T> range(g.peaks);
+        const float delta = here ? g.delta[mine.head * a.tokens_q + mine.token] * range.factor : 0;
+        const int limit = lse == -INFINITY ? 0 : mine.limit;
+        lse = lse == -INFINITY ? 0 : lse - Range<T>::kShift;
+        int wave_most = limit, wave_least = limit < 0 ? 1 << 30 : limit;
 #pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        wave_most = max(wave_most, __shfl_xor(wave_most, d));
-        wave_least = min(wave_least, __shfl_xor(wave_least, d));
-    }
-    wave_most = __builtin_amdgcn_readfirstlane(wave_most);
-    wave_least = __builtin_amdgcn_readfirstlane(wave_least);
-    Frag q[D / 16], d_o[D / 16];
-    const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
-    const T *from_do = static_cast<const T *>(g.d_o) + mine.token * g.do_token + mine.head * g.do_step;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-        q[k] = eight<T>(from + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
-        d_o[k] = eight<T>(from_do + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
-    }
-    __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
-    Along<T, D> along;
-    Across<T, D> across;
-    f32x16 dq[D / 32] = {};
-    const T *keys = static_cast<const T *>(a.k) + (s.k0 + first * kKeys) * a.k_token + kv * a.k_step;
-    const T *values = static_cast<const T *>(a.v) + (s.k0 + first * kKeys) * a.v_token + kv * a.v_step;
-    Stream<T, D, kKeys, kThreads> sk, sv;
-    sk.begin(keys, a.k_token);
-    sv.begin(values, a.v_token);
-    auto ask = [&](int t) {
-        if (t >= end) return;
-        sk.ask(a.k_token, s.used - t * kKeys, a.head);
-        sv.ask(a.v_token, s.used - t * kKeys, a.head);
-    };
-    // A tile's matrix instructions, one operand of each from LDS, and what goes on under them:
-    //   S of the first 32 keys;  their dP, exponentials;  S of the others, dS of the first;  dP, exponentials;  dQ of the first,
-    //   dS of the others;  dQ of those.
-    constexpr int kPart = D / 16, kAhead = 2;
-    auto tile_of_keys = [&](int t, int buffer, auto masked) {
-        f32x16 p[2], dp[2];
-        Frag f[kAhead + 1], w[2][2];
-        auto read = [&](auto n) {
-            constexpr int part = n / kPart, j = n % kPart;
-            Frag &to = f[n % (kAhead + 1)];
-            if (part < 4) to = along.read(part % 2 ? lv[buffer] : lk[buffer], part / 2 * 32, j);
-            else to = across.read(lk[buffer], (part - 4) * 32 + j / (D / 32) * 16, j % (D / 32));
-        };
-        auto exponential = [&](int u, int e) { p[u][e] = __builtin_amdgcn_exp2f(fmaf(p[u][e], a.c, -lse)); };
-        auto gradient = [&](int u, int e) {
-            float ds = p[u][e] * range.less(dp[u][e], delta);
-            if (masked.value && t * kKeys + 32 * u + 8 * (e / 4) + 4 * h + e % 4 >= limit) ds = 0;
-            w[u][e / 8][e % 8] = T(ds);
-        };
-        written_out<kAhead>(read);
-        written_out<6 * kPart>([&](auto n) {
-            constexpr int part = n / kPart, j = n % kPart, from = 16 * j / kPart, to = 16 * (j + 1) / kPart;
-            const Frag &x = f[n % (kAhead + 1)];
-            if constexpr (part == 0 || part == 2) p[part / 2] = Mfma32<T>::run(x, q[j], j ? p[part / 2] : f32x16{});
-            else if constexpr (part == 1 || part == 3) dp[part / 2] = Mfma32<T>::run(x, d_o[j], j ? dp[part / 2] : f32x16{});
-            else dq[j % (D / 32)] = Mfma32<T>::run(x, w[part - 4][j / (D / 32)], dq[j % (D / 32)]);
-            if constexpr (n + kAhead < 6 * kPart) read(std::integral_constant<int, n + kAhead>());
-#pragma unroll
-            for (int e = from; e < to; ++e) {
-                if (part == 1 || part == 3) exponential(part / 2, e);
-                if (part == 2) gradient(0, e);
-                if (part == 4) gradient(1, e);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        });
-    };
-    ask(first);
-    if (first < end) {
-        sk.put(lk[0]);
-        sv.put(lv[0]);
-    }
-    ask(first + 1);
-    __syncthreads();
-    const int whole = min(end, wave_least / kKeys);              // tiles of which nothing is hidden
-    auto turn = [&](int t, int buffer, auto masked) {
-        along.refresh();
-        across.refresh();
-        if (t * kKeys < wave_most) tile_of_keys(t, buffer, masked);
-        if (t + 1 < end) {
-            sk.put(lk[1 - buffer]);
-            sv.put(lv[1 - buffer]);
+        for (int d = 1; d < 32; d *= 2) {
+            wave_most = max(wave_most, __shfl_xor(wave_most, d));
+            wave_least = min(wave_least, __shfl_xor(wave_least, d));
         }
-        ask(t + 2);
+        wave_most = __builtin_amdgcn_readfirstlane(wave_most);
+        wave_least = __builtin_amdgcn_readfirstlane(wave_least);
+        Frag q[D / 16], d_o[D / 16];
+        const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
+        const T *from_do = static_cast<const T *>(g.d_o) + mine.token * g.do_token + mine.head * g.do_step;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            q[k] = eight<T>(from + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
+            d_o[k] = eight<T>(from_do + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
+        Along<T, D> along;
+        Across<T, D> across;
+        f32x16 dq[D / 32] = {};
+        const T *keys = static_cast<const T *>(a.k) + (s.k0 + first * kKeys) * a.k_token + kv * a.k_step;
+        const T *values = static_cast<const T *>(a.v) + (s.k0 + first * kKeys) * a.v_token + kv * a.v_step;
+        Stream<T, D, kKeys, kThreads> sk, sv;
+        sk.begin(keys, a.k_token);
+        sv.begin(values, a.v_token);
+        auto ask = [&](int t) {
+            if (t >= end) return;
+            sk.ask(a.k_token, s.used - t * kKeys, a.head);
+            sv.ask(a.v_token, s.used - t * kKeys, a.head);
+        };
+        // A tile's matrix instructions, one operand of each from LDS, and what goes on under them:
+        //   S of the first 32 keys;  their dP, exponentials;  S of the others, dS of the first;  dP, exponentials;  dQ of the first,
+        //   dS of the others;  dQ of those.
+        constexpr int kPart = D / 16, kAhead = 2;
+        auto tile_of_keys = [&](int t, int buffer, auto masked) {
+            f32x16 p[2], dp[2];
+            Frag f[kAhead + 1], w[2][2];
+            auto read = [&](auto n) {
+                constexpr int part = n / kPart, j = n % kPart;
+                Frag &to = f[n % (kAhead + 1)];
+                if (part < 4) to = along.read(part % 2 ? lv[buffer] : lk[buffer], part / 2 * 32, j);
+                else to = across.read(lk[buffer], (part - 4) * 32 + j / (D / 32) * 16, j % (D / 32));
+            };
+            auto exponential = [&](int u, int e) { p[u][e] = __builtin_amdgcn_exp2f(fmaf(p[u][e], a.c, -lse)); };
+            auto gradient = [&](int u, int e) {
+                float ds = p[u][e] * range.less(dp[u][e], delta);
+                if (masked.value && t * kKeys + 32 * u + 8 * (e / 4) + 4 * h + e % 4 >= limit) ds = 0;
+                w[u][e / 8][e % 8] = T(ds);
+            };
+            written_out<kAhead>(read);
+            written_out<6 * kPart>([&](auto n) {
+                constexpr int part = n / kPart, j = n % kPart, from = 16 * j / kPart, to = 16 * (j + 1) / kPart;
+                const Frag &x = f[n % (kAhead + 1)];
+                if constexpr (part == 0 || part == 2) p[part / 2] = Mfma32<T>::run(x, q[j], j ? p[part / 2] : f32x16{});
+                else if constexpr (part == 1 || part == 3) dp[part / 2] = Mfma32<T>::run(x, d_o[j], j ? dp[part / 2] : f32x16{});
+                else dq[j % (D / 32)] = Mfma32<T>::run(x, w[part - 4][j / (D / 32)], dq[j % (D / 32)]);
+                if constexpr (n + kAhead < 6 * kPart) read(std::integral_constant<int, n + kAhead>());
+#pragma unroll
+                for (int e = from; e < to; ++e) {
+                    if (part == 1 || part == 3) exponential(part / 2, e);
+                    if (part == 2) gradient(0, e);
+                    if (part == 4) gradient(1, e);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        };
+        ask(first);
+        if (first < end) {
+            sk.put(lk[0]);
+            sv.put(lv[0]);
+        }
+        ask(first + 1);
         __syncthreads();
-    };
-    int t = first;
+        const int whole = min(end, wave_least / kKeys);              // tiles of which nothing is hidden
+        auto turn = [&](int t, int buffer, auto masked) {
+            along.refresh();
+            across.refresh();
+            if (t * kKeys < wave_most) tile_of_keys(t, buffer, masked);
+            if (t + 1 < end) {
+                sk.put(lk[1 - buffer]);
+                sv.put(lv[1 - buffer]);
+            }
+            ask(t + 2);
+            __syncthreads();
+        };
+        int t = first;
 #pragma unroll 1
-    for (; t + 1 < whole; t += 2) {
-        turn(t, 0, std::false_type());
-        turn(t + 1, 1, std::false_type());
-    }
-#pragma unroll 1
-    for (; t < end; ++t) turn(t, t - first & 1, std::true_type());
-    if (!here) return;
-    const float scale = g.scale * range.back();
-    float *sums = shares.sums + ((int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head) * a.head;
-    T *to = static_cast<T *>(g.dq) + mine.token * g.dq_token + mine.head * g.dq_step;
-#pragma unroll
-    for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = 32 * m + 8 * i + 4 * h;
-            if (col >= a.head) continue;
-            const f32x4 v = f32x4{dq[m][4 * i], dq[m][4 * i + 1], dq[m][4 * i + 2], dq[m][4 * i + 3]} * scale;
-            if (shares.count > 1) *reinterpret_cast<f32x4 *>(sums + col) = v;
-            else store4(to + col, v);
+        for (; t + 1 < whole; t += 2) {
+            turn(t, 0, std::false_type());
+            turn(t + 1, 1, std::false_type());
         }
+#pragma unroll 1
+        for (; t < end; ++t) turn(t, t - first & 1, std::true_type());
+        if (!here) return;
+        const float scale = g.scale * range.back();
+        float *sums = shares.sums + ((int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head) * a.head;
+        T *to = static_cast<T *>(g.dq) + mine.token * g.dq_token + mine.head * g.dq_step;
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int col = 32 * m + 8 * i + 4 * h;
+                if (col >= a.head) continue;
+                const f32x4 v = f32x4{dq[m][4 * i], dq[m][4 * i + 1], dq[m][4 * i + 2], dq[m][4 * i + 3]} * scale;
+                if (shares.count > 1) *reinterpret_cast<f32x4 *>(sums + col) = v;
+                else store4(to + col, v);
+            }
+    };
+    // Tiles of rows that see most keys first; with shares.paired a workgroup takes one of them and one of the least in turn.
+    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, places = shares.paired ? (tiles + 1) / 2 : tiles;
+    const int kv = work / shares.count / places, place = work / shares.count % places;
+#pragma unroll 1
+    for (int turn = 0; turn < (shares.paired && place != tiles - 1 - place ? 2 : 1); ++turn) {
+        if (turn) __syncthreads();               // all have read what lies in LDS
+        one(share, kv, turn ? place : tiles - 1 - place);
+    }
 }
 
 // dK and dV of 32 keys a wavefront, whose rows come through LDS kBack at a time.  dV^T = dO^T P, dK^T = Q^T dS, where a lane has
@@ -899,41 +920,69 @@ struct Plan {
     int waves;                       // of a workgroup
     int64_t tiles;                   // of rows, or of keys
     int shares;                      // of what a tile goes through
+    bool paired;                     // a workgroup takes two tiles
+    int64_t places() const { return paired ? (tiles + 1) / 2 : tiles; }
 };
 int64_t tiles_of(int64_t tokens, int64_t times, int batch, int side) {
     const int64_t whole = tokens * times / side, each = (tokens / batch * times + side - 1) / side * batch;
     // equal lengths need `each`; begins on the device at most this
     return whole + batch > each ? whole + batch : each;
 }
-// `through`: rows that a tile goes through on average, `least` of them a share.
-Plan plan_for(const harp_ctx *ctx, int64_t tokens, int64_t times, int batch, int kv_heads, int64_t through, int64_t least) {
-    Plan p = {};
-    p.waves = tokens * times / batch > 128 ? 8 : 4;
-    p.tiles = tiles_of(tokens, times, batch, 32 * p.waves);
-    int64_t busy = (tokens * times + 32 * p.waves - 1) / (32 * p.waves);
-    busy = (busy > batch ? busy : batch) * kv_heads;                    // workgroups that have something to do
-    int64_t shares = 2 * int64_t(ctx->n_cu) * 4 / p.waves / busy;
-    shares = shares < through / least ? shares : through / least;
-    p.shares = int(shares < 1 ? 1 : shares > 64 ? 64 : shares);
-    return p;
+// Microseconds by what was measured: `step` for a tile of 256 by the 64 (32) rows that go through LDS at a time with 128 channels, 6
+// around them.  Tiles of 128 are two to a compute unit, at the same pace where both are there.  `bytes` that a share's sums take
+// are written and read by a launch more.  The `through` rows are shared out where tiles are few, or, under the causal order, differ.
+Plan plan_for(const harp_ctx *ctx, int64_t tokens, int64_t times, int batch, int kv_heads, int64_t through, int unit, double step, int head,
+              double bytes, bool causal, bool may_pair) {
+    Plan best = {};
+    double least = 1e300;
+    const double channels = head <= 64 ? 0.5 : head <= 96 ? 0.75 : 1.0;
+    const int64_t rows = tokens * times / batch;
+    for (int waves = 8; waves >= 4; waves -= 4) {
+        const int64_t side = 32 * waves, slots = int64_t(ctx->n_cu) * 8 / waves;
+        const int64_t busy = (rows > side ? (rows + side - 1) / side : 1) * batch * kv_heads;       // tiles that have something to do
+        for (int shares : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (shares > 1 && through < int64_t(shares) * 4 * unit) break;
+            const int64_t items = busy * shares;
+            const double steps = double((through + unit - 1) / unit) / shares;
+            const double each = step * channels * (waves == 4 && items <= ctx->n_cu ? 0.6 : 1.0);
+            const int64_t rounds = (items + slots - 1) / slots, pairs = (items + 1) / 2, pair_rounds = (pairs + slots - 1) / slots;
+            const double alone = steps * each + 6;
+            double us = double(rounds) * alone;
+            bool paired = false;
+            if (causal) {
+                // heavy tiles first; workgroups are handed to shader engines in turn and wait for their own, so that they do not
+                // even out.  A heavy and a light one in one workgroup are alike.
+                const double spread = 1.25 * double(items) / double(slots) * (steps * each / 2 + 6);
+                us = alone > spread ? alone : spread;
+                const double both = double(pair_rounds) * (steps * each + 12);
+                if (may_pair && both < us) us = both, paired = true;
+            }
+            if (shares > 1) us += 8 + shares * bytes * 2 / 4e6;
+            if (waves == 4) us *= 1.1;                           // keys are read twice as often
+            if (us < least) least = us, best = Plan{waves, tiles_of(tokens, times, batch, int(side)), shares, paired};
+        }
+    }
+    return best;
 }
-constexpr int kLeastKeys = 256;
-Plan plan_queries(const harp_ctx *ctx, const harp_attention *g) {
-    return plan_for(ctx, g->tokens_q, g->heads / g->kv_heads, g->batch, g->kv_heads, g->tokens_k / g->batch, kLeastKeys);
+Plan plan_queries(const harp_ctx *ctx, const harp_attention *g, bool causal) {
+    const int group = g->heads / g->kv_heads;
+    return plan_for(ctx, g->tokens_q, group, g->batch, g->kv_heads, g->tokens_k / g->batch, kKeys, 2.4, g->head,
+                    double(g->tokens_q) * g->heads * g->head * 4, causal, true);
 }
-Plan plan_keys(const harp_ctx *ctx, const harp_attention *g) {
-    return plan_for(ctx, g->tokens_k, 1, g->batch, g->kv_heads, g->tokens_q / g->batch * (g->heads / g->kv_heads), kLeastKeys);
+Plan plan_keys(const harp_ctx *ctx, const harp_attention *g, bool causal) {
+    return plan_for(ctx, g->tokens_k, 1, g->batch, g->kv_heads, g->tokens_q / g->batch * (g->heads / g->kv_heads), kBack, 2.4, g->head,
+                    double(g->tokens_k) * g->kv_heads * g->head * 8, causal, false);
 }
 
-struct Space { size_t peaks, stats, sums, all; };        // where parts of the workspace begin, behind delta
-Space space_for(const harp_ctx *ctx, const harp_attention *g) {
+// Where parts of the workspace begin, behind delta; what the passes need of these plans.
+struct Space { size_t peaks, stats, sums, all; };
+Space space_for(const harp_attention *g, const Plan *q, const Plan *k) {
     const size_t rows = size_t(g->tokens_q) * g->heads, kv = size_t(g->tokens_k) * g->kv_heads;
-    const Plan q = plan_queries(ctx, g), k = plan_keys(ctx, g);
     Space s = {};
     s.peaks = round_up(rows * 4, 256);
-    s.stats = s.peaks + 256;
-    s.sums = s.stats + (q.shares > 1 ? round_up(rows * q.shares * 8, 256) : 0);
-    const size_t of_q = q.shares > 1 ? rows * q.shares * g->head * 4 : 0, of_k = k.shares > 1 ? kv * k.shares * g->head * 8 : 0;
+    s.stats = s.peaks + 2 * kPeaks * 4;
+    s.sums = s.stats + (q && q->shares > 1 ? round_up(rows * q->shares * 8, 256) : 0);
+    const size_t of_q = q && q->shares > 1 ? rows * q->shares * g->head * 4 : 0, of_k = k && k->shares > 1 ? kv * k->shares * g->head * 8 : 0;
     s.all = s.sums + round_up(of_q > of_k ? of_q : of_k, 256) + 256;
     return s;
 }
@@ -953,7 +1002,9 @@ bool clear_of_each_other(int64_t tokens, int64_t heads, int64_t head, int64_t to
     return in_token || in_head;
 }
 
-int check(harp_ctx *ctx, const harp_attention *g, const Tensor *t, int count, const void *workspace, size_t workspace_bytes) {
+// q, k: how the call is launched; k is null in the forward pass.
+int check(harp_ctx *ctx, const harp_attention *g, const Tensor *t, int count, const void *workspace, size_t workspace_bytes, Plan *q, Plan *k,
+          Space *space) {
     const int rc = attention_sizes(ctx, g);
     if (rc != HARP_OK) return rc;
     if (g->type != HARP_BF16 && g->type != HARP_F16) return fail(ctx, HARP_ERR_INVALID_ARG, "type must be HARP_BF16 or HARP_F16");
@@ -972,16 +1023,21 @@ int check(harp_ctx *ctx, const harp_attention *g, const Tensor *t, int count, co
         if (t[i].written && !clear_of_each_other(t[i].tokens, t[i].heads, g->head, t[i].token, t[i].step))
             return fail(ctx, HARP_ERR_SHAPE, "%s: elements lie over each other", t[i].name);
     }
-    const size_t need = space_for(ctx, g).all;
+    *q = plan_queries(ctx, g, g->causal);
+    if (k) *k = plan_keys(ctx, g, g->causal);
+    *space = space_for(g, q, k);
+    const size_t need = space->all;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < need)
         return fail(ctx, HARP_ERR_WORKSPACE, "the workspace needs %zu bytes, aligned to 256", need);
-    const Plan q = plan_queries(ctx, g), k = plan_keys(ctx, g);
-    const int64_t grid = int64_t(1) << 23;               // a launch has less than 2^32 threads
-    const bool q_fits = q.shares == 1 || (tiles_of(g->tokens_q, g->heads, g->batch, kJoinRows) < grid &&
-                                          tiles_of(g->tokens_q, g->heads / g->kv_heads, g->batch, kJoinRows) * g->kv_heads < grid);
-    const bool k_fits = k.shares == 1 || tiles_of(g->tokens_k, g->kv_heads, g->batch, kJoinRows) < grid;
-    if (q.tiles * q.shares * g->kv_heads >= grid || k.tiles * k.shares * g->kv_heads >= grid || !q_fits || !k_fits ||
-        tiles_of(g->tokens_q, g->heads, g->batch, kPeakRows) + tiles_of(g->tokens_k, g->kv_heads, g->batch, kPeakRows) >= grid)
+    const int64_t grid = int64_t(1) << 23, half = int64_t(1) << 31;       // a launch has less than 2^32 threads
+    bool fits = q->places() * q->shares * g->kv_heads < grid && tiles_of(g->tokens_q, g->heads, g->batch, kMeasured) < half &&
+                tiles_of(g->tokens_k, g->kv_heads, g->batch, kMeasured) < half;
+    if (q->shares > 1)
+        fits = fits && tiles_of(g->tokens_q, g->heads, g->batch, kJoinRows) < grid &&
+               tiles_of(g->tokens_q, g->heads / g->kv_heads, g->batch, kJoinRows) * g->kv_heads < grid;
+    if (k) fits = fits && k->places() * k->shares * g->kv_heads < grid;
+    if (k && k->shares > 1) fits = fits && tiles_of(g->tokens_k, g->kv_heads, g->batch, kJoinRows) < grid;
+    if (!fits)
         return fail(ctx, HARP_ERR_SHAPE, "too many rows for one launch");
     const hipError_t e = hipSetDevice(ctx->device);
     return e == hipSuccess ? HARP_OK : hip_fail(ctx, e, "hipSetDevice");
@@ -1006,26 +1062,24 @@ int launched(harp_ctx *ctx) {
 }
 
 template <typename T, int D> void launch_forward(const Plan &p, const Call &a, const Shares &shares, hipStream_t st) {
-    const dim3 grid(uint32_t(p.tiles * p.shares * a.kv_heads));
+    const dim3 grid(uint32_t(p.places() * p.shares * a.kv_heads));
     if (p.waves == 8) forward<T, D, 8><<<grid, dim3(512), 0, st>>>(a, int(p.tiles), shares);
     else forward<T, D, 4><<<grid, dim3(256), 0, st>>>(a, int(p.tiles), shares);
 }
 template <typename T, int D> void launch_queries(const Plan &p, const Call &a, const Grads &g, const Shares &shares, hipStream_t st) {
-    const dim3 grid(uint32_t(p.tiles * p.shares * a.kv_heads));
+    const dim3 grid(uint32_t(p.places() * p.shares * a.kv_heads));
     if (p.waves == 8) grad_queries<T, D, 8><<<grid, dim3(512), 0, st>>>(a, g, int(p.tiles), shares);
     else grad_queries<T, D, 4><<<grid, dim3(256), 0, st>>>(a, g, int(p.tiles), shares);
 }
 template <typename T, int D> void launch_keys(const Plan &p, const Call &a, const Grads &g, const Shares &shares, hipStream_t st) {
-    const dim3 grid(uint32_t(p.tiles * p.shares * a.kv_heads));
+    const dim3 grid(uint32_t(p.places() * p.shares * a.kv_heads));
     if (p.waves == 8) grad_keys<T, D, 8><<<grid, dim3(512), 0, st>>>(a, g, int(p.tiles), shares);
     else grad_keys<T, D, 4><<<grid, dim3(256), 0, st>>>(a, g, int(p.tiles), shares);
 }
 
-template <typename T> void run_forward(const harp_ctx *ctx, const harp_attention *g, unsigned char *ws, hipStream_t st) {
+template <typename T> void run_forward(const harp_attention *g, const Plan &p, const Space &space, unsigned char *ws, hipStream_t st) {
     const Call a = call_of(g);
-    const Plan p = plan_queries(ctx, g);
-    const Space space = space_for(ctx, g);
-    const Shares shares = {p.shares, reinterpret_cast<float *>(ws + space.sums), reinterpret_cast<float *>(ws + space.stats)};
+    const Shares shares = {p.shares, p.paired, reinterpret_cast<float *>(ws + space.sums), reinterpret_cast<float *>(ws + space.stats)};
     if (g->head <= 64) launch_forward<T, 64>(p, a, shares, st);
     else if (g->head <= 96) launch_forward<T, 96>(p, a, shares, st);
     else launch_forward<T, 128>(p, a, shares, st);
@@ -1035,22 +1089,20 @@ template <typename T> void run_forward(const harp_ctx *ctx, const harp_attention
     }
 }
 
-template <typename T> void run_backward(const harp_ctx *ctx, const harp_attention *g, const harp_attention_grads *d, unsigned char *ws, hipStream_t st) {
+template <typename T>
+void run_backward(const harp_attention *g, const harp_attention_grads *d, const Plan &of_queries, const Plan &of_keys, const Space &space,
+                  unsigned char *ws, hipStream_t st) {
     const Call a = call_of(g);
-    const Space space = space_for(ctx, g);
     const Grads grads = {d->dO, d->do_token, d->do_step, d->dq_token, d->dq_step, d->dk_token, d->dk_step, d->dv_token, d->dv_step,
-                         d->dQ, d->dK, d->dV, reinterpret_cast<float *>(ws), reinterpret_cast<uint32_t *>(ws + space.peaks), g->scale};
+                         d->dQ, d->dK, d->dV, reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + space.peaks), g->scale};
     const int64_t rows = g->tokens_q * g->heads;
     float *sums = reinterpret_cast<float *>(ws + space.sums);
-    if (rows) deltas<T><<<dim3(uint32_t(rows < (1 << 20) ? (rows + 15) / 16 : 1 << 16)), dim3(256), 0, st>>>(a, grads);
-    if (Range<T>::kNarrow) {
-        const int64_t of_q = tiles_of(g->tokens_q, g->heads, g->batch, kPeakRows), of_k = tiles_of(g->tokens_k, g->kv_heads, g->batch, kPeakRows);
-        no_peaks<<<dim3(1), dim3(2), 0, st>>>(grads.peaks);
-        find_peaks<T><<<dim3(uint32_t(of_q + of_k)), dim3(256), 0, st>>>(a, grads, int(of_q));
-    }
+    const int of_q = int(tiles_of(g->tokens_q, g->heads, g->batch, kMeasured)), of_k = int(tiles_of(g->tokens_k, g->kv_heads, g->batch, kMeasured));
+    const int groups = Range<T>::kNarrow ? kPeaks : of_q < 1 ? 1 : of_q < 8192 ? of_q : 8192;
+    measure<T><<<dim3(Range<T>::kNarrow ? 2 * kPeaks : groups), dim3(256), 0, st>>>(a, grads, of_q, of_k, groups);
     if (d->dQ && rows) {
-        const Plan p = plan_queries(ctx, g);
-        const Shares shares = {p.shares, sums, nullptr};
+        const Plan &p = of_queries;
+        const Shares shares = {p.shares, p.paired, sums, nullptr};
         if (g->head <= 64) launch_queries<T, 64>(p, a, grads, shares, st);
         else if (g->head <= 96) launch_queries<T, 96>(p, a, grads, shares, st);
         else launch_queries<T, 128>(p, a, grads, shares, st);
@@ -1059,8 +1111,8 @@ template <typename T> void run_backward(const harp_ctx *ctx, const harp_attentio
                 a.q_begin, a.tokens_q, a.batch, a.heads, a.head, sums, p.shares, rows * a.head, static_cast<T *>(d->dQ), d->dq_token, d->dq_step);
     }
     if ((d->dK || d->dV) && g->tokens_k) {
-        const Plan p = plan_keys(ctx, g);
-        const Shares shares = {p.shares, sums, nullptr};
+        const Plan &p = of_keys;
+        const Shares shares = {p.shares, p.paired, sums, nullptr};
         if (g->head <= 64) launch_keys<T, 64>(p, a, grads, shares, st);
         else if (g->head <= 96) launch_keys<T, 96>(p, a, grads, shares, st);
         else launch_keys<T, 128>(p, a, grads, shares, st);
@@ -1079,7 +1131,13 @@ extern "C" {
 
 size_t harp_attention_workspace_bytes(harp_ctx *ctx, const harp_attention *g) {
     if (!ctx || !g || attention_sizes(ctx, g) != HARP_OK) return 0;
-    return space_for(ctx, g).all;
+    size_t most = 0;
+    for (int causal = 0; causal < 2; ++causal) {
+        const Plan q = plan_queries(ctx, g, causal), k = plan_keys(ctx, g, causal);
+        const size_t all = space_for(g, &q, &k).all;
+        most = all > most ? all : most;
+    }
+    return most;
 }
 
 int harp_attention_forward(harp_ctx *ctx, const harp_attention *g, void *workspace, size_t workspace_bytes, void *hip_stream) {
@@ -1090,11 +1148,13 @@ int harp_attention_forward(harp_ctx *ctx, const harp_attention *g, void *workspa
                         {"K", g->K, some ? g->tokens_k : 0, g->kv_heads, g->k_token, g->k_step, true, false},
                         {"V", g->V, some ? g->tokens_k : 0, g->kv_heads, g->v_token, g->v_step, true, false},
                         {"O", g->O, g->tokens_q, g->heads, g->o_token, g->o_step, true, true}};
-    const int rc = check(ctx, g, t, 4, workspace, workspace_bytes);
+    Plan p;
+    Space space;
+    const int rc = check(ctx, g, t, 4, workspace, workspace_bytes, &p, nullptr, &space);
     if (rc != HARP_OK || !some) return rc;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (g->type == HARP_BF16) run_forward<__bf16>(ctx, g, static_cast<unsigned char *>(workspace), st);
-    else run_forward<_Float16>(ctx, g, static_cast<unsigned char *>(workspace), st);
+    if (g->type == HARP_BF16) run_forward<__bf16>(g, p, space, static_cast<unsigned char *>(workspace), st);
+    else run_forward<_Float16>(g, p, space, static_cast<unsigned char *>(workspace), st);
     return launched(ctx);
 }
 
@@ -1111,11 +1171,13 @@ int harp_attention_backward(harp_ctx *ctx, const harp_attention *g, const harp_a
                         {"dQ", d->dQ, g->tokens_q, g->heads, d->dq_token, d->dq_step, false, true},
                         {"dK", d->dK, g->tokens_k, g->kv_heads, d->dk_token, d->dk_step, false, true},
                         {"dV", d->dV, g->tokens_k, g->kv_heads, d->dv_token, d->dv_step, false, true}};
-    const int rc = check(ctx, g, t, 8, workspace, workspace_bytes);
+    Plan q, k;
+    Space space;
+    const int rc = check(ctx, g, t, 8, workspace, workspace_bytes, &q, &k, &space);
     if (rc != HARP_OK) return rc;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (g->type == HARP_BF16) run_backward<__bf16>(ctx, g, d, static_cast<unsigned char *>(workspace), st);
-    else run_backward<_Float16>(ctx, g, d, static_cast<unsigned char *>(workspace), st);
+    if (g->type == HARP_BF16) run_backward<__bf16>(g, d, q, k, space, static_cast<unsigned char *>(workspace), st);
+    else run_backward<_Float16>(g, d, q, k, space, static_cast<unsigned char *>(workspace), st);
     return launched(ctx);
 }
 
