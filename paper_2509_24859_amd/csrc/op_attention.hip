@@ -120,10 +120,27 @@ __device__ __forceinline__ bool locate(const int32_t *begin, int64_t tokens, int
     return false;
 }
 
-// Workgroups go to the 8 dies in turn, each with an L2 of its own: a die takes neighbours, which share keys.
-__device__ __forceinline__ int work_of(int id, int n) {
-    const int die = id % kDies, each = n / kDies, more = n % kDies;
-    return id / kDies + die * each + (die < more ? die : more);
+// What a workgroup takes of `places` tiles, the heaviest first, of every kv head, shared out.  Workgroups go to the 8 dies in turn, each
+// with an L2 of its own: a die takes neighbours, which share keys.  Within a die they go to its shader engines in turn, and wait
+// for room in that one: under the causal order, where tiles differ in their work, a die takes some of the heads, and the same place of
+// each comes first, then the next, so that every engine has tiles of all weights and those that follow find room where
+// the lightest end (gradients of 4,096 keys, 32 heads: 332 us, heads one after the other 448).
+struct Work { int share, kv, place; };
+__device__ __forceinline__ Work work_of(int id, int places, int kv_heads, int shares, bool causal) {
+    Work w;
+    if (causal && kv_heads % kDies == 0) {
+        const int heads = kv_heads / kDies, i = id / kDies, each = heads * shares;
+        w.place = i / each;
+        w.share = i % each % shares;
+        w.kv = id % kDies * heads + i % each / shares;
+    } else {
+        const int n = places * kv_heads * shares, die = id % kDies, each = n / kDies, more = n % kDies;
+        id = id / kDies + die * each + (die < more ? die : more);
+        w.share = id % shares;
+        w.place = id / shares % places;
+        w.kv = id / shares / places;
+    }
+    return w;
 }
 
 // LDS holds rows of D elements in pieces of 16 bytes.  It gives 256 bytes a cycle: to 16 lanes that read a piece each, or to 32
@@ -273,11 +290,6 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
         wave_most = __builtin_amdgcn_readfirstlane(wave_most);
         wave_least = __builtin_amdgcn_readfirstlane(wave_least);
 
-        Frag q[D / 16];
-        const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) q[k] = eight<T>(from + 16 * k + 8 * h, mine.limit >= 0 && 16 * k + 8 * h < a.head);
-        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
         const Along<T, D> along;
         const Across<T, D> across;
         f32x16 o[D / 32] = {}, p = {}, n = {};
@@ -295,6 +307,13 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
         auto ask_v = [&](int t) {
             if (t < end) sv.ask(a.v_token, s.used - t * kKeys, a.head);
         };
+        ask_k(first);
+        ask_v(first);
+        Frag q[D / 16];
+        const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) q[k] = eight<T>(from + 16 * k + 8 * h, mine.limit >= 0 && 16 * k + 8 * h < a.head);
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
         // Scores of half a tile of keys; weighted values of one.
         auto scores = [&](int buffer, int half) {
             f32x16 x = {};
@@ -400,8 +419,6 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
             if (refer(now)) shrink_o();
             weights(now, w);
         };
-        ask_k(first);
-        ask_v(first);
         if (first < end) {
             sk.put(lk[0]);
             sv.put(lv[0]);
@@ -445,13 +462,16 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
         if (first < end) edge(2 * end, p, n);                        // the last weighted values
         if (mine.limit < 0) return;
         sum += other_half(sum);
+        if (sum == 0) {                                              // no key seen, or none of any weight: zeros whatever the values
+#pragma unroll
+            for (int m = 0; m < D / 32; ++m) o[m] = f32x16{};
+        }
         if (shares.count > 1) {
             const int64_t at = (int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head;
             if (h == 0) {
                 shares.stats[2 * at] = top;
                 shares.stats[2 * at + 1] = sum;
             }
-            if (sum == 0) return;                            // nothing that the join looks at
 #pragma unroll
             for (int m = 0; m < D / 32; ++m)
 #pragma unroll
@@ -473,12 +493,11 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
             }
     };
     // Tiles of rows that see most keys first; with shares.paired a workgroup takes one of them and one of the least in turn.
-    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, places = shares.paired ? (tiles + 1) / 2 : tiles;
-    const int kv = work / shares.count / places, place = work / shares.count % places;
+    const Work work = work_of(blockIdx.x, shares.paired ? (tiles + 1) / 2 : tiles, a.kv_heads, shares.count, a.causal);
 #pragma unroll 1
-    for (int turn = 0; turn < (shares.paired && place != tiles - 1 - place ? 2 : 1); ++turn) {
+    for (int turn = 0; turn < (shares.paired && work.place != tiles - 1 - work.place ? 2 : 1); ++turn) {
         if (turn) __syncthreads();               // all have read what lies in LDS
-        one(share, kv, turn ? place : tiles - 1 - place);
+        one(work.share, work.kv, turn ? work.place : tiles - 1 - work.place);
     }
 }
 
@@ -491,18 +510,38 @@ template <typename T> __global__ __launch_bounds__(kJoinRows * 32) void forward_
     const Row mine = row_of(a, s, blockIdx.x / tiles, tile * kJoinRows + threadIdx.x / 32);
     if (mine.limit < 0) return;
     const int64_t each = a.tokens_q * a.heads, at = mine.token * a.heads + mine.head;
-    float top = -INFINITY;
-    for (int i = 0; i < shares.count; ++i) top = fmaxf(top, shares.stats[2 * (i * each + at)]);
-    float sum = 0;
-    f32x4 o = {0, 0, 0, 0};
-    const int col = threadIdx.x % 32 * 4;
-    for (int i = 0; i < shares.count; ++i) {
+    // a lane looks at two shares' reference and sum
+    const int lane = threadIdx.x % 32, col = lane * 4;
+    float refer[2], part[2], top = -INFINITY, sum = 0;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = lane + 32 * k;
         const float *stats = shares.stats + 2 * (i * each + at);
-        if (stats[1] == 0) continue;
-        const float w = stats[0] == top ? 1.0f : __builtin_amdgcn_exp2f(stats[0] - top);
-        sum += w * stats[1];
-        if (col < a.head) o += w * load4(shares.sums + (i * each + at) * a.head + col);
+        part[k] = i < shares.count ? stats[1] : 0;
+        refer[k] = part[k] == 0 ? -INFINITY : stats[0];
+        top = fmaxf(top, refer[k]);
     }
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    float weight[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        weight[k] = part[k] == 0 ? 0.0f : refer[k] == top ? 1.0f : __builtin_amdgcn_exp2f(refer[k] - top);
+        sum += weight[k] * part[k];
+    }
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) sum += __shfl_xor(sum, d);
+    f32x4 o = {0, 0, 0, 0};
+    const float *sums = shares.sums + at * a.head + (col < a.head ? col : 0);
+    int i = 0;
+    for (; i + 8 <= shares.count; i += 8) {
+        f32x4 x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = load4(sums + (i + k) * each * a.head);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o += __shfl(i < 32 ? weight[0] : weight[1], (i + k) % 32, 32) * x[k];
+    }
+    for (; i < shares.count; ++i) o += __shfl(i < 32 ? weight[0] : weight[1], i % 32, 32) * load4(sums + i * each * a.head);
     const float scale = sum == 0 ? 0.0f : 1.0f / sum;    // no key: zeros; scores that are NaN: NaN
     if (col < a.head) store4(static_cast<T *>(a.o) + mine.token * a.o_token + mine.head * a.o_step + col, o * scale);
     if (a.lse && col == 0) a.lse[mine.head * a.tokens_q + mine.token] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
@@ -521,7 +560,7 @@ struct Grads {
 // Weights and their gradients on their way into the matrix instructions.  bfloat16 has the range of 32 bits.  In float16 weights go in
 // times 2^12 (they are normal numbers down to 2^-26: 10^5 equal ones of a row are still rounded to 2^-11 of themselves), and
 // gradients times a power of two taken from the largest norms: |P (dP - D)| <= 2 |dO_i| |v_j|, which is brought to 2^14 at most.
-constexpr int kPeaks = 256;
+constexpr int kPeaks = 512;
 template <typename T> struct Range {
     static constexpr bool kNarrow = sizeof(T) == 2 && __is_same(T, _Float16);
     static constexpr float kShift = kNarrow ? 12.0f : 0.0f, kWeight = kNarrow ? 0.000244140625f : 1.0f;
@@ -546,8 +585,8 @@ template <typename T> struct Range {
 };
 
 // Sums over channels of dO O of every row of a sequence, 16 lanes a row; in HARP_F16 the largest norms of dO's rows too, and, by as many
-// workgroups more (kPeaks), of V's.  A workgroup takes a tile of 64 rows in `groups`.
-constexpr int kMeasured = 64;
+// workgroups more (kPeaks), of V's.  A workgroup takes a tile of 128 rows in `groups`.
+constexpr int kMeasured = 128;
 template <typename T>
 __global__ __launch_bounds__(256) void measure(Call a, Grads g, int of_q, int of_k, int groups) {
     __shared__ uint32_t highest[4];
@@ -619,15 +658,6 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
         }
         wave_most = __builtin_amdgcn_readfirstlane(wave_most);
         wave_least = __builtin_amdgcn_readfirstlane(wave_least);
-        Frag q[D / 16], d_o[D / 16];
-        const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
-        const T *from_do = static_cast<const T *>(g.d_o) + mine.token * g.do_token + mine.head * g.do_step;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            q[k] = eight<T>(from + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
-            d_o[k] = eight<T>(from_do + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
-        }
-        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
         Along<T, D> along;
         Across<T, D> across;
         f32x16 dq[D / 32] = {};
@@ -641,6 +671,16 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
             sk.ask(a.k_token, s.used - t * kKeys, a.head);
             sv.ask(a.v_token, s.used - t * kKeys, a.head);
         };
+        ask(first);
+        Frag q[D / 16], d_o[D / 16];
+        const T *from = static_cast<const T *>(a.q) + mine.token * a.q_token + mine.head * a.q_step;
+        const T *from_do = static_cast<const T *>(g.d_o) + mine.token * g.do_token + mine.head * g.do_step;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k) {
+            q[k] = eight<T>(from + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
+            d_o[k] = eight<T>(from_do + 16 * k + 8 * h, here && 16 * k + 8 * h < a.head);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): or the loop would wait for these, and with them for its own
         // A tile's matrix instructions, one operand of each from LDS, and what goes on under them:
         //   S of the first 32 keys;  their dP, exponentials;  S of the others, dS of the first;  dP, exponentials;  dQ of the first,
         //   dS of the others;  dQ of those.
@@ -677,7 +717,6 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
                 __builtin_amdgcn_sched_barrier(0);
             });
         };
-        ask(first);
         if (first < end) {
             sk.put(lk[0]);
             sv.put(lv[0]);
@@ -720,12 +759,11 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
             }
     };
     // Tiles of rows that see most keys first; with shares.paired a workgroup takes one of them and one of the least in turn.
-    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, places = shares.paired ? (tiles + 1) / 2 : tiles;
-    const int kv = work / shares.count / places, place = work / shares.count % places;
+    const Work work = work_of(blockIdx.x, shares.paired ? (tiles + 1) / 2 : tiles, a.kv_heads, shares.count, a.causal);
 #pragma unroll 1
-    for (int turn = 0; turn < (shares.paired && place != tiles - 1 - place ? 2 : 1); ++turn) {
+    for (int turn = 0; turn < (shares.paired && work.place != tiles - 1 - work.place ? 2 : 1); ++turn) {
         if (turn) __syncthreads();               // all have read what lies in LDS
-        one(share, kv, turn ? place : tiles - 1 - place);
+        one(work.share, work.kv, turn ? work.place : tiles - 1 - work.place);
     }
 }
 
@@ -741,9 +779,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
     __shared__ __align__(16) T lv[kCols * D];
     __shared__ __align__(16) float l_lse[2][kBack], l_delta[2][kBack];
     __shared__ __align__(16) int l_limit[2][kBack];
-    const int work = work_of(blockIdx.x, gridDim.x), share = work % shares.count, kv = work / shares.count / tiles;
+    const Work work = work_of(blockIdx.x, tiles, a.kv_heads, shares.count, a.causal);
+    const int share = work.share, kv = work.kv;
     int b, tile;
-    if (!locate(a.k_begin, a.tokens_k, a.batch, 1, kCols, work / shares.count % tiles, b, tile)) return;
+    if (!locate(a.k_begin, a.tokens_k, a.batch, 1, kCols, work.place, b, tile)) return;
     const Sequence s = sequence(a, b);
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, h = lane / 32;
     const int key0 = tile * kCols, key = key0 + wave * 32 + lane % 32, rows = int(int64_t(s.nq) * a.group);
@@ -758,12 +797,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
     const T *from_k = static_cast<const T *>(a.k) + (s.k0 + (used ? key : 0)) * a.k_token + kv * a.k_step;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) k[i] = eight<T>(from_k + 16 * i + 8 * h, used && 16 * i + 8 * h < a.head);
-    {   // V stays in LDS: dK and dV leave no room for it in registers
-        Stage<T, D, kCols, kThreads> sv;
-        const T *values = static_cast<const T *>(a.v) + (s.k0 + key0) * a.v_token + kv * a.v_step;
-        sv.ask([&](int row) { return values + row * a.v_token; }, s.used - key0, a.head);
-        sv.put(lv);
-    }
+    // V stays in LDS: dK and dV leave no room for it in registers
+    Stage<T, D, kCols, kThreads> sv;
+    const T *values = static_cast<const T *>(a.v) + (s.k0 + key0) * a.v_token + kv * a.v_step;
+    sv.ask([&](int row) { return values + row * a.v_token; }, s.used - key0, a.head);
     Along<T, D> along;
     Across<T, D> across;
     f32x16 dk[D / 32] = {}, dv[D / 32] = {};
@@ -794,10 +831,9 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         sd.put(ld[at]);
         if (threadIdx.x < kBack) l_lse[at][threadIdx.x] = lse, l_delta[at][threadIdx.x] = delta, l_limit[at][threadIdx.x] = limit;
     };
-    if (first < end) {
-        ask(first);
-        put(0);
-    }
+    if (first < end) ask(first);
+    sv.put(lv);
+    if (first < end) put(0);
     __syncthreads();
     // A step's matrix instructions and what goes on under them:  S;  dP, weights;  dV, their gradients;  dK.
     constexpr int kPart = D / 16, kAhead = 2;
@@ -941,7 +977,7 @@ Plan plan_for(const harp_ctx *ctx, int64_t tokens, int64_t times, int batch, int
         const int64_t side = 32 * waves, slots = int64_t(ctx->n_cu) * 8 / waves;
         const int64_t busy = (rows > side ? (rows + side - 1) / side : 1) * batch * kv_heads;       // tiles that have something to do
         for (int shares : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            if (shares > 1 && through < int64_t(shares) * 4 * unit) break;
+            if (shares > 1 && through < int64_t(shares) * unit) break;
             const int64_t items = busy * shares;
             const double steps = double((through + unit - 1) / unit) / shares;
             const double each = step * channels * (waves == 4 && items <= ctx->n_cu ? 0.6 : 1.0);
