@@ -653,7 +653,7 @@ int harp_rotary_frequencies(int32_t turned, double base, int32_t scaling, double
  * where they are multiplied with V, K, Q and dO (what the matrix instructions take; in HARP_F16 the gradients times a power
  * of two that keeps them from both ends of its range).
  * head a multiple of 8, at most HARP_ATTENTION_MAX_HEAD; heads a multiple of kv_heads, heads <= 2^14;
- * 0 <= tokens < 2^31, tokens_q * heads / kv_heads < 2^31; 1 <= batch <= 2^20. */
+ * 0 <= tokens < 2^30, tokens_q * heads / kv_heads < 2^30; 1 <= batch <= 2^20. */
 #define HARP_ATTENTION_MAX_HEAD 128
 typedef struct {
     int64_t tokens_q, tokens_k;

@@ -151,20 +151,25 @@ template <int D> __device__ __forceinline__ int moved(int row, int piece) {
     if (D == 64) return piece ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
     return piece ^ (row >> 2 & 3);
 }
-// Fragments of 32 rows by 16 columns: lane l has row l % 32 and columns 16 k + 8 (l / 32) .. + 7.  Only low bits of a place in the
-// row are moved: another k is another place by those bits, the rest is in the instruction.  refresh(): the places are not kept in
-// registers over it.
+template <typename T> __device__ __forceinline__ uint32_t lds_address(const T *p) {
+    return uint32_t(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void *)p));
+}
+// Fragments of 32 rows by 16 columns: lane l has row l % 32 and columns 16 k + 8 (l / 32) .. + 7.  `at` is the lane's place in LDS, rows
+// aligned to 256 bytes.  Only low bits of a place in the row are moved: another k is another place by those bits, and what else is
+// known when compiled is in the instruction.  refresh(): the places are not kept in registers over it.
 template <typename T, int D> struct Along {
     static constexpr int N = D == 96 ? 2 : D / 16;
-    uint32_t at;                     // bytes
-    __device__ __forceinline__ Along() {
+    uint32_t at;
+    __device__ __forceinline__ explicit Along(const T *lds) {
         const int lane = threadIdx.x % kWave, row = lane % 32;
-        at = uint32_t(row * D + moved<D>(row, lane / 32) * 8) * 2;
+        at = lds_address(lds) + uint32_t(row * D + moved<D>(row, lane / 32) * 8) * 2;
     }
     __device__ __forceinline__ void refresh() { asm volatile("" : "+v"(at)); }
     // row0 a multiple of 32
-    __device__ __forceinline__ typename Mfma32<T>::Frag read(const T *lds, int row0, int k) const {
-        return *reinterpret_cast<const typename Mfma32<T>::Frag *>(reinterpret_cast<const char *>(lds + row0 * D + k / N * (N * 16)) + (at ^ uint32_t(k % N * 32)));
+    __device__ __forceinline__ typename Mfma32<T>::Frag read(int row0, int k) const {
+        typedef __attribute__((address_space(3))) const char *Bytes;
+        typedef __attribute__((address_space(3))) const typename Mfma32<T>::Frag *Lds;
+        return *(Lds)((Bytes)(uintptr_t)(at ^ uint32_t(k % N * 32)) + (row0 * D + k / N * (N * 16)) * 2);
     }
 };
 // Fragments of 32 columns by 16 rows, transposed: lane l has column 32 m + l % 32 and, h = l / 32, rows row0 + 4 h .. + 3 and
@@ -172,17 +177,19 @@ template <typename T, int D> struct Along {
 template <typename T, int D> struct Across {
     static constexpr int N = D == 96 ? 1 : D / 32;
     uint32_t at;
-    __device__ __forceinline__ Across() {
+    __device__ __forceinline__ explicit Across(const T *lds) {
         const int lane = threadIdx.x % kWave, i = lane % 16, row = lane / 32 * 4 + i / 4;
-        at = uint32_t(row * D + moved<D>(row, lane / 16 % 2 * 2 + i % 4 / 2) * 8 + i % 2 * 4) * 2;
+        at = lds_address(lds) + uint32_t(row * D + moved<D>(row, lane / 16 % 2 * 2 + i % 4 / 2) * 8 + i % 2 * 4) * 2;
     }
     __device__ __forceinline__ void refresh() { asm volatile("" : "+v"(at)); }
     // row0 a multiple of 16; a row 8 further on has its pieces moved by 2 more
-    __device__ __forceinline__ typename Mfma32<T>::Frag read(const T *lds, int row0, int m) const {
+    __device__ __forceinline__ typename Mfma32<T>::Frag read(int row0, int m) const {
+        typedef __attribute__((address_space(3))) char *Bytes;
         typedef __attribute__((address_space(3))) s16x4 *Lds;
-        const char *p = reinterpret_cast<const char *>(lds + row0 * D + m / N * (N * 32));
+        const int more = (row0 * D + m / N * (N * 32)) * 2;
         const uint32_t lo = at ^ uint32_t(m % N * 64), hi = lo ^ 32;
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + lo)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 16 * D + hi));
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)((Bytes)(uintptr_t)lo + more));
+        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)((Bytes)(uintptr_t)hi + more + 16 * D));
         const s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         return __builtin_bit_cast(typename Mfma32<T>::Frag, v);
     }
@@ -268,8 +275,8 @@ template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, Shares shares) {
     constexpr int kThreads = WAVES * kWave, kRows = WAVES * 32;
     typedef typename Mfma32<T>::Frag Frag;
-    __shared__ __align__(16) T lk[2][kKeys * D];
-    __shared__ __align__(16) T lv[2][kKeys * D];
+    __shared__ __align__(1024) T lds[4][kKeys * D];               // two tiles of K, two of V
+    T(*const lk)[kKeys * D] = lds, (*const lv)[kKeys * D] = lds + 2;
     auto one = [&](int share, int kv, int id) {
         int b, tile;
         if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kRows, id, b, tile)) return;
@@ -290,8 +297,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
         wave_most = __builtin_amdgcn_readfirstlane(wave_most);
         wave_least = __builtin_amdgcn_readfirstlane(wave_least);
 
-        const Along<T, D> along;
-        const Across<T, D> across;
+        const Along<T, D> along(lds[0]);
+        const Across<T, D> across(lds[0]);
         f32x16 o[D / 32] = {}, p = {}, n = {};
         Frag w[2] = {};
         float top = -INFINITY, against = 0, sum = 0, shrink = 1;
@@ -318,14 +325,14 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
         auto scores = [&](int buffer, int half) {
             f32x16 x = {};
 #pragma unroll
-            for (int k = 0; k < D / 16; ++k) x = Mfma32<T>::run(along.read(lk[buffer], half * 32, k), q[k], x);
+            for (int k = 0; k < D / 16; ++k) x = Mfma32<T>::run(along.read(buffer * kKeys + half * 32, k), q[k], x);
             return x;
         };
         auto weigh = [&](int buffer, int half) {
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int m = 0; m < D / 32; ++m) o[m] = Mfma32<T>::run(across.read(lv[buffer], half * 32 + 16 * k, m), w[k], o[m]);
+                for (int m = 0; m < D / 32; ++m) o[m] = Mfma32<T>::run(across.read((2 + buffer) * kKeys + half * 32 + 16 * k, m), w[k], o[m]);
         };
         // Of step i's scores p: hides what a row does not see; the reference that exponents are taken against follows the maximum only
         // when that has grown by 2^8 over it (sums in 32 bits and weights of 16 have room for the factor), and o has then to
@@ -372,8 +379,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
             constexpr int kPairs = D / 16, kAhead = 2;
             Frag kf[kAhead + 1], vf[kAhead + 1], x[2];
             auto read = [&](int j) {
-                kf[j % (kAhead + 1)] = along.read(lk[k_buffer], half * 32, j);
-                vf[j % (kAhead + 1)] = across.read(lv[v_buffer], half * 32 + j / (D / 32) * 16, j % (D / 32));
+                kf[j % (kAhead + 1)] = along.read(k_buffer * kKeys + half * 32, j);
+                vf[j % (kAhead + 1)] = across.read((2 + v_buffer) * kKeys + half * 32 + j / (D / 32) * 16, j % (D / 32));
             };
             auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
 #pragma unroll
@@ -633,8 +640,8 @@ template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g, int tiles, Shares shares) {
     constexpr int kThreads = WAVES * kWave, kRows = WAVES * 32;
     typedef typename Mfma32<T>::Frag Frag;
-    __shared__ __align__(16) T lk[2][kKeys * D];
-    __shared__ __align__(16) T lv[2][kKeys * D];
+    __shared__ __align__(1024) T lds[4][kKeys * D];               // two tiles of K, two of V
+    T(*const lk)[kKeys * D] = lds, (*const lv)[kKeys * D] = lds + 2;
     auto one = [&](int share, int kv, int id) {
         int b, tile;
         if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kRows, id, b, tile)) return;
@@ -658,8 +665,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
         }
         wave_most = __builtin_amdgcn_readfirstlane(wave_most);
         wave_least = __builtin_amdgcn_readfirstlane(wave_least);
-        Along<T, D> along;
-        Across<T, D> across;
+        Along<T, D> along(lds[0]);
+        Across<T, D> across(lds[0]);
         f32x16 dq[D / 32] = {};
         const T *keys = static_cast<const T *>(a.k) + (s.k0 + first * kKeys) * a.k_token + kv * a.k_step;
         const T *values = static_cast<const T *>(a.v) + (s.k0 + first * kKeys) * a.v_token + kv * a.v_step;
@@ -691,8 +698,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
             auto read = [&](auto n) {
                 constexpr int part = n / kPart, j = n % kPart;
                 Frag &to = f[n % (kAhead + 1)];
-                if (part < 4) to = along.read(part % 2 ? lv[buffer] : lk[buffer], part / 2 * 32, j);
-                else to = across.read(lk[buffer], (part - 4) * 32 + j / (D / 32) * 16, j % (D / 32));
+                if (part < 4) to = along.read((part % 2 * 2 + buffer) * kKeys + part / 2 * 32, j);
+                else to = across.read(buffer * kKeys + (part - 4) * 32 + j / (D / 32) * 16, j % (D / 32));
             };
             auto exponential = [&](int u, int e) { p[u][e] = __builtin_amdgcn_exp2f(fmaf(p[u][e], a.c, -lse)); };
             auto gradient = [&](int u, int e) {
@@ -774,9 +781,8 @@ template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, int tiles, Shares shares) {
     constexpr int kThreads = WAVES * kWave, kCols = WAVES * 32;
     typedef typename Mfma32<T>::Frag Frag;
-    __shared__ __align__(16) T lq[2][kBack * D];
-    __shared__ __align__(16) T ld[2][kBack * D];
-    __shared__ __align__(16) T lv[kCols * D];
+    __shared__ __align__(1024) T lds[4][kBack * D];               // two steps of Q, two of dO
+    __shared__ __align__(1024) T lv[kCols * D];
     __shared__ __align__(16) float l_lse[2][kBack], l_delta[2][kBack];
     __shared__ __align__(16) int l_limit[2][kBack];
     const Work work = work_of(blockIdx.x, tiles, a.kv_heads, shares.count, a.causal);
@@ -801,12 +807,13 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
     Stage<T, D, kCols, kThreads> sv;
     const T *values = static_cast<const T *>(a.v) + (s.k0 + key0) * a.v_token + kv * a.v_step;
     sv.ask([&](int row) { return values + row * a.v_token; }, s.used - key0, a.head);
-    Along<T, D> along;
-    Across<T, D> across;
+    // of rows in the buffer of the step, by turns one and the other; of V
+    Along<T, D> along(lds[0]), along_v(lv + wave * 32 * D);
+    Across<T, D> across(lds[0]);
     f32x16 dk[D / 32] = {}, dv[D / 32] = {};
     Stage<T, D, kBack, kThreads> sq, sd;
     const Range<T> range(g.peaks);
-    float lse = 0, delta = 0;
+    float lse = 0, delta = 0;        // as they are in memory: looked at when they are put, so that nothing waits for them before
     int limit = 0;
     auto ask = [&](int t) {
         const int r0 = row_first + t * kBack;
@@ -818,18 +825,22 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         sd.ask([&](int row) { return static_cast<const T *>(g.d_o) + place(row, g.do_token, g.do_step); }, rows - r0, a.head);
         if (threadIdx.x < kBack) {
             const Row r = row_of(a, s, kv, r0 + int(threadIdx.x));
-            const bool there = r.limit >= 0;
-            // of no row, or one that saw no key: infinity, against which every weight is 0
-            lse = there ? a.lse[r.head * a.tokens_q + r.token] * kLog2e - Range<T>::kShift : INFINITY;
-            lse = lse == -INFINITY ? INFINITY : lse;
-            delta = there ? g.delta[r.head * a.tokens_q + r.token] * range.factor : 0;
             limit = r.limit;
+            if (limit >= 0) {
+                lse = a.lse[r.head * a.tokens_q + r.token];
+                delta = g.delta[r.head * a.tokens_q + r.token];
+            }
         }
     };
     auto put = [&](int at) {
-        sq.put(lq[at]);
-        sd.put(ld[at]);
-        if (threadIdx.x < kBack) l_lse[at][threadIdx.x] = lse, l_delta[at][threadIdx.x] = delta, l_limit[at][threadIdx.x] = limit;
+        sq.put(lds[at]);
+        sd.put(lds[2 + at]);
+        if (threadIdx.x < kBack) {
+            // of no row, or one that saw no key: infinity, against which every weight is 0
+            l_lse[at][threadIdx.x] = limit < 0 || lse == -INFINITY ? INFINITY : lse * kLog2e - Range<T>::kShift;
+            l_delta[at][threadIdx.x] = limit < 0 ? 0 : delta * range.factor;
+            l_limit[at][threadIdx.x] = limit;
+        }
     };
     if (first < end) ask(first);
     sv.put(lv);
@@ -843,9 +854,9 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         auto read = [&](auto n) {
             constexpr int part = n / kPart, j = n % kPart;
             Frag &to = f[n % (kAhead + 1)];
-            if (part < 2) to = along.read(part ? ld[at] : lq[at], 0, j);
-            else to = across.read(part == 2 ? ld[at] : lq[at], j / (D / 32) * 16, j % (D / 32));
-            if (part == 1) v[n % (kAhead + 1)] = along.read(lv, wave * 32, j);
+            if (part < 2) to = along.read(part * 2 * kBack, j);
+            else to = across.read((part == 2 ? 2 * kBack : 0) + j / (D / 32) * 16, j % (D / 32));
+            if (part == 1) v[n % (kAhead + 1)] = along_v.read(0, j);
         };
         written_out<kAhead>(read);
         f32x4 against = {}, less = {};
@@ -888,8 +899,12 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         const int at = t - first & 1;
         if (t + 1 < end) ask(t + 1);
         along.refresh();
+        along_v.refresh();
         across.refresh();
         if (row_first + (t + 1) * kBack > none) rows_step(at, row_first + t * kBack < some);
+        const uint32_t other = at ? -uint32_t(kBack * D * 2) : kBack * D * 2;
+        along.at += other;
+        across.at += other;
         if (t + 1 < end) put(1 - at);
         __syncthreads();
     }
@@ -944,7 +959,7 @@ __global__ __launch_bounds__(kJoinRows * 32) void join_sums(const int32_t *begin
 
 // ---------------------------------------------------------------------------------------------- on the host
 bool sizes_fit(const harp_attention *g) {
-    const int64_t most = (int64_t(1) << 31) - 1;
+    const int64_t most = (int64_t(1) << 30) - 1;
     return g->tokens_q >= 0 && g->tokens_k >= 0 && g->tokens_q <= most && g->tokens_k <= most && g->batch >= 1 && g->batch <= 1 << 20 &&
            g->heads >= 1 && g->heads <= 1 << 14 && g->kv_heads >= 1 && g->heads % g->kv_heads == 0 && g->head >= 8 && g->head % 8 == 0 &&
            g->head <= HARP_ATTENTION_MAX_HEAD && g->tokens_q * (g->heads / g->kv_heads) <= most;

@@ -397,6 +397,6 @@ def test_refusals(monkeypatch):
     for a, kw in (((q, k, k, o, None, o, q, k, k), {}), ((q, k, k, o, lse, None, q, k, k), {}), ((q, k, k, o, lse, o, k, k, k), {}),
                   ((q, k, k, o, lse, o, q, q, k), {}), ((q, k, k, None, lse, o, q, k, k), {}), ((q, k, k, o, lse, o, q, k[:1].expand(9, 2, 16), k), {})):
         bwd(*a, **kw)
-    for sizes in ((-1, 9, 1, 4, 2, 16), (1 << 31, 9, 1, 4, 2, 16), (6, 9, 0, 4, 2, 16), (6, 9, 1, 4, 3, 16), (6, 9, 1, 4, 2, 12), (6, 9, 1, 4, 2, 136),
-                  (6, 9, 1, 0, 1, 16), (1 << 30, 9, 1, 8, 2, 16)):
+    for sizes in ((-1, 9, 1, 4, 2, 16), (1 << 30, 9, 1, 4, 2, 16), (6, 9, 0, 4, 2, 16), (6, 9, 1, 4, 3, 16), (6, 9, 1, 4, 2, 12), (6, 9, 1, 4, 2, 136),
+                  (6, 9, 1, 0, 1, 16), (1 << 29, 9, 1, 4, 2, 16)):
         refused(monkeypatch, ops.attention_workspace, ctx, *sizes)
