@@ -83,8 +83,17 @@ __device__ __forceinline__ Sequence sequence(const Call &a, int b) {
     return s;
 }
 
+// Sum over the lanes up to and with this one.
+__device__ __forceinline__ int up_to(int x) {
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int below = __shfl_up(x, d);
+        if (int(threadIdx.x % kWave) >= d) x += below;
+    }
+    return x;
+}
 // The sequence that tile `id` of `side` rows belongs to, rows being `times` the tokens of `begin`'s spans, and its place there;
-// false behind the last.  Every wavefront looks for itself, 64 sequences at a time.
+// false behind the last.  Every wavefront looks for itself: runs of up to 16 sequences a lane, then the sequences of one run.
 __device__ __forceinline__ bool locate(const int32_t *begin, int64_t tokens, int batch, int times, int side, int id, int &b, int &tile) {
     if (!begin) {
         const int each = int((tokens / batch * times + side - 1) / side);
@@ -93,29 +102,36 @@ __device__ __forceinline__ bool locate(const int32_t *begin, int64_t tokens, int
         tile = id - b * each;
         return b < batch;
     }
-    const int lane = threadIdx.x % kWave;
-    for (int first = 0; first < batch; first += kWave) {
+    const int lane = threadIdx.x % kWave, run = batch <= kWave ? 1 : 16;
+    auto tiles_of_one = [&](int i) {
+        if (i >= batch) return 0;
+        int64_t at;
+        int count;
+        span(begin, tokens, batch, i, at, count);
+        return int((int64_t(count) * times + side - 1) / side);
+    };
+    for (int first = 0; first < batch; first += kWave * run) {
         int tiles = 0;
-        if (first + lane < batch) {
-            int64_t at;
-            int count;
-            span(begin, tokens, batch, first + lane, at, count);
-            tiles = int((int64_t(count) * times + side - 1) / side);
+        for (int i = 0; i < run; ++i) tiles += tiles_of_one(first + lane * run + i);
+        int upto = up_to(tiles);
+        uint64_t past = __ballot(id < upto);
+        if (!past) {
+            id -= __builtin_amdgcn_readlane(upto, kWave - 1);
+            continue;
         }
-        int upto = tiles;
-#pragma unroll
-        for (int d = 1; d < kWave; d *= 2) {
-            const int below = __shfl_up(upto, d);
-            if (lane >= d) upto += below;
+        int at = __builtin_ctzll(past);
+        id -= __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at);
+        b = first + at * run;
+        if (run > 1) {
+            tiles = lane < run ? tiles_of_one(b + lane) : 0;
+            upto = up_to(tiles);
+            past = __ballot(id < upto);
+            at = __builtin_ctzll(past);
+            id -= __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at);
+            b += at;
         }
-        const uint64_t past = __ballot(id < upto);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            b = first + at;
-            tile = id - (__builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at));
-            return true;
-        }
-        id -= __builtin_amdgcn_readlane(upto, kWave - 1);
+        tile = id;
+        return true;
     }
     return false;
 }

@@ -350,6 +350,108 @@ def test_begins_and_counts_out_of_range_touch_nothing_else(harp):
     ctx.close()
 
 
+def _plain(q, k, v, group, causal=False):
+    """o of one sequence in 64 bits, and the sum of p |v|."""
+    import torch
+    q, k, v = (x.double() for x in (q, k, v))
+    out, mag = torch.empty_like(q), torch.empty_like(q)
+    for h in range(q.shape[1]):
+        s = q[:, h].contiguous() @ k[:, h // group].t().contiguous() * q.shape[2] ** -0.5
+        if causal:
+            s = s.masked_fill(torch.ones_like(s).triu(1 + s.shape[1] - s.shape[0]).bool(), -math.inf)
+        p = torch.softmax(s, 1)
+        out[:, h], mag[:, h] = p @ v[:, h // group].contiguous(), p @ v[:, h // group].abs().contiguous()
+    return out, mag
+
+
+def _near(got, want, mag):
+    """Weights and result rounded to 2^-8, scores' and sums' roundings within 2^-10 of the terms at these sizes."""
+    assert ((got.double() - want).abs() <= (2.0 ** -8 + 2.0 ** -10) * mag + 2.0 ** -8 * want.abs()).all()
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(harp):
+    """Keys and values 65,536 elements apart: the last ones begin behind 2^31 elements.  Queries and their gradients likewise."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    n, far = 34000, 65536
+    buf = torch.empty(n, far, dtype=torch.bfloat16, device="cuda")
+    heads = lambda at, rows: buf[:rows, at:at + 128].unflatten(1, (2, 64))  # noqa: E731
+    k, v, dk, dv = (heads(at, n) for at in (0, 1000, 2000, 3000))
+    k.copy_(torch.randn(n, 2, 64, device="cuda"))
+    v.copy_(torch.randn(n, 2, 64, device="cuda"))
+    q, do = (torch.randn(3, 4, 64, device="cuda").bfloat16() for _ in range(2))
+    o, dq, lse = torch.empty_like(q), torch.empty_like(q), torch.empty(4, 3, device="cuda")
+    ws = ops.attention_workspace(ctx, 3, n, 1, 4, 2, 64)
+    ops.harp_attention_forward(ctx, q, k, v, o, lse=lse, workspace=ws)
+    _near(o, *_plain(q, k, v, 2))
+    ops.harp_attention_backward(ctx, q, k, v, o, lse, do, dq, dk, dv, workspace=ws)
+    near = [torch.empty_like(x, memory_format=torch.contiguous_format) for x in (k, v)]
+    dq2 = torch.empty_like(dq)
+    ops.harp_attention_backward(ctx, q, k.contiguous(), v.contiguous(), o, lse, do, dq2, *near, workspace=ws)
+    assert torch.equal(dq, dq2) and torch.equal(dk, near[0]) and torch.equal(dv, near[1])
+    many = heads(4000, n)                                        # as queries, of a few keys
+    many.copy_(torch.randn(n, 2, 64, device="cuda"))
+    out, lse = heads(5000, n), torch.empty(2, n, device="cuda")
+    ops.harp_attention_forward(ctx, many, k[:5], v[:5], out, lse=lse, workspace=ops.attention_workspace(ctx, n, 5, 1, 2, 2, 64))
+    _near(out, *_plain(many, k[:5], v[:5], 1))
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_begins_on_one_side_and_keys_that_heads_share(harp):
+    """Queries packed, keys of equal lengths; one head's keys seen as four by a distance of 0."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    q, k, v = (torch.randn(n, h, 64, device="cuda").bfloat16() for n, h in ((100, 4), (90, 1), (90, 1)))
+    at = [0, 17, 17, 100]
+    begin = torch.tensor(at, dtype=torch.int32, device="cuda")
+    for kv in (1, 4):
+        o = torch.empty_like(q)
+        wide = [x.expand(90, kv, 64) for x in (k, v)]
+        ops.harp_attention_forward(ctx, q, *wide, o, q_begin=begin, workspace=ops.attention_workspace(ctx, 100, 90, 3, 4, kv, 64))
+        for b in range(3):
+            rows, keys = slice(at[b], at[b + 1]), slice(30 * b, 30 * b + 30)
+            _near(o[rows], *_plain(q[rows], k[keys], v[keys], 4))
+    ctx.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("batch", [65, 1500, 3000])
+def test_many_sequences(harp, batch):
+    """More than a wavefront's lanes, and more than one turn of them; some empty, one long."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    rng = np.random.default_rng(batch)
+    lengths = rng.integers(0, 9, batch)
+    lengths[batch // 2] = 700
+    at = [0] + np.cumsum(lengths).tolist()
+    n = at[-1]
+    q, k, v, do = (torch.randn(n, h, 64, device="cuda").bfloat16() for h in (2, 1, 1, 2))
+    begin = torch.tensor(at, dtype=torch.int32, device="cuda")
+    form = dict(q_begin=begin, k_begin=begin, causal=True, workspace=ops.attention_workspace(ctx, n, n, batch, 2, 1, 64))
+    o, lse = torch.full_like(q, 7), torch.empty(2, n, device="cuda")
+    grads = [torch.full_like(x, 7) for x in (q, k, v)]
+    ops.harp_attention_forward(ctx, q, k, v, o, lse=lse, **form)
+    ops.harp_attention_backward(ctx, q, k, v, o, lse, do, *grads, **form)
+    for b in (0, 1, 31, 63, 64, batch // 2 - 1, batch // 2, batch // 2 + 1, batch - 2, batch - 1):
+        rows = slice(at[b], at[b + 1])
+        if at[b] == at[b + 1]:
+            continue
+        _near(o[rows], *_plain(q[rows], k[rows], v[rows], 2, True))
+        m = at[b + 1] - at[b]
+        alone = [torch.empty_like(x[rows]) for x in (q, k, v)]
+        ops.harp_attention_backward(ctx, q[rows], k[rows], v[rows], o[rows], lse[:, rows].contiguous(), do[rows], *alone, causal=True,
+                                    workspace=ops.attention_workspace(ctx, m, m, 1, 2, 1, 64))
+        # sums may be shared out otherwise: the same to their roundings, half a unit of each and 2^-10 of the largest
+        assert all(((x[rows].double() - y.double()).abs() <= 2.0 ** -8 * (x[rows].double().abs() + y.double().abs()) / 2 + 2.0 ** -10 * y.abs().max()).all()
+                   for x, y in zip(grads, alone))
+    ctx.close()
+
+
 @pytest.mark.gpu
 def test_no_tokens(harp):
     import torch

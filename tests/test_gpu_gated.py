@@ -188,6 +188,27 @@ def test_streams_graphs_and_no_tokens(harp):
     ctx.close()
 
 
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(harp):
+    """Rows 2^22 elements and more apart, 600 of them."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    buf = torch.empty(600, (1 << 22) + 8, dtype=torch.bfloat16, device="cuda")
+    m, k, f = 600, 136, 72
+    x, h, z, dz = (buf[:, at:at + n] for at, n in ((0, k), (1000, f), (2000, 2 * f), (3000, 2 * f)))
+    x.copy_(torch.randn(m, k, device="cuda"))
+    w, w2, dy = (torch.randn(s, device="cuda").bfloat16() for s in ((2 * f, k), (k, f), (m, k)))
+    ws = ops.gated_workspace(ctx, m, f, k)
+    near = [torch.empty(m, n, dtype=torch.bfloat16, device="cuda") for n in (f, 2 * f, 2 * f)]
+    ops.harp_gated_forward(ctx, x, w, h, z=z, workspace=ws)
+    ops.harp_gated_forward(ctx, x.contiguous(), w, near[0], z=near[1], workspace=ws)
+    ops.harp_gated_grad(ctx, dy, w2, z, dz, workspace=ws)
+    ops.harp_gated_grad(ctx, dy, w2, near[1], near[2], workspace=ws)
+    assert torch.equal(h, near[0]) and torch.equal(z, near[1]) and torch.equal(dz, near[2])
+    ctx.close()
+
+
 def test_refusals(monkeypatch):
     import torch
     from paper_2509_24859_amd import operators as ops

@@ -146,6 +146,29 @@ def test_other_streams_and_graphs(harp):
     ctx.close()
 
 
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(harp):
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx = harp.Context(0)
+    f, _ = ops.rotary_frequencies(ctx, 64)
+    buf = torch.empty(2200, 1 << 20, dtype=torch.bfloat16, device="cuda")
+    x, y = (buf[:, at:at + 128].unflatten(1, (2, 64)) for at in (0, 1000))
+    x.copy_(torch.randn(2200, 2, 64, device="cuda"))
+    near = torch.empty(2200, 2, 64, dtype=torch.bfloat16, device="cuda")
+    ops.harp_rotary(ctx, x, y, f)
+    ops.harp_rotary(ctx, x.contiguous(), near, f)
+    assert torch.equal(y, near)
+    # heads 2^29 elements apart, tokens next to each other
+    wide = buf.view(-1).as_strided((5, 4, 64), (64, 1 << 29, 1))
+    wide.copy_(torch.randn(5, 4, 64, device="cuda"))
+    near = torch.empty(5, 4, 64, dtype=torch.bfloat16, device="cuda")
+    ops.harp_rotary(ctx, wide.contiguous(), near, f)
+    ops.harp_rotary(ctx, wide, wide, f)
+    assert torch.equal(wide, near)
+    ctx.close()
+
+
 def test_refusals(monkeypatch):
     import torch
     from paper_2509_24859_amd import operators as ops
