@@ -952,12 +952,18 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         }
 }
 
-// Sums of shares, in their order, for the rows of sequences: `rows` of them per token of begin's spans, element (token, row) of
-// sums[share * stride + ...], to `to`.
+// Sums of shares, in their order, for the rows of sequences: `rows` of them per token of begin's spans, share i's of element (token, row)
+// at first + i * stride + .., to p.  Two results that lie alike in one launch.
+template <typename T> struct Joined {
+    T *p;
+    int64_t token, step, first;
+};
 template <typename T>
 __global__ __launch_bounds__(kJoinRows * 32) void join_sums(const int32_t *begin, int64_t tokens, int batch, int rows, int head, const float *sums, int count,
-                                                            int64_t stride, T *to, int64_t to_token, int64_t to_step) {
+                                                            int64_t stride, Joined<T> one, Joined<T> two) {
+    const Joined<T> to = blockIdx.y ? two : one;
     int b, tile;
+    if (!to.p) return;
     if (!locate(begin, tokens, batch, rows, kJoinRows, blockIdx.x, b, tile)) return;
     int64_t first;
     int n;
@@ -966,11 +972,11 @@ __global__ __launch_bounds__(kJoinRows * 32) void join_sums(const int32_t *begin
     const int col = threadIdx.x % 32 * 4;
     if (r >= int64_t(n) * rows || col >= head) return;
     const int64_t token = first + r / rows, row = r % rows;
-    const float *at = sums + (token * rows + row) * head + col;
+    const float *at = sums + to.first + (token * rows + row) * head + col;
     f32x4 x = {0, 0, 0, 0};
 #pragma unroll 4
     for (int i = 0; i < count; ++i) x += load4(at + i * stride);
-    store4(to + token * to_token + row * to_step + col, x);
+    store4(to.p + token * to.token + row * to.step + col, x);
 }
 
 // ---------------------------------------------------------------------------------------------- on the host
@@ -1175,7 +1181,7 @@ void run_backward(const harp_attention *g, const harp_attention_grads *d, const 
         else launch_queries<T, 128>(p, a, grads, shares, st);
         if (p.shares > 1)
             join_sums<T><<<dim3(uint32_t(tiles_of(g->tokens_q, g->heads, g->batch, kJoinRows))), dim3(kJoinRows * 32), 0, st>>>(
-                a.q_begin, a.tokens_q, a.batch, a.heads, a.head, sums, p.shares, rows * a.head, static_cast<T *>(d->dQ), d->dq_token, d->dq_step);
+                a.q_begin, a.tokens_q, a.batch, a.heads, a.head, sums, p.shares, rows * a.head, Joined<T>{static_cast<T *>(d->dQ), d->dq_token, d->dq_step, 0}, Joined<T>());
     }
     if ((d->dK || d->dV) && g->tokens_k) {
         const Plan &p = of_keys;
@@ -1185,9 +1191,9 @@ void run_backward(const harp_attention *g, const harp_attention_grads *d, const 
         else launch_keys<T, 128>(p, a, grads, shares, st);
         if (p.shares > 1) {
             const int64_t each = a.tokens_k * a.kv_heads * a.head;
-            const dim3 grid(uint32_t(tiles_of(g->tokens_k, g->kv_heads, g->batch, kJoinRows))), block(kJoinRows * 32);
-            if (d->dK) join_sums<T><<<grid, block, 0, st>>>(a.k_begin, a.tokens_k, a.batch, a.kv_heads, a.head, sums, p.shares, 2 * each, static_cast<T *>(d->dK), d->dk_token, d->dk_step);
-            if (d->dV) join_sums<T><<<grid, block, 0, st>>>(a.k_begin, a.tokens_k, a.batch, a.kv_heads, a.head, sums + each, p.shares, 2 * each, static_cast<T *>(d->dV), d->dv_token, d->dv_step);
+            join_sums<T><<<dim3(uint32_t(tiles_of(g->tokens_k, g->kv_heads, g->batch, kJoinRows)), 2), dim3(kJoinRows * 32), 0, st>>>(
+                a.k_begin, a.tokens_k, a.batch, a.kv_heads, a.head, sums, p.shares, 2 * each,
+                Joined<T>{static_cast<T *>(d->dK), d->dk_token, d->dk_step, 0}, Joined<T>{static_cast<T *>(d->dV), d->dv_token, d->dv_step, each});
         }
     }
 }
