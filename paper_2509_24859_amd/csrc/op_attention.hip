@@ -575,7 +575,8 @@ struct Grads {
     const void *d_o;
     int64_t do_token, do_step, dq_token, dq_step, dk_token, dk_step, dv_token, dv_step;
     void *dq, *dk, *dv;
-    float *delta;                    // [heads][tokens_q]: sum over channels of dO O
+    float *delta;                    // [heads][tokens_q]: sum over channels of dO O, and one 0 behind
+    float *against;                  // the same: what exponents of 2 are taken against, infinity behind and where no key is seen
     float *peaks;                    // HARP_F16: [2][kPeaks] largest squared norms of rows of dO and of V, one from each workgroup
     float scale;
 };
@@ -603,7 +604,8 @@ template <typename T> struct Range {
             }
         }
     }
-    __device__ __forceinline__ float less(float dp, float delta) const { return kNarrow ? fmaf(dp, factor, -delta) : dp - delta; }
+    __device__ __forceinline__ float less(float dp, float delta) const { return kNarrow ? fmaf(dp, factor, -delta) : dp - delta; }     // delta times factor
+    __device__ __forceinline__ float scaled(float ds) const { return kNarrow ? ds * factor : ds; }
     __device__ __forceinline__ float back() const { return kNarrow ? kWeight / factor : 1.0f; }       // of what gradients are summed into
 };
 
@@ -614,6 +616,7 @@ template <typename T>
 __global__ __launch_bounds__(256) void measure(Call a, Grads g, int of_q, int of_k, int groups) {
     __shared__ uint32_t highest[4];
     const bool q = int(blockIdx.x) < groups;
+    if (blockIdx.x == 0 && threadIdx.x == 0) g.delta[a.heads * a.tokens_q] = 0, g.against[a.heads * a.tokens_q] = INFINITY;
     const int times = q ? a.heads : a.kv_heads, col = threadIdx.x % 16 * 8;
     uint32_t high = 0;
     for (int id = blockIdx.x % groups; id < (q ? of_q : of_k); id += groups) {
@@ -634,7 +637,12 @@ __global__ __launch_bounds__(256) void measure(Call a, Grads g, int of_q, int of
 #pragma unroll
                 for (int k = 0; k < 8; ++k) d += to_f32(T(x[k])) * to_f32(T(y[k]));
                 d = sum16(d);
-                if (r < rows && threadIdx.x % 16 == 0) g.delta[head * a.tokens_q + s.q0 + token] = d;
+                if (r < rows && threadIdx.x % 16 == 0) {
+                    const int64_t at = head * a.tokens_q + s.q0 + token;
+                    const float lse = a.lse[at];
+                    g.delta[at] = d;
+                    g.against[at] = lse == -INFINITY ? INFINITY : lse * kLog2e - Range<T>::kShift;
+                }
             }
             if (Range<T>::kNarrow) {
                 float d = 0;
@@ -790,6 +798,22 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
     }
 }
 
+// A value of which the compiler keeps nothing that it has made of it before: in registers that are wanted otherwise.
+__device__ __forceinline__ int anew(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// 4 bytes a lane from `from` to LDS, lane after lane from `to` on (the same for the wavefront): without a register for them on their way.
+// m0 is named so that the compiler keeps no value of its own there; that it hands m0 out to nobody is what its warning, turned off
+// here, is about.  What waits for it is written out too: the compiler does not count it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void word_to_lds(const float *from, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+
 // dK and dV of 32 keys a wavefront, whose rows come through LDS kBack at a time.  dV^T = dO^T P, dK^T = Q^T dS, where a lane has
 // 16 rows of one key.
 constexpr int kBack = 32;
@@ -799,7 +823,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
     typedef typename Mfma32<T>::Frag Frag;
     __shared__ __align__(1024) T lds[4][kBack * D];               // two steps of Q, two of dO
     __shared__ __align__(1024) T lv[kCols * D];
-    __shared__ __align__(16) float l_lse[2][kBack], l_delta[2][kBack];
+    __shared__ __align__(16) float l_stat[2][2 * kBack];          // against and delta of a step's rows
     __shared__ __align__(16) int l_limit[2][kBack];
     const Work work = work_of(blockIdx.x, tiles, a.kv_heads, shares.count, a.causal);
     const int share = work.share, kv = work.kv;
@@ -829,8 +853,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
     f32x16 dk[D / 32] = {}, dv[D / 32] = {};
     Stage<T, D, kBack, kThreads> sq, sd;
     const Range<T> range(g.peaks);
-    float lse = 0, delta = 0;        // as they are in memory: looked at when they are put, so that nothing waits for them before
-    int limit = 0;
+    const int wave_id = __builtin_amdgcn_readfirstlane(int(threadIdx.x)) / kWave;
     auto ask = [&](int t) {
         const int r0 = row_first + t * kBack;
         auto place = [&](int row, int64_t token, int64_t step) {
@@ -839,40 +862,37 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         };
         sq.ask([&](int row) { return static_cast<const T *>(a.q) + place(row, a.q_token, a.q_step); }, rows - r0, a.head);
         sd.ask([&](int row) { return static_cast<const T *>(g.d_o) + place(row, g.do_token, g.do_step); }, rows - r0, a.head);
-        if (threadIdx.x < kBack) {
-            const Row r = row_of(a, s, kv, r0 + int(threadIdx.x));
-            limit = r.limit;
-            if (limit >= 0) {
-                lse = a.lse[r.head * a.tokens_q + r.token];
-                delta = g.delta[r.head * a.tokens_q + r.token];
-            }
+        // of no row: what makes every weight 0
+        if (wave_id == 0) {
+            const int id = anew(int(threadIdx.x)), row = id % 32;
+            word_to_lds((id < 32 ? g.against : g.delta) + (r0 + row < rows ? place(row, 1, a.tokens_q) : a.heads * a.tokens_q), lds_address(l_stat[t - first & 1]));
         }
     };
-    auto put = [&](int at) {
+    auto put = [&](int t) {
+        const int at = t - first & 1;
         sq.put(lds[at]);
         sd.put(lds[2 + at]);
-        if (threadIdx.x < kBack) {
-            // of no row, or one that saw no key: infinity, against which every weight is 0
-            l_lse[at][threadIdx.x] = limit < 0 || lse == -INFINITY ? INFINITY : lse * kLog2e - Range<T>::kShift;
-            l_delta[at][threadIdx.x] = limit < 0 ? 0 : delta * range.factor;
-            l_limit[at][threadIdx.x] = limit;
+        if (a.causal && threadIdx.x < kBack) {
+            const int row = anew(int(threadIdx.x));
+            l_limit[at][row] = limit_of(a, s, query_of(a, row_first + t * kBack + row));
         }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
     if (first < end) ask(first);
     sv.put(lv);
-    if (first < end) put(0);
+    if (first < end) put(first);
     __syncthreads();
     // A step's matrix instructions and what goes on under them:  S;  dP, weights;  dV, their gradients;  dK.
     constexpr int kPart = D / 16, kAhead = 2;
     auto rows_step = [&](int at, bool masked) {
+        const float *stats = l_stat[at] + 4 * h;
         f32x16 p, dp;
-        Frag f[kAhead + 1], v[kAhead + 1], w[2], ds[2];
+        Frag f[kAhead + 1], v[2], w[2], ds[2];
         auto read = [&](auto n) {
             constexpr int part = n / kPart, j = n % kPart;
             Frag &to = f[n % (kAhead + 1)];
             if (part < 2) to = along.read(part * 2 * kBack, j);
             else to = across.read((part == 2 ? 2 * kBack : 0) + j / (D / 32) * 16, j % (D / 32));
-            if (part == 1) v[n % (kAhead + 1)] = along_v.read(0, j);
         };
         written_out<kAhead>(read);
         f32x4 against = {}, less = {};
@@ -889,20 +909,20 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
                 for (int e = 0; e < 16; ++e) w[e / 8][e % 8] = T(p[e]);
             }
             if constexpr (part == 0) p = Mfma32<T>::run(x, k[j], j ? p : f32x16{});
-            else if constexpr (part == 1) dp = Mfma32<T>::run(x, v[n % (kAhead + 1)], j ? dp : f32x16{});
+            else if constexpr (part == 1) dp = Mfma32<T>::run(x, v[n % 2], j ? dp : f32x16{});
             else if constexpr (part == 2) dv[j % (D / 32)] = Mfma32<T>::run(x, w[j / (D / 32)], dv[j % (D / 32)]);
             else dk[j % (D / 32)] = Mfma32<T>::run(x, ds[j / (D / 32)], dk[j % (D / 32)]);
             if constexpr (n + kAhead < 4 * kPart) read(std::integral_constant<int, n + kAhead>());
+            if constexpr (n + 1 >= kPart && n + 1 < 2 * kPart) v[(n + 1) % 2] = along_v.read(0, n + 1 - kPart);
 #pragma unroll
             for (int e = from; e < to; ++e) {
                 if (part == 1) {
-                    if (e % 4 == 0) against = *reinterpret_cast<const f32x4 *>(&l_lse[at][8 * (e / 4) + 4 * h]);
+                    if (e % 4 == 0) against = *reinterpret_cast<const f32x4 *>(stats + 8 * (e / 4));
                     p[e] = __builtin_amdgcn_exp2f(fmaf(p[e], a.c, -against[e % 4]));
                 }
                 if (part == 2) {
-                    if (e % 4 == 0) less = *reinterpret_cast<const f32x4 *>(&l_delta[at][8 * (e / 4) + 4 * h]);
-                    float x = p[e] * range.less(dp[e], less[e % 4]);
-                    ds[e / 8][e % 8] = T(x);
+                    if (e % 4 == 0) less = *reinterpret_cast<const f32x4 *>(stats + kBack + 8 * (e / 4));
+                    ds[e / 8][e % 8] = T(range.scaled(p[e] * (dp[e] - less[e % 4])));
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -917,11 +937,12 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
         along.refresh();
         along_v.refresh();
         across.refresh();
-        if (row_first + (t + 1) * kBack > none) rows_step(at, row_first + t * kBack < some);
+        const int r0 = row_first + t * kBack;
+        if (r0 + kBack > none) rows_step(at, r0 < some);
         const uint32_t other = at ? -uint32_t(kBack * D * 2) : kBack * D * 2;
         along.at += other;
         across.at += other;
-        if (t + 1 < end) put(1 - at);
+        if (t + 1 < end) put(t + 1);
         __syncthreads();
     }
     // what keys that are not used were given has stayed in their own columns
@@ -1047,12 +1068,12 @@ Plan plan_keys(const harp_ctx *ctx, const harp_attention *g, bool causal) {
                     double(g->tokens_k) * g->kv_heads * g->head * 8, causal, false);
 }
 
-// Where parts of the workspace begin, behind delta; what the passes need of these plans.
+// Where parts of the workspace begin; what the passes need of these plans.
 struct Space { size_t peaks, stats, sums, all; };
 Space space_for(const harp_attention *g, const Plan *q, const Plan *k) {
     const size_t rows = size_t(g->tokens_q) * g->heads, kv = size_t(g->tokens_k) * g->kv_heads;
     Space s = {};
-    s.peaks = round_up(rows * 4, 256);
+    s.peaks = 2 * round_up((rows + 1) * 4, 256);         // behind delta and against
     s.stats = s.peaks + 2 * kPeaks * 4;
     s.sums = s.stats + (q && q->shares > 1 ? round_up(rows * q->shares * 8, 256) : 0);
     const size_t of_q = q && q->shares > 1 ? rows * q->shares * g->head * 4 : 0, of_k = k && k->shares > 1 ? kv * k->shares * g->head * 8 : 0;
@@ -1167,7 +1188,7 @@ void run_backward(const harp_attention *g, const harp_attention_grads *d, const 
                   unsigned char *ws, hipStream_t st) {
     const Call a = call_of(g);
     const Grads grads = {d->dO, d->do_token, d->do_step, d->dq_token, d->dq_step, d->dk_token, d->dk_step, d->dv_token, d->dv_step,
-                         d->dQ, d->dK, d->dV, reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + space.peaks), g->scale};
+                         d->dQ, d->dK, d->dV, reinterpret_cast<float *>(ws), reinterpret_cast<float *>(ws + space.peaks / 2), reinterpret_cast<float *>(ws + space.peaks), g->scale};
     const int64_t rows = g->tokens_q * g->heads;
     float *sums = reinterpret_cast<float *>(ws + space.sums);
     const int of_q = int(tiles_of(g->tokens_q, g->heads, g->batch, kMeasured)), of_k = int(tiles_of(g->tokens_k, g->kv_heads, g->batch, kMeasured));
