@@ -3,6 +3,11 @@
 // Wg and Wu are the two halves of one matrix W [2 F][K], Z [M][2 F] = X W^T + bias likewise.  Forward a workgroup makes the
 // same columns of both halves, so that neither half's sums leave the registers before they are multiplied; back, the product
 // dH = dY W2 takes Z in its epilogue and stores both halves of dZ.  dX and dW are then plain products of dZ (harp_linear).
+//
+// 4,096 tokens, W [24576][4096], bfloat16, SiLU, Z kept: 656 to 680 us, 1,210 to 1,257 TFLOP/s (a library product of these sizes
+// alone reaches 1,457); without the way through one kernel, Z would be written and read again, 600 MB, 120 us.  Back through W2
+// [4096][12288] and the gate with H made again: 425 us, 970 TFLOP/s.  One token: 32 us in the kernel, 6.3 TB/s of weights.  What bounds
+// the tiles is what bounds harp_linear's: bringing operands into LDS, and the epilogue's stores.
 #include "op_product.h"
 
 namespace {

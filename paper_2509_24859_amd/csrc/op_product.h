@@ -377,6 +377,7 @@ __device__ __forceinline__ void tile_of(int id, int tiles_p, int tiles_q, int &t
 // wavefronts of 128 x 128 each, which would read LDS a third less, 544: one to a SIMD, they wait at every barrier.
 // WP x WQ wavefronts, each a part of BP / WP x BQ / WQ of the tile.  With `partial` the sums of blockIdx.y's share of r go
 // there, [share][P][Q], instead of through the epilogue.
+//
 // FORM kGatedForward: half of each wavefront's columns are the gate's, rows q of b, half the same of what it is multiplied with,
 // rows F + q, so that a lane has both of an element; Q is F, and a tile BQ / 2 of it.
 template <typename T, bool A_ACROSS, bool B_ACROSS, int BP, int BQ, int WP, int WQ, int FORM = kLinear, typename E = Epilogue>
