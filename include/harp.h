@@ -711,7 +711,7 @@ int harp_gated_forward(harp_ctx *ctx, const harp_gated *args, void *workspace, s
  *   dH = dY W,   dZ's first F columns = dH * Z's last F * act'(Z's first F),   its last F = dH * act(Z's first F)
  * and H again, for that product's weight gradient, so that it need not be kept (H NULL: not wanted).  W NULL: dY [M][F] is dH (N
  * unused).  Then harp_linear_grad_input and harp_linear_grad_weight of dZ with the block's W [2 F][K] and X give the rest.
- * dY [M][N], Z and dZ [M][2 F], H [M][F] of `type`; dZ may be Z. */
+ * dY [M][N], Z and dZ [M][2 F], H [M][F] of `type`; dZ may be Z (then lddz is ldz). */
 typedef struct {
     int64_t M, F, N;
     int32_t type, act;

@@ -163,6 +163,7 @@ int harp_gated_grad(harp_ctx *ctx, const harp_gated_grads *g, void *workspace, s
     if (!g) return fail(ctx, HARP_ERR_INVALID_ARG, "null args");
     const bool some = g->M > 0;
     const int64_t N = g->W ? g->N : g->F;
+    if (g->M > 1 && g->dZ && g->dZ == g->Z && g->lddz != g->ldz) return fail(ctx, HARP_ERR_SHAPE, "dZ is Z with another distance of rows");
     const Matrix m[] = {{"dY", g->dY, g->lddy, N, 2, some}, {"W", g->W, g->ldw, g->F, 2, false}, {"Z", g->Z, g->ldz, 2 * g->F, 2, some},
                         {"dZ", g->dZ, g->lddz, 2 * g->F, 2, some}, {"H", g->H, g->ldh, g->F, 2, false}};
     const int rc = gated_check(ctx, g->M, g->F, N, g->type, g->act, m, 5, g->W != nullptr, workspace, workspace_bytes);

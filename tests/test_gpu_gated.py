@@ -230,3 +230,11 @@ def test_refusals(monkeypatch):
         refused(monkeypatch, ops.harp_gated_grad, ctx, *a, **k)
     for sizes in ((-1, 6, 8), (1 << 31, 6, 8), (4, 0, 8), (4, 6, 0), (4, 1 << 21, 8), (4, 6, 1 << 21)):
         refused(monkeypatch, ops.gated_workspace, ctx, *sizes)
+
+
+def test_gradient_over_z_at_other_distances_is_refused(monkeypatch):
+    import torch
+    from paper_2509_24859_amd import binding, operators as ops
+    ctx, memory = HostContext(), torch.zeros(4, 16, dtype=torch.bfloat16)
+    z, dz, dh = memory[:, :12], memory.view(-1)[:48].view(4, 12), torch.zeros(4, 6, dtype=torch.bfloat16)
+    assert refused(monkeypatch, ops.harp_gated_grad, ctx, dh, None, z, dz) == binding.ERR_SHAPE
