@@ -645,8 +645,9 @@ int harp_rotary_frequencies(int32_t turned, double base, int32_t scaling, double
  * that sees no key (or whose scores are all -infinity) has o = 0, lse = -infinity, and no part in any gradient.  Keys that are not
  * used are not read into any result, whatever they hold.  A key or value that is not finite and hidden from a query by the causal
  * order alone may make that query's results NaN.
+ * What a pass writes lies over nothing else that it reads or writes.
  * Q and O [tokens_q][heads][head], K and V [tokens_k][kv_heads][head], of `type` (HARP_BF16 or HARP_F16), element (t, h, c) at
- * t * token + h * step + c.  lse: float [heads][tokens_q], or NULL in the forward pass.  scale > 0.
+ * t * token + h * step + c.  lse: float [heads][tokens_q], or NULL in the forward pass.  0 < scale < 2^127.
  * Begins and counts are DEVICE int32, read when the kernels run, so that a captured call takes those of each replay; begins rise
  * and end within tokens; whatever they hold, nothing outside the tensors is touched.  Rows of no sequence are left as they were.
  * Scores, weights' sums and all sums over keys or queries are in 32 bits; weights and their gradients are rounded to `type`

@@ -1117,7 +1117,7 @@ int check(harp_ctx *ctx, const harp_attention *g, const Tensor *t, int count, co
     const int rc = attention_sizes(ctx, g);
     if (rc != HARP_OK) return rc;
     if (g->type != HARP_BF16 && g->type != HARP_F16) return fail(ctx, HARP_ERR_INVALID_ARG, "type must be HARP_BF16 or HARP_F16");
-    if (!(g->scale > 0) || !isfinite(g->scale)) return fail(ctx, HARP_ERR_INVALID_ARG, "scale must be positive");
+    if (!(g->scale > 0) || !isfinite(g->scale * kLog2e)) return fail(ctx, HARP_ERR_INVALID_ARG, "scale must be positive and below 2^127");
     if ((!g->q_begin && g->tokens_q % g->batch) || (!g->k_begin && g->tokens_k % g->batch))
         return fail(ctx, HARP_ERR_SHAPE, "tokens are no multiple of the batch, and begins are missing");
     if (!aligned(g->q_begin, 4) || !aligned(g->k_begin, 4) || !aligned(g->k_count, 4) || !aligned(g->lse, 4))
@@ -1131,6 +1131,9 @@ int check(harp_ctx *ctx, const harp_attention *g, const Tensor *t, int count, co
             return fail(ctx, HARP_ERR_SHAPE, "%s: distances must be in 0 .. 2^40", t[i].name);
         if (t[i].written && !clear_of_each_other(t[i].tokens, t[i].heads, g->head, t[i].token, t[i].step))
             return fail(ctx, HARP_ERR_SHAPE, "%s: elements lie over each other", t[i].name);
+        for (int j = 0; t[i].written && j < count; ++j)
+            if (j != i && t[j].p == t[i].p && t[i].tokens > 0 && t[j].tokens > 0)
+                return fail(ctx, HARP_ERR_INVALID_ARG, "%s is %s", t[i].name, t[j].name);
     }
     *q = plan_queries(ctx, g, g->causal);
     if (k) *k = plan_keys(ctx, g, g->causal);

@@ -502,3 +502,18 @@ def test_refusals(monkeypatch):
     for sizes in ((-1, 9, 1, 4, 2, 16), (1 << 30, 9, 1, 4, 2, 16), (6, 9, 0, 4, 2, 16), (6, 9, 1, 4, 3, 16), (6, 9, 1, 4, 2, 12), (6, 9, 1, 4, 2, 136),
                   (6, 9, 1, 0, 1, 16), (1 << 29, 9, 1, 4, 2, 16)):
         refused(monkeypatch, ops.attention_workspace, ctx, *sizes)
+
+
+def test_results_over_operands_are_refused(monkeypatch):
+    import torch
+    from paper_2509_24859_amd import binding, operators as ops
+    ctx, b = HostContext(), torch.bfloat16
+    new = lambda n, h: torch.zeros(n, h, 16, dtype=b)  # noqa: E731
+    q, k, v, o, do, dq, dk, dv, lse = new(6, 4), new(9, 2), new(9, 2), new(6, 4), new(6, 4), new(6, 4), new(9, 2), new(9, 2), torch.zeros(4, 6)
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    ws = ws[-ws.data_ptr() % 256:]
+    assert refused(monkeypatch, ops.harp_attention_forward, ctx, q, k, v, q, workspace=ws) == binding.ERR_INVALID_ARG
+    for out in ((q, dk, dv), (do, dk, dv), (o, dk, dv), (dq, k, dv), (dq, dk, v), (dq, dk, dk)):
+        assert refused(monkeypatch, ops.harp_attention_backward, ctx, q, k, v, o, lse, do, *out, workspace=ws) == binding.ERR_INVALID_ARG
+    # times log2(e) it is beyond 32 bits
+    assert refused(monkeypatch, ops.harp_attention_forward, ctx, q, k, v, o, scale=3e38, workspace=ws) == binding.ERR_INVALID_ARG
