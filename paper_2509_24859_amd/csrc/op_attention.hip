@@ -83,12 +83,13 @@ __device__ __forceinline__ Sequence sequence(const Call &a, int b) {
     return s;
 }
 
-// Sum over the lanes up to and with this one.
+// Sum over the lanes up to and with this one.  Sums of tiles stop at 2^31 - 1: spans that lie over each other (begins that do not
+// rise) may have more, and a sum that turned negative would find a sequence that is none.
 __device__ __forceinline__ int up_to(int x) {
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) {
         const int below = __shfl_up(x, d);
-        if (int(threadIdx.x % kWave) >= d) x += below;
+        if (int(threadIdx.x % kWave) >= d) x = __builtin_elementwise_add_sat(x, below);
     }
     return x;
 }
@@ -110,9 +111,10 @@ __device__ __forceinline__ bool locate(const int32_t *begin, int64_t tokens, int
         span(begin, tokens, batch, i, at, count);
         return int((int64_t(count) * times + side - 1) / side);
     };
+    auto before = [](int upto, int lane) { return lane > 0 ? __builtin_amdgcn_readlane(upto, lane - 1) : 0; };
     for (int first = 0; first < batch; first += kWave * run) {
         int tiles = 0;
-        for (int i = 0; i < run; ++i) tiles += tiles_of_one(first + lane * run + i);
+        for (int i = 0; i < run; ++i) tiles = __builtin_elementwise_add_sat(tiles, tiles_of_one(first + lane * run + i));
         int upto = up_to(tiles);
         uint64_t past = __ballot(id < upto);
         if (!past) {
@@ -120,14 +122,14 @@ __device__ __forceinline__ bool locate(const int32_t *begin, int64_t tokens, int
             continue;
         }
         int at = __builtin_ctzll(past);
-        id -= __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at);
+        id -= before(upto, at);
         b = first + at * run;
         if (run > 1) {
             tiles = lane < run ? tiles_of_one(b + lane) : 0;
             upto = up_to(tiles);
             past = __ballot(id < upto);
             at = __builtin_ctzll(past);
-            id -= __builtin_amdgcn_readlane(upto, at) - __builtin_amdgcn_readlane(tiles, at);
+            id -= before(upto, at);
             b += at;
         }
         tile = id;

@@ -517,3 +517,27 @@ def test_results_over_operands_are_refused(monkeypatch):
         assert refused(monkeypatch, ops.harp_attention_backward, ctx, q, k, v, o, lse, do, *out, workspace=ws) == binding.ERR_INVALID_ARG
     # times log2(e) it is beyond 32 bits
     assert refused(monkeypatch, ops.harp_attention_forward, ctx, q, k, v, o, scale=3e38, workspace=ws) == binding.ERR_INVALID_ARG
+
+
+@pytest.mark.gpu
+def test_begins_that_do_not_rise_stay_within_the_tensors(harp):
+    """1,024 sequences of which every other one claims all 2^29 rows, 2^22 tiles of 128 each: together more than 31 bits hold.  No keys are
+    anybody's, so queries' gradients are not asked for and keys' stay as they were."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx, b, tokens, heads, n = harp.Context(0), torch.bfloat16, 1 << 25, 16, 1024
+    one = torch.ones(1, 1, 8, dtype=b, device="cuda")
+    q = one.expand(tokens, heads, 8)
+    k = torch.ones(n, 2, 8, dtype=b, device="cuda")
+    lse = torch.zeros(heads, tokens, device="cuda")
+    dk, dv = torch.full_like(k, -7), torch.full_like(k, -7)
+    q_begin = torch.tensor([0, tokens] * (n // 2) + [0], dtype=torch.int32, device="cuda")
+    need = ops.attention_workspace(ctx, tokens, n, n, heads, 2, 8).numel()
+    lent = torch.full((need + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    ops.harp_attention_backward(ctx, q, k, k, q, lse, q, None, dk, dv, q_begin=q_begin, k_begin=torch.zeros(n + 1, dtype=torch.int32, device="cuda"),
+                                workspace=lent[:need])
+    torch.cuda.synchronize()
+    assert (dk == -7).all() and (dv == -7).all() and (lent[need:] == 0x5A).all()
+    # lse 0 and dO = O of ones: 8 a row, whatever came of the other sequences
+    delta = lent[:tokens * heads * 4].view(torch.float32)
+    assert (delta == 8).all()
