@@ -590,7 +590,7 @@ struct Grads {
     void *dq, *dk, *dv;
     float *delta;                    // [heads][tokens_q]: sum over channels of dO O, and one 0 behind
     float *against;                  // the same: what exponents of 2 are taken against, infinity behind and where no key is seen
-    float *peaks;                    // HARP_F16: [2][kPeaks] largest squared norms of rows of dO and of V, one from each workgroup
+    float *peaks;                    // HARP_F16: [2][kPeaks] largest finite squared norms of rows of dO and of V, one from each workgroup
     float scale;
 };
 
@@ -604,14 +604,14 @@ template <typename T> struct Range {
     float factor = 1;                // of dP - D where a weight carries 2^kShift
     __device__ __forceinline__ explicit Range(const float *peaks) {
         if constexpr (kNarrow) {
-            uint32_t high[2] = {0, 0};                           // of floats that are not negative, or NaN: as their bits
+            uint32_t high[2] = {0, 0};                           // of floats that are not negative: as their bits
 #pragma unroll
             for (int i = 0; i < kPeaks; i += kWave)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) high[j] = larger(high[j], __float_as_uint(peaks[j * kPeaks + i + threadIdx.x % kWave]));
             const float bound = 4 * __uint_as_float(wave_max(high[0])) * __uint_as_float(wave_max(high[1]));
             int e = 0;
-            if (bound > 0 && bound < INFINITY) {
+            if (bound > 0) {
                 (void)frexpf(bound, &e);
                 factor = ldexpf(1.0f, 14 - ((e + 1) >> 1) - int(kShift));
             }
@@ -644,15 +644,18 @@ __global__ __launch_bounds__(256) void measure(Call a, Grads g, int of_q, int of
             const T *from = q ? static_cast<const T *>(g.d_o) + (s.q0 + token) * g.do_token + head * g.do_step
                               : static_cast<const T *>(a.v) + (s.k0 + token) * a.v_token + head * a.v_step;
             const auto x = eight<T>(from + col, there);
+            bool counts = true;
             if (q) {
                 const auto y = eight<T>(static_cast<const T *>(a.o) + (s.q0 + token) * a.o_token + head * a.o_step + col, there);
                 float d = 0;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) d += to_f32(T(x[k])) * to_f32(T(y[k]));
                 d = sum16(d);
+                const int64_t at = head * a.tokens_q + s.q0 + token;
+                float lse = 0;
+                if (r < rows && (Range<T>::kNarrow || threadIdx.x % 16 == 0)) lse = a.lse[at];
+                counts = lse != -INFINITY;
                 if (r < rows && threadIdx.x % 16 == 0) {
-                    const int64_t at = head * a.tokens_q + s.q0 + token;
-                    const float lse = a.lse[at];
                     g.delta[at] = d;
                     g.against[at] = lse == -INFINITY ? INFINITY : lse * kLog2e - Range<T>::kShift;
                 }
@@ -661,7 +664,9 @@ __global__ __launch_bounds__(256) void measure(Call a, Grads g, int of_q, int of
                 float d = 0;
 #pragma unroll
                 for (int k = 0; k < 8; ++k) d += to_f32(T(x[k])) * to_f32(T(x[k]));
-                high = larger(high, __float_as_uint(sum16(d)) & 0x7fffffff);
+                // not of rows that see nothing, nor of those that are not finite, whose results scaling does not save
+                const uint32_t norm = __float_as_uint(sum16(d));
+                if (counts && norm < 0x7f800000) high = larger(high, norm);
             }
         }
     }
@@ -789,6 +794,10 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
 #pragma unroll 1
         for (; t < end; ++t) turn(t, t - first & 1, std::true_type());
         if (!here) return;
+        if (limit == 0) {                                            // nothing seen: zeros whatever the keys
+#pragma unroll
+            for (int m = 0; m < D / 32; ++m) dq[m] = f32x16{};
+        }
         const float scale = g.scale * range.back();
         float *sums = shares.sums + ((int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head) * a.head;
         T *to = static_cast<T *>(g.dq) + mine.token * g.dq_token + mine.head * g.dq_step;

@@ -541,3 +541,61 @@ def test_begins_that_do_not_rise_stay_within_the_tensors(harp):
     # lse 0 and dO = O of ones: 8 a row, whatever came of the other sequences
     delta = lent[:tokens * heads * 4].view(torch.float32)
     assert (delta == 8).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("head", [64, 96, 128])
+@pytest.mark.parametrize("kind", ["bfloat16", "float16"])
+def test_queries_without_keys_have_no_part_in_gradients(harp, kind, head):
+    """70 and 600 queries, causal, of 40 and 300 keys: whatever the first 30 and 300 and their gradients hold, the others' results and the
+    keys' are the same bits.  Gradients of a few hundred, so that float16 has to scale them.  A key that only the last query sees, and
+    is not finite, leaves the queries without keys their zeros."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx, t = harp.Context(0), getattr(torch, kind)
+    rng = np.random.default_rng(head)
+    draw = lambda n, h: torch.from_numpy(rng.standard_normal((n, h, head))).to(t).cuda()  # noqa: E731
+    q, do, k, v = draw(670, 4), draw(670, 4) * 256, draw(340, 2), draw(340, 2)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    form = dict(q_begin=i32(0, 70, 670), k_begin=i32(0, 40, 340), causal=True, workspace=ops.attention_workspace(ctx, 670, 340, 2, 4, 2, head))
+    empty = torch.zeros(670, dtype=torch.bool, device="cuda")
+    empty[:30] = empty[70:370] = True
+    results = []
+    for fill in (0.0, math.nan, math.inf, 6e4):
+        q[empty], do[empty] = fill, fill
+        o, lse, grads = torch.empty_like(q), torch.empty(4, 670, device="cuda"), [torch.empty_like(x) for x in (q, k, v)]
+        ops.harp_attention_forward(ctx, q, k, v, o, lse=lse, **form)
+        ops.harp_attention_backward(ctx, q, k, v, o, lse, do, *grads, **form)
+        assert (o[empty] == 0).all() and (lse[:, empty] == -math.inf).all() and (grads[0][empty] == 0).all(), fill
+        assert all(torch.isfinite(x).all() for x in grads), fill
+        results.append([o, lse] + grads)
+        assert all(torch.equal(x, y) for x, y in zip(results[0], results[-1])), fill
+    k[39], v[339] = math.nan, math.inf
+    o, lse, dq = torch.empty_like(q), torch.empty(4, 670, device="cuda"), torch.empty_like(q)
+    ops.harp_attention_forward(ctx, q, k, v, o, lse=lse, **form)
+    ops.harp_attention_backward(ctx, q, k, v, o, lse, do, dq, None, None, **form)
+    assert (o[empty] == 0).all() and (lse[:, empty] == -math.inf).all() and (dq[empty] == 0).all()
+    ctx.close()
+
+
+@pytest.mark.gpu
+def test_what_is_not_finite_in_one_sequence_leaves_the_others_as_they_are(harp):
+    """float16, gradients of a few hundred: a gradient or value of one sequence that is not finite changes no bit of the other's."""
+    import torch
+    from paper_2509_24859_amd import operators as ops
+    ctx, t = harp.Context(0), torch.float16
+    q, do, k, v = (torch.randn(200, 2, 64, device="cuda").to(t) for _ in range(4))
+    do *= 256
+    form = dict(batch=2, workspace=ops.attention_workspace(ctx, 200, 200, 2, 2, 2, 64))
+    results = []
+    for bad in (0.0, math.nan, math.inf):
+        do[3, 1, 5], v[40, 0, 7] = bad, 0.0
+        for of_v in (0.0, bad):
+            v[40, 0, 7] = of_v
+            o, lse, grads = torch.empty_like(q), torch.empty(2, 200, device="cuda"), [torch.empty_like(x) for x in (q, k, v)]
+            ops.harp_attention_forward(ctx, q, k, v, o, lse=lse, **form)
+            ops.harp_attention_backward(ctx, q, k, v, o, lse, do, *grads, **form)
+            results.append([x[100:] for x in [o] + grads])
+            assert all(torch.isfinite(x).all() for x in results[-1]), bad
+            assert all(torch.equal(x, y) for x, y in zip(results[0], results[-1])), bad
+    ctx.close()
