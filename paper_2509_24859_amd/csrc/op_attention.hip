@@ -384,16 +384,17 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
             sum *= shrink;
             return true;
         };
+        // A step's weights are summed apart before they meet the sum of all: one rounding of that for 16 of them, or those that are less
+        // than 2^-24 of it would be lost one by one, however many (2^16 of them beside a first key of weight 1: 6e-4 of the sum).
         auto weights = [&](f32x16 &p, Frag (&x)[2]) {
-            float part = 0;
+            float part[2] = {0, 0};
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
                 p[j] = __builtin_amdgcn_exp2f(fmaf(p[j], a.c, -against));
-                if (j % 2) part += p[j];
-                else sum += p[j];
+                part[j % 2] += p[j];
                 x[j / 8][j % 8] = T(p[j]);
             }
-            sum += part;
+            sum += part[0] + part[1];
         };
         auto shrink_o = [&] {
 #pragma unroll
@@ -417,10 +418,9 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
             fence();
             int grown = __builtin_amdgcn_readfirstlane(refer(now));
             asm volatile("" : "+s"(grown));                          // so that there is one copy of what follows, not one for either case
-            float part = 0;
+            float part[2] = {0, 0};
             auto summed = [&](int e) {                               // of exponentials
-                if (e % 2) part += now[e];
-                else sum += now[e];
+                part[e % 2] += now[e];
                 x[e / 8][e % 8] = T(now[e]);
             };
             fence();
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
             }
 #pragma unroll
             for (int e = 16 * (kPairs - 1) / kPairs; e < 16; ++e) summed(e);
-            sum += part;
+            sum += part[0] + part[1];
             w[0] = x[0], w[1] = x[1];
             asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(sum));    // here, not where they are used
             if (grown) shrink_o();
