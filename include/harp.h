@@ -651,8 +651,8 @@ int harp_rotary_frequencies(int32_t turned, double base, int32_t scaling, double
  * Begins and counts are DEVICE int32, read when the kernels run, so that a captured call takes those of each replay; begins rise
  * and end within tokens; whatever they hold, nothing outside the tensors is touched.  Rows of no sequence are left as they were.
  * Scores, weights' sums and all sums over keys or queries are in 32 bits; weights and their gradients are rounded to `type`
- * where they are multiplied with V, K, Q and dO (what the matrix instructions take; in HARP_F16 the gradients times a power
- * of two that keeps them from both ends of its range).
+ * where they are multiplied with V, K, Q and dO (what the matrix instructions take; in HARP_F16 weights times 2^12, so that
+ * those below 2^-37 of a row's largest are lost, and their gradients times a power of two that keeps them from both ends of its range).
  * head a multiple of 8, at most HARP_ATTENTION_MAX_HEAD; heads a multiple of kv_heads, heads <= 2^14;
  * 0 <= tokens < 2^30, tokens_q * heads / kv_heads < 2^30; 1 <= batch <= 2^20. */
 #define HARP_ATTENTION_MAX_HEAD 128

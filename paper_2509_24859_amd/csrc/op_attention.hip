@@ -287,7 +287,16 @@ __device__ __forceinline__ Row row_of(const Call &a, const Sequence &s, int kv, 
     return Row{s.q0 + query, kv * a.group + r - query * a.group, limit_of(a, s, query)};
 }
 
-// Partial results of a share of the keys: unscaled sums [share][token][head][channel], reference and sum [share][token][head].
+// Weights go into the matrix instructions rounded to T.  bfloat16 has the range of 32 bits.  float16 loses what is below 2^-25, so there
+// they are taken times 2^kShift: they are normal numbers from 2^-26 of the row's largest on and lost below 2^-37 of it, 2^-17 of a
+// result over 2^20 keys at most.  In the forward pass the reference may be 2^kBehind less than the largest: together they stay below 2^16.
+template <typename T> struct Weights {
+    static constexpr bool kNarrow = __is_same(T, _Float16);
+    static constexpr float kShift = kNarrow ? 12.0f : 0.0f, kBehind = kNarrow ? 3.0f : 8.0f;
+};
+
+// Partial results of a share of the keys: unscaled sums [share][token][head][channel], what exponents were taken against and the sum of
+// weights [share][token][head].
 struct Shares {
     int count, paired;
     float *sums, *stats;
@@ -364,7 +373,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
                 for (int m = 0; m < D / 32; ++m) o[m] = Mfma32<T>::run(across.read((2 + buffer) * kKeys + half * 32 + 16 * k, m), w[k], o[m]);
         };
         // Of step i's scores p: hides what a row does not see; the reference that exponents are taken against follows the maximum only
-        // when that has grown by 2^8 over it (sums in 32 bits and weights of 16 have room for the factor), and o has then to
+        // when that has grown by 2^kBehind over it (sums in 32 bits and weights of 16 have room for the factor), and o has then to
         // be shrunk once the weights of the step before are in it.
         auto hide = [&](int i, f32x16 &p) {
 #pragma unroll
@@ -376,11 +385,11 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
 #pragma unroll
             for (int j = 1; j < 16; ++j) high = fmaxf(high, p[j]);
             high *= a.c;
-            if (!__any(high > top + 8.0f)) return false;
+            if (!__any(high > top + Weights<T>::kBehind)) return false;
             high = fmaxf(fmaxf(high, other_half(high)), top);
             shrink = top == high ? 1.0f : __builtin_amdgcn_exp2f(top - high);
             top = high;
-            against = top == -INFINITY ? 0.0f : top;
+            against = top == -INFINITY ? 0.0f : top - Weights<T>::kShift;
             sum *= shrink;
             return true;
         };
@@ -505,7 +514,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
         if (shares.count > 1) {
             const int64_t at = (int64_t(share) * a.tokens_q + mine.token) * a.heads + mine.head;
             if (h == 0) {
-                shares.stats[2 * at] = top;
+                shares.stats[2 * at] = against;
                 shares.stats[2 * at + 1] = sum;
             }
 #pragma unroll
@@ -518,7 +527,7 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
             return;
         }
         const float scale = sum == 0 ? 0.0f : 1.0f / sum;    // no key: zeros; scores that are NaN: NaN
-        if (a.lse && h == 0) a.lse[mine.head * a.tokens_q + mine.token] = sum == 0 ? -INFINITY : (top + __log2f(sum)) * kLn2;
+        if (a.lse && h == 0) a.lse[mine.head * a.tokens_q + mine.token] = sum == 0 ? -INFINITY : (against + __log2f(sum)) * kLn2;
         T *to = static_cast<T *>(a.o) + mine.token * a.o_token + mine.head * a.o_step;
 #pragma unroll
         for (int m = 0; m < D / 32; ++m)
@@ -594,13 +603,13 @@ struct Grads {
     float scale;
 };
 
-// Weights and their gradients on their way into the matrix instructions.  bfloat16 has the range of 32 bits.  In float16 weights go in
-// times 2^12 (they are normal numbers down to 2^-26: 10^5 equal ones of a row are still rounded to 2^-11 of themselves), and
-// gradients times a power of two taken from the largest norms: |P (dP - D)| <= 2 |dO_i| |v_j|, which is brought to 2^14 at most.
+// Weights and their gradients on their way into the matrix instructions.  In float16 weights go in times 2^12 as in the forward pass
+// (10^5 equal ones of a row are still rounded to 2^-11 of themselves), and gradients times a power of two taken from the largest
+// norms: |P (dP - D)| <= 2 |dO_i| |v_j|, which is brought to 2^14 at most.
 constexpr int kPeaks = 512;
 template <typename T> struct Range {
-    static constexpr bool kNarrow = sizeof(T) == 2 && __is_same(T, _Float16);
-    static constexpr float kShift = kNarrow ? 12.0f : 0.0f, kWeight = kNarrow ? 0.000244140625f : 1.0f;
+    static constexpr bool kNarrow = Weights<T>::kNarrow;
+    static constexpr float kShift = Weights<T>::kShift, kWeight = kNarrow ? 0.000244140625f : 1.0f;
     float factor = 1;                // of dP - D where a weight carries 2^kShift
     __device__ __forceinline__ explicit Range(const float *peaks) {
         if constexpr (kNarrow) {

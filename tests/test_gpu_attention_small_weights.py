@@ -40,7 +40,7 @@ def _run(harp, kind, head, tokens, heads, scores, values):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("place", ["first", "middle", "last"])
-@pytest.mark.parametrize("kind,head", [("bfloat16", 64), ("bfloat16", 96), ("bfloat16", 128)])
+@pytest.mark.parametrize("kind,head", [("float16", 64), ("float16", 96), ("float16", 128), ("bfloat16", 128)])
 @pytest.mark.parametrize("above", [12.0, 15.0, 17.0])
 def test_one_key_far_above_the_others(harp, above, kind, head, place):
     """e^-12, e^-15 and e^-17 are 2^-17.3, 2^-21.6 and 2^-24.5.  The key above has a value of 0, so that the result is the others'; all rows
