@@ -13,9 +13,11 @@
 #include <utility>
 
 #include "harp_ctx.h"
+#include "op_attention_plan.h"
 #include "ops_common.h"
 
 using namespace harp;
+using namespace harp::attention;
 using namespace harp::ops;
 
 namespace {
@@ -37,8 +39,6 @@ template <> struct Mfma32<_Float16> {
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kKeys = 64;            // keys of a tile in LDS
-constexpr int kDies = 8;
 
 // What the kernels know of a call.
 struct Call {
@@ -300,6 +300,7 @@ template <typename T> struct Weights {
 struct Shares {
     int count, paired;
     float *sums, *stats;
+    int first_kv, kv_heads;          // of this launch
 };
 
 // One pass over the keys with the running reference and sum of a softmax: o = sum of 2^(c s - top) v, sum likewise, both times
@@ -538,16 +539,15 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, S
             }
     };
     // Tiles of rows that see most keys first; with shares.paired a workgroup takes one of them and one of the least in turn.
-    const Work work = work_of(blockIdx.x, shares.paired ? (tiles + 1) / 2 : tiles, a.kv_heads, shares.count, a.causal);
+    const Work work = work_of(blockIdx.x, shares.paired ? (tiles + 1) / 2 : tiles, shares.kv_heads, shares.count, a.causal);
 #pragma unroll 1
     for (int turn = 0; turn < (shares.paired && work.place != tiles - 1 - work.place ? 2 : 1); ++turn) {
         if (turn) __syncthreads();               // all have read what lies in LDS
-        one(work.share, work.kv, turn ? work.place : tiles - 1 - work.place);
+        one(work.share, shares.first_kv + work.kv, turn ? work.place : tiles - 1 - work.place);
     }
 }
 
 // Shares of the keys, joined: 32 lanes a row of four channels each, rows of sequences only.
-constexpr int kJoinRows = 8;
 template <typename T> __global__ __launch_bounds__(kJoinRows * 32) void forward_join(Call a, int tiles, Shares shares) {
     int b, tile;
     if (!locate(a.q_begin, a.tokens_q, a.batch, a.group, kJoinRows, blockIdx.x % tiles, b, tile)) return;
@@ -822,11 +822,11 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g
             }
     };
     // Tiles of rows that see most keys first; with shares.paired a workgroup takes one of them and one of the least in turn.
-    const Work work = work_of(blockIdx.x, shares.paired ? (tiles + 1) / 2 : tiles, a.kv_heads, shares.count, a.causal);
+    const Work work = work_of(blockIdx.x, shares.paired ? (tiles + 1) / 2 : tiles, shares.kv_heads, shares.count, a.causal);
 #pragma unroll 1
     for (int turn = 0; turn < (shares.paired && work.place != tiles - 1 - work.place ? 2 : 1); ++turn) {
         if (turn) __syncthreads();               // all have read what lies in LDS
-        one(work.share, work.kv, turn ? work.place : tiles - 1 - work.place);
+        one(work.share, shares.first_kv + work.kv, turn ? work.place : tiles - 1 - work.place);
     }
 }
 
@@ -851,7 +851,6 @@ __device__ __forceinline__ void word_to_lds(const float *from, uint32_t to) {
 // that nothing is added up in memory but shares.  4,096 queries and keys, 32 heads of 128, bfloat16, not causal: 530 us (1,040 TFLOP/s of
 // its four products), matrix units busy 51%; causal 295.  Bound as the forward pass, and by registers: with five of them spilled,
 // whose reloads wait for the rows on their way, it took 590.
-constexpr int kBack = 32;
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, int tiles, Shares shares) {
     constexpr int kThreads = WAVES * kWave, kCols = WAVES * 32;
@@ -860,8 +859,8 @@ __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, i
     __shared__ __align__(1024) T lv[kCols * D];
     __shared__ __align__(16) float l_stat[2][2 * kBack];          // against and delta of a step's rows
     __shared__ __align__(16) int l_limit[2][kBack];
-    const Work work = work_of(blockIdx.x, tiles, a.kv_heads, shares.count, a.causal);
-    const int share = work.share, kv = work.kv;
+    const Work work = work_of(blockIdx.x, tiles, shares.kv_heads, shares.count, a.causal);
+    const int share = work.share, kv = shares.first_kv + work.kv;
     int b, tile;
     if (!locate(a.k_begin, a.tokens_k, a.batch, 1, kCols, work.place, b, tile)) return;
     const Sequence s = sequence(a, b);
@@ -1036,73 +1035,6 @@ __global__ __launch_bounds__(kJoinRows * 32) void join_sums(const int32_t *begin
 }
 
 // ---------------------------------------------------------------------------------------------- on the host
-bool sizes_fit(const harp_attention *g) {
-    const int64_t most = (int64_t(1) << 30) - 1;
-    return g->tokens_q >= 0 && g->tokens_k >= 0 && g->tokens_q <= most && g->tokens_k <= most && g->batch >= 1 && g->batch <= 1 << 20 &&
-           g->heads >= 1 && g->heads <= 1 << 14 && g->kv_heads >= 1 && g->heads % g->kv_heads == 0 && g->head >= 8 && g->head % 8 == 0 &&
-           g->head <= HARP_ATTENTION_MAX_HEAD && g->tokens_q * (g->heads / g->kv_heads) <= most;
-}
-
-// How the passes are launched; of sizes that the host knows.  With begins on the device a pass has room for a partial tile
-// of every sequence.
-struct Plan {
-    int waves;                       // of a workgroup
-    int64_t tiles;                   // of rows, or of keys
-    int shares;                      // of what a tile goes through
-    bool paired;                     // a workgroup takes two tiles
-    int64_t places() const { return paired ? (tiles + 1) / 2 : tiles; }
-};
-int64_t tiles_of(int64_t tokens, int64_t times, int batch, int side) {
-    const int64_t whole = tokens * times / side, each = (tokens / batch * times + side - 1) / side * batch;
-    // equal lengths need `each`; begins on the device at most this
-    return whole + batch > each ? whole + batch : each;
-}
-// Microseconds by what was measured: `step` for a tile of 256 by the 64 (32) rows that go through LDS at a time with 128 channels, 6
-// around them.  Tiles of 128 are two to a compute unit, at the same pace where both are there.  `bytes` that a share's sums take
-// are written and read by a launch more.  The `through` rows are shared out where tiles are few, or, under the causal order, differ.
-Plan plan_for(const harp_ctx *ctx, int64_t tokens, int64_t times, int batch, int kv_heads, int64_t through, int unit, double step, int head,
-              double bytes, bool causal, bool may_pair) {
-    Plan best = {};
-    double least = 1e300;
-    const double channels = head <= 64 ? 0.5 : head <= 96 ? 0.75 : 1.0;
-    const int64_t rows = tokens * times / batch;
-    for (int waves = 8; waves >= 4; waves -= 4) {
-        const int64_t side = 32 * waves, slots = int64_t(ctx->n_cu) * 8 / waves;
-        const int64_t busy = (rows > side ? (rows + side - 1) / side : 1) * batch * kv_heads;       // tiles that have something to do
-        for (int shares : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            if (shares > 1 && through < int64_t(shares) * unit) break;
-            const int64_t items = busy * shares;
-            const double steps = double((through + unit - 1) / unit) / shares;
-            const double each = step * channels * (waves == 4 && items <= ctx->n_cu ? 0.6 : 1.0);
-            const int64_t rounds = (items + slots - 1) / slots, pairs = (items + 1) / 2, pair_rounds = (pairs + slots - 1) / slots;
-            const double alone = steps * each + 6;
-            double us = double(rounds) * alone;
-            bool paired = false;
-            if (causal) {
-                // heavy tiles first; workgroups are handed to shader engines in turn and wait for their own, so that they do not
-                // even out.  A heavy and a light one in one workgroup are alike.
-                const double spread = 1.25 * double(items) / double(slots) * (steps * each / 2 + 6);
-                us = alone > spread ? alone : spread;
-                const double both = double(pair_rounds) * (steps * each + 12);
-                if (may_pair && both < us) us = both, paired = true;
-            }
-            if (shares > 1) us += 8 + shares * bytes * 2 / 4e6;
-            if (waves == 4) us *= 1.1;                           // keys are read twice as often
-            if (us < least) least = us, best = Plan{waves, tiles_of(tokens, times, batch, int(side)), shares, paired};
-        }
-    }
-    return best;
-}
-Plan plan_queries(const harp_ctx *ctx, const harp_attention *g, bool causal) {
-    const int group = g->heads / g->kv_heads;
-    return plan_for(ctx, g->tokens_q, group, g->batch, g->kv_heads, g->tokens_k / g->batch, kKeys, 2.4, g->head,
-                    double(g->tokens_q) * g->heads * g->head * 4, causal, true);
-}
-Plan plan_keys(const harp_ctx *ctx, const harp_attention *g, bool causal) {
-    return plan_for(ctx, g->tokens_k, 1, g->batch, g->kv_heads, g->tokens_q / g->batch * (g->heads / g->kv_heads), kBack, 2.4, g->head,
-                    double(g->tokens_k) * g->kv_heads * g->head * 8, causal, false);
-}
-
 // Where parts of the workspace begin; what the passes need of these plans.
 struct Space { size_t peaks, stats, sums, all; };
 Space space_for(const harp_attention *g, const Plan *q, const Plan *k) {
@@ -1155,20 +1087,14 @@ int check(harp_ctx *ctx, const harp_attention *g, const Tensor *t, int count, co
             if (j != i && t[j].p == t[i].p && t[i].tokens > 0 && t[j].tokens > 0)
                 return fail(ctx, HARP_ERR_INVALID_ARG, "%s is %s", t[i].name, t[j].name);
     }
-    *q = plan_queries(ctx, g, g->causal);
-    if (k) *k = plan_keys(ctx, g, g->causal);
+    *q = plan_queries(ctx->n_cu, g, g->causal);
+    if (k) *k = plan_keys(ctx->n_cu, g, g->causal);
     *space = space_for(g, q, k);
     const size_t need = space->all;
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < need)
         return fail(ctx, HARP_ERR_WORKSPACE, "the workspace needs %zu bytes, aligned to 256", need);
-    const int64_t grid = int64_t(1) << 23, half = int64_t(1) << 31;       // a launch has less than 2^32 threads
-    bool fits = q->places() * q->shares * g->kv_heads < grid && tiles_of(g->tokens_q, g->heads, g->batch, kMeasured) < half &&
-                tiles_of(g->tokens_k, g->kv_heads, g->batch, kMeasured) < half;
-    if (q->shares > 1)
-        fits = fits && tiles_of(g->tokens_q, g->heads, g->batch, kJoinRows) < grid &&
-               tiles_of(g->tokens_q, g->heads / g->kv_heads, g->batch, kJoinRows) * g->kv_heads < grid;
-    if (k) fits = fits && k->places() * k->shares * g->kv_heads < grid;
-    if (k && k->shares > 1) fits = fits && tiles_of(g->tokens_k, g->kv_heads, g->batch, kJoinRows) < grid;
+    const int64_t half = int64_t(1) << 31;
+    const bool fits = tiles_of(g->tokens_q, g->heads, g->batch, kMeasured) < half && tiles_of(g->tokens_k, g->kv_heads, g->batch, kMeasured) < half;
     if (!fits)
         return fail(ctx, HARP_ERR_SHAPE, "too many rows for one launch");
     const hipError_t e = hipSetDevice(ctx->device);
@@ -1193,31 +1119,43 @@ int launched(harp_ctx *ctx) {
     return e == hipSuccess ? HARP_OK : hip_fail(ctx, e, "launching the attention's kernels");
 }
 
-template <typename T, int D> void launch_forward(const Plan &p, const Call &a, const Shares &shares, hipStream_t st) {
-    const dim3 grid(uint32_t(p.places() * p.shares * a.kv_heads));
-    if (p.waves == 8) forward<T, D, 8><<<grid, dim3(512), 0, st>>>(a, int(p.tiles), shares);
-    else forward<T, D, 4><<<grid, dim3(256), 0, st>>>(a, int(p.tiles), shares);
+// A pass in as many launches as its kv heads take: one, but for a great many short sequences.
+template <typename L> void over_heads(const Plan &p, int kv_heads, Shares shares, L launch) {
+    const int most = int(p.heads_of_a_launch(kv_heads));
+    for (int first = 0; first < kv_heads; first += most) {
+        shares.first_kv = first;
+        shares.kv_heads = kv_heads - first < most ? kv_heads - first : most;
+        launch(dim3(uint32_t(p.places() * p.shares * shares.kv_heads)), shares);
+    }
 }
-template <typename T, int D> void launch_queries(const Plan &p, const Call &a, const Grads &g, const Shares &shares, hipStream_t st) {
-    const dim3 grid(uint32_t(p.places() * p.shares * a.kv_heads));
-    if (p.waves == 8) grad_queries<T, D, 8><<<grid, dim3(512), 0, st>>>(a, g, int(p.tiles), shares);
-    else grad_queries<T, D, 4><<<grid, dim3(256), 0, st>>>(a, g, int(p.tiles), shares);
+template <typename T, int D> void launch_forward(const Plan &p, const Call &a, const Shares &all, hipStream_t st) {
+    over_heads(p, a.kv_heads, all, [&](dim3 grid, const Shares &shares) {
+        if (p.waves == 8) forward<T, D, 8><<<grid, dim3(512), 0, st>>>(a, int(p.tiles), shares);
+        else forward<T, D, 4><<<grid, dim3(256), 0, st>>>(a, int(p.tiles), shares);
+    });
 }
-template <typename T, int D> void launch_keys(const Plan &p, const Call &a, const Grads &g, const Shares &shares, hipStream_t st) {
-    const dim3 grid(uint32_t(p.places() * p.shares * a.kv_heads));
-    if (p.waves == 8) grad_keys<T, D, 8><<<grid, dim3(512), 0, st>>>(a, g, int(p.tiles), shares);
-    else grad_keys<T, D, 4><<<grid, dim3(256), 0, st>>>(a, g, int(p.tiles), shares);
+template <typename T, int D> void launch_queries(const Plan &p, const Call &a, const Grads &g, const Shares &all, hipStream_t st) {
+    over_heads(p, a.kv_heads, all, [&](dim3 grid, const Shares &shares) {
+        if (p.waves == 8) grad_queries<T, D, 8><<<grid, dim3(512), 0, st>>>(a, g, int(p.tiles), shares);
+        else grad_queries<T, D, 4><<<grid, dim3(256), 0, st>>>(a, g, int(p.tiles), shares);
+    });
+}
+template <typename T, int D> void launch_keys(const Plan &p, const Call &a, const Grads &g, const Shares &all, hipStream_t st) {
+    over_heads(p, a.kv_heads, all, [&](dim3 grid, const Shares &shares) {
+        if (p.waves == 8) grad_keys<T, D, 8><<<grid, dim3(512), 0, st>>>(a, g, int(p.tiles), shares);
+        else grad_keys<T, D, 4><<<grid, dim3(256), 0, st>>>(a, g, int(p.tiles), shares);
+    });
 }
 
 template <typename T> void run_forward(const harp_attention *g, const Plan &p, const Space &space, unsigned char *ws, hipStream_t st) {
     const Call a = call_of(g);
-    const Shares shares = {p.shares, p.paired, reinterpret_cast<float *>(ws + space.sums), reinterpret_cast<float *>(ws + space.stats)};
+    const Shares shares = {p.shares, p.paired, reinterpret_cast<float *>(ws + space.sums), reinterpret_cast<float *>(ws + space.stats), 0, 0};
     if (g->head <= 64) launch_forward<T, 64>(p, a, shares, st);
     else if (g->head <= 96) launch_forward<T, 96>(p, a, shares, st);
     else launch_forward<T, 128>(p, a, shares, st);
     if (p.shares > 1) {
         const int64_t tiles = tiles_of(g->tokens_q, a.group, g->batch, kJoinRows);
-        forward_join<T><<<dim3(uint32_t(tiles * a.kv_heads)), dim3(kJoinRows * 32), 0, st>>>(a, int(tiles), shares);
+        forward_join<T><<<dim3(uint32_t(query_joins(g))), dim3(kJoinRows * 32), 0, st>>>(a, int(tiles), shares);
     }
 }
 
@@ -1234,7 +1172,7 @@ void run_backward(const harp_attention *g, const harp_attention_grads *d, const 
     measure<T><<<dim3(Range<T>::kNarrow ? 2 * kPeaks : groups), dim3(256), 0, st>>>(a, grads, of_q, of_k, groups);
     if (d->dQ && rows) {
         const Plan &p = of_queries;
-        const Shares shares = {p.shares, p.paired, sums, nullptr};
+        const Shares shares = {p.shares, p.paired, sums, nullptr, 0, 0};
         if (g->head <= 64) launch_queries<T, 64>(p, a, grads, shares, st);
         else if (g->head <= 96) launch_queries<T, 96>(p, a, grads, shares, st);
         else launch_queries<T, 128>(p, a, grads, shares, st);
@@ -1244,7 +1182,7 @@ void run_backward(const harp_attention *g, const harp_attention_grads *d, const 
     }
     if ((d->dK || d->dV) && g->tokens_k) {
         const Plan &p = of_keys;
-        const Shares shares = {p.shares, p.paired, sums, nullptr};
+        const Shares shares = {p.shares, p.paired, sums, nullptr, 0, 0};
         if (g->head <= 64) launch_keys<T, 64>(p, a, grads, shares, st);
         else if (g->head <= 96) launch_keys<T, 96>(p, a, grads, shares, st);
         else launch_keys<T, 128>(p, a, grads, shares, st);
@@ -1265,7 +1203,7 @@ size_t harp_attention_workspace_bytes(harp_ctx *ctx, const harp_attention *g) {
     if (!ctx || !g || attention_sizes(ctx, g) != HARP_OK) return 0;
     size_t most = 0;
     for (int causal = 0; causal < 2; ++causal) {
-        const Plan q = plan_queries(ctx, g, causal), k = plan_keys(ctx, g, causal);
+        const Plan q = plan_queries(ctx->n_cu, g, causal), k = plan_keys(ctx->n_cu, g, causal);
         const size_t all = space_for(g, &q, &k).all;
         most = all > most ? all : most;
     }
