@@ -22,8 +22,6 @@ using namespace harp::ops;
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
@@ -1056,12 +1054,6 @@ int attention_sizes(harp_ctx *ctx, const harp_attention *g) {
 }
 
 struct Tensor { const char *name; const void *p; int64_t tokens, heads, token, step; bool needed, written; };
-bool clear_of_each_other(int64_t tokens, int64_t heads, int64_t head, int64_t token, int64_t step) {
-    typedef __int128 Wide;
-    const bool in_token = (heads <= 1 || step >= head) && (tokens <= 1 || token >= Wide(heads - 1) * step + head);
-    const bool in_head = (tokens <= 1 || token >= head) && (heads <= 1 || step >= Wide(tokens - 1) * token + head);
-    return in_token || in_head;
-}
 
 // q, k: how the call is launched; k is null in the forward pass.
 int check(harp_ctx *ctx, const harp_attention *g, const Tensor *t, int count, const void *workspace, size_t workspace_bytes, Plan *q, Plan *k,

@@ -13,9 +13,6 @@ namespace {
 using namespace harp;
 using namespace harp::ops;
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-
 template <typename T> struct Mfma;
 template <> struct Mfma<__bf16> {
     typedef bf16x8 Frag;

@@ -118,15 +118,6 @@ __global__ __launch_bounds__(256) void turn(Rotary r, const T *x, T *y, int piec
     }
 }
 
-// Whether rows of `head` elements, `heads` of them `step` apart for each of `tokens` that are `token` apart, lie clear of each
-// other: heads inside a token, or tokens inside a head.
-bool clear_of_each_other(int64_t tokens, int64_t heads, int64_t head, int64_t token, int64_t step) {
-    typedef __int128 Wide;
-    const bool in_token = (heads <= 1 || step >= head) && (tokens <= 1 || token >= Wide(heads - 1) * step + head);
-    const bool in_head = (tokens <= 1 || token >= head) && (heads <= 1 || step >= Wide(tokens - 1) * token + head);
-    return in_token || in_head;
-}
-
 template <typename T> void launch(const harp_ctx *ctx, const harp_rotary_args *g, hipStream_t st) {
     const bool copy = g->X != g->Y && g->turned < g->head;
     const Rotary r = {g->tokens, g->x_token, g->x_step, g->y_token, g->y_step, g->first, g->period, g->heads, g->head, g->turned,

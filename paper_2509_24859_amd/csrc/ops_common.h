@@ -14,6 +14,8 @@ constexpr int kWave = 64;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // Elements as they are stored and as they are computed with.  Conversions round to nearest, ties to even.
 __device__ __forceinline__ float to_f32(float x) { return x; }
@@ -76,6 +78,15 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t x) {
 inline int type_bytes(int type) { return type == HARP_F32 ? 4 : type == HARP_BF16 || type == HARP_F16 ? 2 : 0; }
 inline bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+// Whether rows of `head` elements, `heads` of them `step` apart for each of `tokens` that are `token` apart, lie clear of each
+// other: heads inside a token, or tokens inside a head.
+inline bool clear_of_each_other(int64_t tokens, int64_t heads, int64_t head, int64_t token, int64_t step) {
+    typedef __int128 Wide;
+    const bool in_token = (heads <= 1 || step >= head) && (tokens <= 1 || token >= Wide(heads - 1) * step + head);
+    const bool in_head = (tokens <= 1 || token >= head) && (heads <= 1 || step >= Wide(tokens - 1) * token + head);
+    return in_token || in_head;
+}
 
 }  // namespace ops
 }  // namespace harp
