@@ -642,9 +642,11 @@ int harp_rotary_frequencies(int32_t turned, double base, int32_t scaling, double
  * Sequence b has queries q_begin[b] .. q_begin[b + 1] - 1 of tokens_q, and keys k_begin[b] .. k_begin[b + 1] - 1 of tokens_k, of
  * which it uses the first k_count[b] (NULL: all).  Where a begin is NULL the sequences have tokens / batch each.  With Lq
  * queries and Lk used keys, i sees all of them, or with causal not 0 those j <= i + Lk - Lq: the last query sees all.  A query
- * that sees no key (or whose scores are all -infinity) has o = 0, lse = -infinity, and no part in any gradient.  Keys that are not
- * used are not read into any result, whatever they hold.  A key or value that is not finite and hidden by the causal order alone
- * may make results of a query that sees other keys NaN, and a query or gradient of it the gradients of keys hidden from it.
+ * that sees no key has o = 0, lse = -infinity, and no part in any gradient, whatever it holds.  One whose scores are all -infinity
+ * has o = 0, lse = -infinity and dQ = 0, and where it, its row of dO and a key and value are finite no part in their gradients.
+ * Gradients of a key or value that is not finite may be NaN.  Keys that are not used are not read into any result, whatever they
+ * hold.  A key or value that is not finite and hidden by the causal order alone may make results of a query that sees other keys
+ * NaN, and a query that is not finite, or whose row of dO is not, the gradients of keys hidden from it.
  * What a pass writes lies over nothing else that it reads or writes.
  * Q and O [tokens_q][heads][head], K and V [tokens_k][kv_heads][head], of `type` (HARP_BF16 or HARP_F16), element (t, h, c) at
  * t * token + h * step + c.  lse: float [heads][tokens_q], or NULL in the forward pass.  0 < scale < 2^127.
