@@ -651,7 +651,8 @@ int harp_rotary_frequencies(int32_t turned, double base, int32_t scaling, double
  * Q and O [tokens_q][heads][head], K and V [tokens_k][kv_heads][head], of `type` (HARP_BF16 or HARP_F16), element (t, h, c) at
  * t * token + h * step + c.  lse: float [heads][tokens_q], or NULL in the forward pass.  0 < scale < 2^127.
  * Begins and counts are DEVICE int32, read when the kernels run, so that a captured call takes those of each replay; begins rise
- * and end within tokens; whatever they hold, nothing outside the tensors is touched.  Rows of no sequence are left as they were.
+ * and end within tokens; whatever they hold, nothing outside the tensors is touched.  Work is dealt out by what the host knows,
+ * tokens / batch: sequences much longer than that take their time alone.  Rows of no sequence are left as they were.
  * Scores, weights' sums and all sums over keys or queries are in 32 bits; weights and their gradients are rounded to `type`
  * where they are multiplied with V, K, Q and dO (what the matrix instructions take; in HARP_F16 weights times 2^12, so that
  * those below 2^-37 of a row's largest are lost, and their gradients times a power of two that keeps them from both ends of its range).

@@ -140,8 +140,8 @@ __device__ __forceinline__ bool locate(const int32_t *begin, int64_t tokens, int
 // with an L2 of its own: a die takes neighbours, which share keys.  Within a die they go to its shader engines in turn, and wait
 // for room in that one: under the causal order, where tiles differ in their work, the same place of each head comes first, then the
 // next, so that every engine has tiles of all weights and those that follow find room where the lightest end (gradients of
-// 4,096 keys, 32 heads: 332 us, heads one after the other 448; 4 heads of 96, 2 sequences: 307 and 491).  A die takes
-// whole heads where they can be dealt out.
+// 4,096 keys, 32 heads, when this was made: 332 us, heads one after the other 448; 4 heads of 96, 2 sequences: 307 and 491).
+// A die takes whole heads where they can be dealt out.
 struct Work { int share, kv, place; };
 __device__ __forceinline__ Work work_of(int id, int places, int kv_heads, int shares, bool causal) {
     Work w;
@@ -304,10 +304,12 @@ struct Shares {
 // One pass over the keys with the running reference and sum of a softmax: o = sum of 2^(c s - top) v, sum likewise, both times
 // 2^(top before - top) when the reference grows.  WAVES wavefronts of 32 rows; keys go through LDS 64 at a time, two tiles of them, in
 // steps of 32.  8 wavefronts read a key from L2 once for 256 rows; 4 where rows are few.
-// 4,096 queries and keys, 32 heads of 128, bfloat16: 256 us, 1,070 TFLOP/s, matrix units busy 56% of the cycles; causal 148 to
-// 162.  What bounds it: a tile's 32 matrix instructions of a wavefront take 1,024 cycles, its 175 vector instructions some 800 that a SIMD's
-// two wavefronts do not fully hide.  LDS, 256 bytes a cycle, is busy a third.  One token of 16 sequences, 174,103 keys in all, 8 heads
-// of 128: 152 us, 4.7 TB/s.
+// 4,096 queries and keys, 32 heads of 128, bfloat16: 255 to 268 us by the card, 1,025 to 1,078 TFLOP/s, matrix units busy 56% of the
+// cycles; causal 146 to 162.  What bounds it: a tile's 32 matrix instructions of a wavefront take 1,024 cycles, its 179 vector
+// instructions some 800, and 56% is what one after the other gives: a SIMD's two wavefronts hardly have the one's beside the other's.
+// LDS, 256 bytes a cycle, is busy a third.  One token of 16 sequences, 174,103 keys in all, 8 heads of 128: 151 us, 4.7 TB/s, where
+// reading reaches 6.1: shares are as many for each sequence, the longest's are the last.  With 4 wavefronts and 128 channels 11
+// registers are spilled, outside the loop of whole tiles.
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void forward(Call a, int tiles, Shares shares) {
     constexpr int kThreads = WAVES * kWave, kRows = WAVES * 32;
@@ -685,7 +687,8 @@ __global__ __launch_bounds__(256) void measure(Call a, Grads g, int of_q, int of
 }
 
 // dQ, as the forward pass goes: dQ^T = K^T dS^T, dS^T = P^T (V dO^T - delta).  4,096 queries and keys, 32 heads of 128, not causal: 350 us
-// (1,180 TFLOP/s of its three products), causal 205.  Bound as the forward pass.
+// (1,180 TFLOP/s of its three products), causal 205 to 215.  Bound as the forward pass.  With 128 channels 3 and 7 registers (bfloat16,
+// float16) are spilled by 8 wavefronts, 16 and 23 by 4.
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void grad_queries(Call a, Grads g, int tiles, Shares shares) {
     constexpr int kThreads = WAVES * kWave, kRows = WAVES * 32;
@@ -847,8 +850,9 @@ __device__ __forceinline__ void word_to_lds(const float *from, uint32_t to) {
 // dK and dV of 32 keys a wavefront, whose rows come through LDS kBack at a time.  dV^T = dO^T P, dK^T = Q^T dS, where a lane has
 // 16 rows of one key: both sums of a wavefront stay in registers over all rows and heads of the group, 128 of 256 with 128 channels, so
 // that nothing is added up in memory but shares.  4,096 queries and keys, 32 heads of 128, bfloat16, not causal: 530 us (1,040 TFLOP/s of
-// its four products), matrix units busy 51%; causal 295.  Bound as the forward pass, and by registers: with five of them spilled,
-// whose reloads wait for the rows on their way, it took 590.
+// its four products), matrix units busy 51%; causal 310 to 330.  Bound as the forward pass, and by registers: with five of them spilled,
+// whose reloads wait for the rows on their way, it took 590.  8 wavefronts spill none; 4, which take few keys, spill 9 and 10 with 128
+// channels (bfloat16, float16), one or two of them reloaded every step.
 template <typename T, int D, int WAVES>
 __global__ __launch_bounds__(WAVES * kWave, 2) void grad_keys(Call a, Grads g, int tiles, Shares shares) {
     constexpr int kThreads = WAVES * kWave, kCols = WAVES * 32;

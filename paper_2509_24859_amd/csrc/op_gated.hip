@@ -6,7 +6,8 @@
 //
 // 4,096 tokens, W [24576][4096], bfloat16, SiLU, Z kept: 656 to 680 us, 1,210 to 1,257 TFLOP/s (a library product of these sizes
 // alone reaches 1,457); without the way through one kernel, Z would be written and read again, 600 MB, 120 us.  Back through W2
-// [4096][12288] and the gate with H made again: 425 us, 970 TFLOP/s.  One token: 32 us in the kernel, 6.3 TB/s of weights.  What bounds
+// [4096][12288] and the gate with H made again: 425 us, 970 TFLOP/s.  One token: 32 us in the kernel, 6.3 TB/s of weights, which the last cache
+// partly holds (1 to 4 GiB of them: 5.3 to 5.7 TB/s).  What bounds
 // the tiles is what bounds harp_linear's: bringing operands into LDS, and the epilogue's stores.
 #include "op_product.h"
 
